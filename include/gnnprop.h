@@ -383,6 +383,135 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
                          float* v, double lr, double beta1, double beta2,
                          double eps, int32_t t, hipStream_t stream);
 
+/* ------------------------------- policy loss, clipping, update of many tensors */
+
+/* Networks trained as policies: row i (a node, or a whole graph) chooses one
+ * of C actions from the logits Z (n x C, stride ld_z), e.g. gnn_gemm's
+ * product of the stack's output with a head's weights.
+ *   lp_i = Z[i, a_i] - log sum_j exp Z[i, j]
+ * action: n int32.  A row whose action lies outside [0, C) is left out: its
+ * logits are not used (they may hold anything), its lp is written as 0 and
+ * its gradient as 0.  Logits of -inf take an action out of a row's choice; a
+ * row with every logit -inf is left out too, with lp = -inf.  Sums of
+ * exponentials, logarithms and the loss are formed in double.
+ *
+ * gnn_action_logp writes lp (n floats): what acting needs, and the old_logp /
+ * ref_logp that gnn_policy_loss takes.
+ *
+ * gnn_policy_loss: the clipped surrogate loss with a KL term, and its
+ * gradient, with
+ *   rho_i = exp(lp_i - old_logp_i)          (old_logp NULL: old_logp = lp)
+ *   d_i   = ref_logp_i - lp_i,  kl_i = exp(d_i) - d_i - 1 >= 0
+ *           (an unbiased sample of KL(policy || reference); ref_logp NULL: 0)
+ *   l_i   = -min(rho_i A_i, clip(rho_i, 1 - clip_lo, 1 + clip_hi) A_i)
+ *           + beta kl_i
+ *   out   = [ sum_i w_i l_i,  sum_i w_i kl_i,  sum_i w_i 1[i is clipped] ]
+ *   dZ[i, j] = w_i (dl_i / dlp_i) (1[j = a_i] - exp(Z[i, j]) / sum exp)
+ *   dl_i / dlp_i = -A_i rho_i 1[i is not clipped] + beta (1 - exp(d_i))
+ * where i is clipped if rho_i A_i > clip(rho_i, ...) A_i (decided in double).
+ * advantage A, old_logp, ref_logp and weight w are n floats; weight NULL:
+ * 1/n.  A row of weight 0 adds nothing and has a gradient of 0, whatever its
+ * logits.  A chosen action with a logit of -inf has lp = -inf: its kl is
+ * infinite, and its gradient not finite where beta > 0.  0 <= clip_lo <= 1,
+ * clip_hi >= 0 (infinity: no upper clip), beta finite >= 0, needing ref_logp
+ * where beta > 0 (else GNN_ERR_SHAPE / GNN_ERR_NULL).
+ * out: three floats.  logp (n floats) and dZ (n x C, stride ld_dz) may be
+ * NULL.  Columns of dZ's rows past C are not written.  Everything is summed
+ * in a fixed order (bit-reproducible).  n = 0 gives out = 0.  No output may
+ * overlap an input, another output or the workspace
+ * (gnn_policy_workspace_bytes, for both calls). */
+size_t gnn_policy_workspace_bytes(int32_t n, int32_t C);
+gnn_status gnn_action_logp(int32_t n, int32_t C, const float* Z, int64_t ld_z,
+                           const int32_t* action, float* logp, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
+                           const int32_t* action, const float* advantage,
+                           const float* old_logp, const float* ref_logp,
+                           const float* weight, double clip_lo, double clip_hi,
+                           double beta, float* out, float* logp, float* dZ,
+                           int64_t ld_dz, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/* A set of tensors that are updated together (all weights of a model), each
+ * of `count` contiguous elements (count 0: nothing).
+ *   W, G     weights and gradients (device, 4-byte aligned; gradients may be
+ *            shared by several tensors)
+ *   m, v     Adam's moments: state_bits 32: floats; state_bits 8: one byte
+ *            each, m in OCP e4m3 and v in OCP e5m2, times the scale of its
+ *            block of 256 consecutive elements
+ *   m_scale, v_scale  state_bits 8: ceil(count / 256) floats each; state_bits
+ *            32: not used
+ *   weight_decay      of this tensor (0 for biases, say)
+ * Moments start as zeros (scales too).  16-byte aligned W, G, m, v (8-bit
+ * moments: 4-byte) enable the vector paths.  gnn_grad_norm alone needs only
+ * count and G: W, m, v and the scales may then be NULL. */
+typedef struct gnn_param {
+  int64_t count;
+  float* W;
+  const float* G;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  double weight_decay;
+} gnn_param;
+#define GNN_STATE_BLOCK 256 /* elements that share a scale of 8-bit moments */
+
+/* n tensors (host array p) with state_bits 32 or 8 and, for the calls below,
+ * `plan`: the device buffer that gnn_params_build_plan filled for exactly
+ * these tensors (pointers, counts, decay). */
+typedef struct gnn_params {
+  int32_t n;
+  int32_t state_bits;
+  const gnn_param* p;
+  const void* plan;
+} gnn_params;
+
+/* Bytes of the plan, and its filling (a device buffer of at least that size,
+ * 16-byte aligned): a table of the tensors and of the pieces of 2,048
+ * elements that one workgroup takes, so that one launch covers every tensor.
+ * Nothing is read from the host after the call returns.  No W, m, v or scale
+ * may overlap anything else in the set or the plan (GNN_ERR_ALIAS).
+ * params->plan is not read. */
+size_t gnn_params_plan_bytes(const gnn_params* params);
+gnn_status gnn_params_build_plan(const gnn_params* params, void* plan,
+                                 size_t plan_bytes, hipStream_t stream);
+
+/* norm (one device float) = square root of the sum of squares of every
+ * gradient of the set, squares and sums in double, in a fixed order. */
+size_t gnn_grad_norm_workspace_bytes(const gnn_params* params);
+gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream);
+
+/* AdamW step t >= 1 on every tensor of the set, one launch:
+ *   g = k G;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
+ *   W = (1 - lr weight_decay) W
+ *       - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
+ * norm: device float (gnn_grad_norm's) or NULL.  NULL: k = 1.  Else
+ * k = max_norm / norm where norm > max_norm (max_norm > 0) and 1 elsewhere,
+ * and a norm that is not finite skips the step: nothing is changed.
+ * Without norm a NaN or infinite gradient makes its own weight and moments
+ * non-finite, with 8-bit moments those of its whole block of 256.
+ * Hyperparameters are host values, taken at the call (a captured launch
+ * replays with them): 0 <= beta1, beta2 < 1, eps >= 0, lr finite.
+ *
+ * 8-bit moments: m, v and the update are formed from unrounded new moments
+ * (in double), which are then stored with scale = max over the block / 448
+ * (m) or / 57344 (v), at least 2^-126, and rounded stochastically: up with
+ * the probability of their distance from the lower neighbour.  An average
+ * with b2 = 0.999 moves by 0.1 % a step where e5m2's neighbours are 14 to
+ * 25 % apart: rounding to nearest would hold it where it is, stochastic
+ * rounding keeps its expectation.  A positive v is never stored as 0 (its
+ * weight's next step would be divided by a root that is too small).  Element
+ * e of a tensor whose predecessors in the set hold B blocks of 256 takes bits
+ * of output (256 B + e) / 2 of the SplitMix64 generator started at output t
+ * of the one started at `seed` (the lower 32 bits for even e: the lower 16 of
+ * them for m, the upper 16 for v; r stands for (r + 1/2) / 2^16), so results
+ * are a function of the arguments only.  seed is not used with 32 bits. */
+gnn_status gnn_adamw_step(const gnn_params* params, double lr, double beta1,
+                          double beta2, double eps, int32_t t, const float* norm,
+                          double max_norm, uint64_t seed, hipStream_t stream);
+
 /* ------------------------------------------- subgraph preparation (prep) */
 
 /* The subgraph of the full training graph induced by a sampled node set
@@ -546,13 +675,14 @@ gnn_status gnn_mfma_rate_probe(int32_t kind, int32_t blocks, int32_t iters,
 #define GNN_K_COLSUM 8        /* bias-gradient column sums */
 #define GNN_K_PLAN 9          /* aggregation plan build */
 #define GNN_K_TRANSPOSE 10    /* transposed values (Algorithm 6) */
-#define GNN_K_LOSS 11         /* classifier loss and its gradient */
-#define GNN_K_UPDATE 12       /* weight update (SGD or Adam) */
+#define GNN_K_LOSS 11         /* classifier or policy loss and its gradient */
+#define GNN_K_UPDATE 12       /* weight update (SGD, Adam or AdamW) */
 #define GNN_K_INDUCE 13       /* induced subgraph on the GPU */
 #define GNN_K_GATHER 14       /* feature / label row gather */
 #define GNN_K_SDDMM 15        /* GAT per-entry dot products */
 #define GNN_K_WSPLIT 16       /* weights split into bf16 pieces (split products) */
-#define GNN_K_COUNT 17
+#define GNN_K_NORM 17         /* norm of all gradients */
+#define GNN_K_COUNT 18
 
 /* When enabled, every kernel launch is bracketed by a pair of HIP events on
  * its stream.  gnn_timer_read synchronises on the recorded events and

@@ -27,6 +27,20 @@ inline bool vec4_ok(const void* p, int64_t ld) {
   return p != nullptr && aligned16(p) && (ld % 4) == 0;
 }
 
+// ------------------------------------------------------- random numbers
+
+// SplitMix64 (Steele, Lea, Flood, OOPSLA 2014) as a counter-based generator:
+// the k-th output of a generator started at `state`.
+constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ull;
+__host__ __device__ inline uint64_t mix64(uint64_t z) {
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+__host__ __device__ inline uint64_t splitmix(uint64_t state, uint64_t k) {
+  return mix64(state + (k + 1) * GOLDEN);
+}
+
 // ------------------------------------------------------------ work plan
 
 // Layout of the aggregation plan buffer (device memory), at the offsets of

@@ -36,17 +36,6 @@ using namespace gnnprop;
 
 namespace {
 
-constexpr uint64_t GOLDEN = 0x9E3779B97F4A7C15ull;
-
-inline uint64_t mix64(uint64_t z) {
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
-  return z ^ (z >> 31);
-}
-
-// k-th output of a SplitMix64 generator started at `state`
-inline uint64_t splitmix(uint64_t state, uint64_t k) { return mix64(state + (k + 1) * GOLDEN); }
-
 inline uint64_t below(uint64_t r, uint64_t k) {
   return (uint64_t)(((unsigned __int128)r * (unsigned __int128)k) >> 64);
 }

@@ -29,7 +29,8 @@ GNN_LOSS_SIGMOID = 1
 KERNELS = {"spmm": 0, "spmm_reduce": 1, "gemm_nn": 2, "gemm_tn": 3,
            "gemm_nt": 4, "gemm_tt": 5, "gemm_reduce": 6, "mask": 7,
            "colsum": 8, "plan": 9, "transpose": 10, "loss": 11, "update": 12,
-           "induce": 13, "gather": 14, "sddmm": 15, "wsplit": 16}
+           "induce": 13, "gather": 14, "sddmm": 15, "wsplit": 16, "norm": 17}
+GNN_STATE_BLOCK = 256
 GNN_NORM_ROW = 0
 GNN_NORM_SYM = 1
 GNN_PROBE_MFMA_BF16 = 0
@@ -58,6 +59,18 @@ class gnn_layer(ctypes.Structure):
                 ("ld_x", ctypes.c_int64), ("ld_y", ctypes.c_int64),
                 ("ld_dx", ctypes.c_int64), ("order", ctypes.c_int32),
                 ("flags", ctypes.c_uint32)]
+
+
+class gnn_param(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("W", ctypes.c_void_p), ("G", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("weight_decay", ctypes.c_double)]
+
+
+class gnn_params(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("state_bits", ctypes.c_int32),
+                ("p", ctypes.POINTER(gnn_param)), ("plan", ctypes.c_void_p)]
 
 
 EXPORTS = {
@@ -129,6 +142,23 @@ EXPORTS = {
                                       ctypes.c_double, ctypes.c_void_p]),
     "gnn_adam_step": (ctypes.c_int32, [ctypes.c_int64] + [ctypes.c_void_p] * 4
                       + [ctypes.c_double] * 4 + [ctypes.c_int32, ctypes.c_void_p]),
+    "gnn_policy_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32] * 2),
+    "gnn_action_logp": (ctypes.c_int32, [ctypes.c_int32] * 2 + [
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+        ctypes.c_size_t, ctypes.c_void_p]),
+    "gnn_policy_loss": (ctypes.c_int32, [ctypes.c_int32] * 2 + [
+        ctypes.c_void_p, ctypes.c_int64] + [ctypes.c_void_p] * 5 + [ctypes.c_double] * 3
+        + [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t,
+                                   ctypes.c_void_p]),
+    "gnn_params_plan_bytes": (ctypes.c_size_t, [ctypes.POINTER(gnn_params)]),
+    "gnn_params_build_plan": (ctypes.c_int32, [ctypes.POINTER(gnn_params), ctypes.c_void_p,
+                                               ctypes.c_size_t, ctypes.c_void_p]),
+    "gnn_grad_norm_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(gnn_params)]),
+    "gnn_grad_norm": (ctypes.c_int32, [ctypes.POINTER(gnn_params), ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "gnn_adamw_step": (ctypes.c_int32, [ctypes.POINTER(gnn_params)] + [ctypes.c_double] * 4
+                       + [ctypes.c_int32, ctypes.c_void_p, ctypes.c_double, ctypes.c_uint64,
+                          ctypes.c_void_p]),
     "gnn_induce_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32]),
     "gnn_induce_subgraph": (ctypes.c_int32, [ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p,
                             ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32,
@@ -222,6 +252,23 @@ def make_layer(f_in: int, h: int, ld_x: int, ld_y: int, ld_dx: int = 0,
                order: int = 0, flags: int = 0) -> gnn_layer:
     return gnn_layer(int(f_in), int(h), int(ld_x), int(ld_y),
                      int(ld_dx or ld_x), int(order), int(flags))
+
+
+def make_params(tensors, state_bits: int = 32, plan=None) -> gnn_params:
+    """A gnn_params of tuples (W, G[, m, v[, m_scale, v_scale[, weight_decay]]])
+    of contiguous tensors (None where a call needs none).  It holds their
+    addresses only: the tensors must outlive it."""
+    p = (gnn_param * max(len(tensors), 1))()
+    for q, t in zip(p, tensors):
+        W, G_, m, v, ms, vs = (tuple(t[:6]) + (None,) * 6)[:6]
+        q.count = G_.numel()
+        q.W, q.G, q.m, q.v = _ptr(W), _ptr(G_), _ptr(m), _ptr(v)
+        q.m_scale, q.v_scale = _ptr(ms), _ptr(vs)
+        q.weight_decay = float(t[6]) if len(t) > 6 else 0.0
+    s = gnn_params(len(tensors), int(state_bits), ctypes.cast(p, ctypes.POINTER(gnn_param)),
+                   _ptr(plan))
+    s._keep = p
+    return s
 
 
 # ------------------------------------------------------------ entry points
@@ -394,6 +441,52 @@ def gnn_adam_step(count: int, W, G_, m, v, lr: float, beta1: float, beta2: float
     _check(lib().gnn_adam_step(int(count), _ptr(W), _ptr(G_), _ptr(m), _ptr(v), float(lr),
                                float(beta1), float(beta2), float(eps), int(t),
                                _stream(stream)), "gnn_adam_step")
+
+
+def gnn_policy_workspace_bytes(n: int, C: int) -> int:
+    return int(lib().gnn_policy_workspace_bytes(int(n), int(C)))
+
+
+def gnn_action_logp(n: int, C: int, Z, ld_z: int, action, logp, workspace, stream=None):
+    _check(lib().gnn_action_logp(int(n), int(C), _ptr(Z), int(ld_z), _ptr(action), _ptr(logp),
+                                 _ptr(workspace), _nbytes(workspace), _stream(stream)),
+           "gnn_action_logp")
+
+
+def gnn_policy_loss(n: int, C: int, Z, ld_z: int, action, advantage, old_logp, ref_logp,
+                    weight, clip_lo: float, clip_hi: float, beta: float, out, logp, dZ,
+                    ld_dz: int, workspace, stream=None):
+    _check(lib().gnn_policy_loss(int(n), int(C), _ptr(Z), int(ld_z), _ptr(action),
+                                 _ptr(advantage), _ptr(old_logp), _ptr(ref_logp), _ptr(weight),
+                                 float(clip_lo), float(clip_hi), float(beta), _ptr(out),
+                                 _ptr(logp), _ptr(dZ), int(ld_dz), _ptr(workspace),
+                                 _nbytes(workspace), _stream(stream)), "gnn_policy_loss")
+
+
+def gnn_params_plan_bytes(params: gnn_params) -> int:
+    return int(lib().gnn_params_plan_bytes(ctypes.byref(params)))
+
+
+def gnn_params_build_plan(params: gnn_params, plan, stream=None):
+    _check(lib().gnn_params_build_plan(ctypes.byref(params), _ptr(plan), _nbytes(plan),
+                                       _stream(stream)), "gnn_params_build_plan")
+
+
+def gnn_grad_norm_workspace_bytes(params: gnn_params) -> int:
+    return int(lib().gnn_grad_norm_workspace_bytes(ctypes.byref(params)))
+
+
+def gnn_grad_norm(params: gnn_params, norm, workspace, stream=None):
+    _check(lib().gnn_grad_norm(ctypes.byref(params), _ptr(norm), _ptr(workspace),
+                               _nbytes(workspace), _stream(stream)), "gnn_grad_norm")
+
+
+def gnn_adamw_step(params: gnn_params, lr: float, beta1: float, beta2: float, eps: float,
+                   t: int, norm=None, max_norm: float = 1.0, seed: int = 0, stream=None):
+    _check(lib().gnn_adamw_step(ctypes.byref(params), float(lr), float(beta1), float(beta2),
+                                float(eps), int(t), _ptr(norm), float(max_norm),
+                                int(seed) & ((1 << 64) - 1), _stream(stream)),
+           "gnn_adamw_step")
 
 
 def gnn_induce_workspace_bytes(n_s: int) -> int:

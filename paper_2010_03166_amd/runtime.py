@@ -371,24 +371,93 @@ class SageStack:
         return self.layers[0]["dX"] if want_dx_first else None
 
 
+class ParamSet:
+    """AdamW on a set of tensors, one launch a step: their moments (in 32
+    bits, or in 8 with a scale for each 256 elements), the plan that lists
+    them and the norm of their gradients.  Weights and gradients are
+    contiguous float32 tensors that stay where they are."""
+
+    def __init__(self, weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
+                 weight_decay: Sequence[float], state_bits: int = 32):
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8")
+        if not len(weights) == len(grads) == len(weight_decay):
+            raise ValueError("as many gradients and decays as weights")
+        for t in list(weights) + list(grads):
+            if t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda:
+                raise ValueError("weights and gradients must be contiguous float32 tensors on "
+                                 "the device")
+        for w, g in zip(weights, grads):
+            if w.shape != g.shape or w.device != g.device:
+                raise ValueError("a weight and its gradient differ in shape or device")
+        self.weights, self.grads, self.state_bits = list(weights), list(grads), state_bits
+        device = weights[0].device if weights else "cuda"
+        kind = torch.float32 if state_bits == 32 else torch.uint8
+        self.state = []  # (m, v), or with 8 bits (m, v, their scales)
+        for w in self.weights:
+            st = tuple(torch.zeros(w.numel(), dtype=kind, device=device) for _ in range(2))
+            if state_bits == 8:
+                blocks = (w.numel() + G.GNN_STATE_BLOCK - 1) // G.GNN_STATE_BLOCK
+                st += tuple(torch.zeros(blocks, device=device) for _ in range(2))
+            self.state.append(st)
+        self.params = G.make_params(
+            [(w, g) + st + (None,) * (4 - len(st)) + (float(d),)
+             for w, g, st, d in zip(self.weights, self.grads, self.state, weight_decay)],
+            state_bits)
+        self.plan = torch.empty(G.gnn_params_plan_bytes(self.params), dtype=torch.uint8,
+                                device=device)
+        self.params.plan = self.plan.data_ptr()
+        self.norm = torch.zeros(1, device=device)
+        self.ws = torch.empty(max(G.gnn_grad_norm_workspace_bytes(self.params), 256),
+                              dtype=torch.uint8, device=device)
+        G.gnn_params_build_plan(self.params, self.plan)
+
+    def grad_norm(self, stream=None) -> torch.Tensor:
+        """Norm of all gradients (one float, on the device)."""
+        G.gnn_grad_norm(self.params, self.norm, self.ws, stream)
+        return self.norm
+
+    def step(self, t: int, lr: float, betas=(0.9, 0.999), eps: float = 1e-8,
+             max_norm: Optional[float] = None, seed: int = 0, stream=None):
+        """AdamW step t (from 1).  With max_norm the gradients are scaled down
+        to that norm where theirs is larger, and a step whose norm is not
+        finite changes nothing.  seed: of the 8-bit moments' rounding."""
+        norm = self.grad_norm(stream) if max_norm is not None else None
+        G.gnn_adamw_step(self.params, lr, betas[0], betas[1], eps, t, norm,
+                         max_norm if max_norm is not None else 1.0, seed, stream)
+
+
 class Trainer:
     """One training iteration of Algorithm 1 on a prepared subgraph: the
     stack's forward pass, the classifier and loss (Section 3.1), the backward
-    pass from the classifier's input gradient down (Section 5.1), then SGD or
-    Adam on every weight.  All arithmetic runs in libgnnprop; the loss stays
-    on the device (read it with `loss.item()` when needed)."""
+    pass from the classifier's input gradient down (Section 5.1), then SGD,
+    Adam or AdamW on every weight.  policy_step is the same iteration with the
+    clipped policy loss in the place of the classifier's.  All arithmetic runs
+    in libgnnprop; the loss stays on the device (read it with `loss.item()`
+    when needed)."""
 
     def __init__(self, graph: DeviceGraph, params: Sequence, f_in: int, w_mlp,
                  multilabel: bool, optimizer: str = "adam", lr: float = 0.01,
                  betas=(0.9, 0.999), eps: float = 1e-8, order: int = 0,
                  flags: int = 0, pad: int = 16, fuse_masks: bool = False,
                  want_probs: bool = False, keep_xm: bool = False,
-                 device: str = "cuda"):
+                 device: str = "cuda", weight_decay: Optional[float] = None,
+                 max_norm: Optional[float] = None, state_bits: int = 32, seed: int = 0):
         """want_probs / keep_xm: keep the class probabilities Y / the MLP
         output X_MLP = ReLU(X^(L) W_MLP) of the last iteration in `probs` /
-        `xm` (n x C views)."""
-        if optimizer not in ("sgd", "adam"):
-            raise ValueError("optimizer must be 'sgd' or 'adam'")
+        `xm` (n x C views).
+        With optimizer "adamw": weight_decay (0.01 unless given) of the weight
+        matrices (biases do not decay), max_norm to clip the norm of all
+        gradients, state_bits 8 for moments of one byte and the seed of their
+        rounding."""
+        if optimizer not in ("sgd", "adam", "adamw"):
+            raise ValueError("optimizer must be 'sgd', 'adam' or 'adamw'")
+        if optimizer != "adamw" and (weight_decay is not None or max_norm is not None or
+                                     state_bits != 32):
+            raise ValueError("weight_decay, max_norm and state_bits go with 'adamw'")
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError("max_norm must be above 0")
+        self.max_norm, self.seed = max_norm, seed
         self.stack = SageStack(graph, params, f_in, order, flags, pad, fuse_masks, device)
         self.kind = G.GNN_LOSS_SIGMOID if multilabel else G.GNN_LOSS_SOFTMAX
         self.flags = flags & (G.GNN_FLAG_BF16 | G.GNN_FLAG_F32_MFMA)
@@ -445,7 +514,18 @@ class Trainer:
             self.state = [(self.flat_m[o: o + w.numel()].view(w.shape),
                            self.flat_v[o: o + w.numel()].view(w.shape))
                           for (w, _), o in zip(self.pairs, offs)]
+        if optimizer == "adamw":
+            decay = 0.01 if weight_decay is None else float(weight_decay)
+            self.params = ParamSet([w for w, _ in self.pairs], [g for _, g in self.pairs],
+                                   [decay if w.dim() == 2 else 0.0 for w, _ in self.pairs],
+                                   state_bits)
+            self.state = self.params.state
         self.t = 0
+        # the policy's logits and their gradient, grown when first used
+        self._Z, self._dZ = _Rows(self.C, ld_p, device), _Rows(self.C, ld_p, device)
+        self.policy_out = torch.zeros(3, device=device)
+        self.logp = torch.empty(0, device=device)
+        self.policy_ws = None
 
     def bind(self, graph: DeviceGraph, rebind_stack: bool = True):
         """Moves the iteration to another prepared subgraph (weights and
@@ -472,11 +552,78 @@ class Trainer:
                          self.dX_top.stride(0) if self.n else self.f_top, self.cls_ws,
                          stream)
         self.stack.backward(self.dX_top, want_dx_first=False, stream=stream)
+        self._update(stream)
+        return self.loss
+
+    def _update(self, stream):
         self.t += 1
         if self.optimizer == "sgd":
             G.gnn_sgd_step(self.flat_w.numel(), self.flat_w, self.flat_g, self.lr, stream)
-        else:
+        elif self.optimizer == "adam":
             G.gnn_adam_step(self.flat_w.numel(), self.flat_w, self.flat_g, self.flat_m,
                             self.flat_v, self.lr, self.betas[0], self.betas[1], self.eps,
                             self.t, stream)
-        return self.loss
+        else:
+            self.params.step(self.t, self.lr, self.betas, self.eps, self.max_norm, self.seed,
+                             stream)
+
+    def _per_row(self, name: str, t: Optional[torch.Tensor], dtype=torch.float32):
+        if t is not None and (t.dtype != dtype or t.shape != (self.n,) or
+                              not t.is_contiguous() or not t.is_cuda):
+            raise ValueError("%s must be %d contiguous values of %s on the device" %
+                             (name, self.n, dtype))
+        return t
+
+    def _logits(self, X: torch.Tensor, stream):
+        """(X^(L), its row stride, logits Z = X^(L) W_MLP, their row stride)."""
+        n, C, f = self.n, self.C, self.f_top
+        top, Z = self.stack.forward(X, stream), self._Z.view(self.n)
+        if self.logp.numel() < n:
+            self.logp = torch.empty(n, device=self.device)
+        self.policy_ws = _grown(self.policy_ws, max(
+            G.gnn_policy_workspace_bytes(n, C), G.gnn_gemm_workspace_bytes(n, C, f),
+            G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C)),
+            self.device)
+        ld_top = top.stride(0) if n else f
+        G.gnn_gemm(False, False, n, C, f, top, ld_top, self.W_mlp, C, Z, self._Z.ld, self.flags,
+                   self.policy_ws, stream)
+        return top, ld_top, Z, self._Z.ld
+
+    def action_logp(self, X: torch.Tensor, actions: torch.Tensor, stream=None) -> torch.Tensor:
+        """Log-probability of each row's action (n int32; outside [0, C): 0)
+        under the present weights: a new tensor, to be kept as old_logp or
+        ref_logp."""
+        self._per_row("actions", actions, torch.int32)
+        _, _, Z, ld = self._logits(X, stream)
+        logp = torch.empty(self.n, device=self.device)
+        G.gnn_action_logp(self.n, self.C, Z, ld, actions, logp, self.policy_ws, stream)
+        return logp
+
+    def policy_step(self, X: torch.Tensor, actions: torch.Tensor, advantage: torch.Tensor,
+                    old_logp: Optional[torch.Tensor] = None,
+                    ref_logp: Optional[torch.Tensor] = None,
+                    weight: Optional[torch.Tensor] = None, clip=(0.2, 0.2), beta: float = 0.0,
+                    stream=None) -> torch.Tensor:
+        """One iteration with the clipped policy loss (gnn_policy_loss) on the
+        logits X^(L) W_MLP: forward, loss, backward, update.  Each row's action
+        (n int32; outside [0, C): the row is left out), advantage, old_logp
+        (None: on-policy), ref_logp (with beta), weight (None: 1/n).  Returns
+        three floats on the device: loss, KL and clipped share (weighted sums);
+        the rows' log-probabilities are in `logp`."""
+        for name, t in (("advantage", advantage), ("old_logp", old_logp),
+                        ("ref_logp", ref_logp), ("weight", weight)):
+            self._per_row(name, t)
+        self._per_row("actions", actions, torch.int32)
+        n, C, f = self.n, self.C, self.f_top
+        top, ld_top, Z, ld = self._logits(X, stream)
+        dZ = self._dZ.view(n)
+        G.gnn_policy_loss(n, C, Z, ld, actions, advantage, old_logp, ref_logp, weight, clip[0],
+                          clip[1], beta, self.policy_out, self.logp, dZ, ld, self.policy_ws,
+                          stream)
+        G.gnn_gemm(True, False, f, C, n, top, ld_top, dZ, ld, self.dW_mlp, C, self.flags,
+                   self.policy_ws, stream)
+        G.gnn_gemm(False, True, n, f, C, dZ, ld, self.W_mlp, C, self.dX_top,
+                   self.dX_top.stride(0) if n else f, self.flags, self.policy_ws, stream)
+        self.stack.backward(self.dX_top, want_dx_first=False, stream=stream)
+        self._update(stream)
+        return self.policy_out
