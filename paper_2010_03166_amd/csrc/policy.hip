@@ -17,6 +17,11 @@ constexpr int THREADS = 256;
 struct Terms {  // a row's share of `out`
   double loss, kl, cut;
 };
+struct Chunk {  // sums of a part of a row
+  double sum;   // of exp(z - top)
+  float top;
+  float pad;
+};
 
 struct PolicyArgs {
   int32_t n, C;
@@ -25,114 +30,577 @@ struct PolicyArgs {
   const int32_t* action;
   const float *adv, *old_lp, *ref_lp, *weight;
   double lo, hi, beta;  // clip to [lo, hi]
+  float* out;
   float* logp;
   float* dZ;
   int64_t ld_dz;
-  Terms* part;
+  Terms* part;    // one per block (split rows: one per row)
+  Chunk* chunks;  // split rows: per_row for each row
+  int32_t per_row;
+  int64_t blocks, block0;  // of all launches, and in the launches before
 };
 
-// exp(x - top) where top = -inf only if no logit is above it: then 0 (or NaN
-// for a NaN), so that the sum is 0 exactly for a row without any action.
-__device__ inline float exp_from(float x, float top) {
-  return expf(x - (top == -INFINITY ? 0.f : top));
+// ------------------------------------------------------------- row scalars
+
+// exp(x - top), where top = -inf only if no logit is above it: then 0 (or
+// NaN for a NaN), so that the sum is 0 exactly for a row without any action.
+__device__ inline float shift_of(float top) { return top == -INFINITY ? 0.f : top; }
+
+// What a row's terms are computed from, besides its sum.
+struct RowIn {
+  int32_t act;
+  float za, adv, old_lp, ref_lp, w;
+  bool chosen;
+};
+__device__ inline RowIn row_in(const PolicyArgs& a, int32_t i, bool loss) {
+  RowIn r = {};
+  r.act = a.action[i];
+  r.chosen = r.act >= 0 && r.act < a.C;
+  r.za = r.chosen ? a.Z[(int64_t)i * a.ld_z + r.act] : 0.f;
+  if (loss) {
+    r.adv = a.adv[i];
+    r.old_lp = a.old_lp ? a.old_lp[i] : 0.f;
+    r.ref_lp = a.ref_lp ? a.ref_lp[i] : 0.f;
+    r.w = a.weight ? a.weight[i] : 0.f;
+  }
+  return r;
 }
 
-// The loss terms of row i and its slope, from its log-probability; `live`:
-// the row has an action and at least one logit above -inf.
-__device__ inline Terms row_terms(const PolicyArgs& a, int32_t i, bool live, double lp, float* c) {
-  Terms t = {0.0, 0.0, 0.0};
+// Scalar functions.  Sums of fp32 exponentials are good to (20 + ln C) 2^-24
+// at worst, 2e-6, so logarithms and exponentials as good as 2e-7 lose nothing
+// beside them, and library functions of doubles would hold a hundred registers
+// for their coefficients.  Where a ratio is as near to a border of the clip
+// as those errors (rows are rarely), everything is computed once more in
+// doubles, slowly.
+
+// exp(x) to a few 2^-53 for |x| < 700: 2^k times the series of the remainder
+// (below 0.35, 15 terms), each term from the one before.
+__device__ inline double exp_exact(double x) {
+  if (!(x > -700.0)) return x < 0.0 ? 0.0 : x;  // 0, or NaN
+  const double k = rint(x * 1.4426950408889634);
+  const double r = fma(-k, 2.3190468138462996e-17, fma(-k, 0.6931471805599453, x));
+  double term = 1.0, sum = 1.0;
+#pragma unroll 1
+  for (int i = 1; i < 16; ++i) {
+    term *= r / i;
+    sum += term;
+  }
+  return ldexp(sum, (int)fmin(k, 2000.0));
+}
+
+// log(s) as k ln 2 + log(m), 0.7 < m < 1.42: good to 4e-8.
+__device__ inline double log_quick(double s) {
+  int k;
+  double m = frexp(s, &k);
+  if (m < 0.70710678) {
+    m *= 2.0;
+    --k;
+  }
+  const float f = (float)m;
+  const float more = (float)(m - f);  // a NaN or an infinity shows in logf(f)
+  return k * 0.6931471805599453 + (double)(logf(f) + (more == more ? more : 0.f) / f);
+}
+
+// One step of third order from there (e^y is s but for 1e-7).
+__device__ inline double log_exact(double s) {
+  const double y = log_quick(s), e = exp_exact(y);
+  return y + 2.0 * (s - e) / (s + e);
+}
+
+// The part of x beyond its rounding to fp32 (0 for infinities).
+__device__ inline double beyond(double x, float f) {
+  const double d = x - (double)f;
+  return fabs(d) < INFINITY ? d : 0.0;
+}
+__device__ inline double exp_quick(double x) {
+  const float f = (float)x;
+  return (double)expf(f) * (1.0 + beyond(x, f));
+}
+__device__ inline double expm1_quick(double x) {
+  const float f = (float)x;
+  const double e = (double)expm1f(f);
+  return e + (1.0 + e) * beyond(x, f);
+}
+
+template <bool EXACT>
+__device__ inline double log_prob(const RowIn& r, float top, double sum) {
+  if (!r.chosen) return 0.0;
+  if (sum == 0.0) return -INFINITY;
+  return (double)r.za - top - (EXACT ? log_exact(sum) : log_quick(sum));
+}
+
+// The row's terms, and its slope c = w dl/dlp.  Returns whether the ratio is
+// so close to a border of the clip that only doubles decide.
+template <bool EXACT>
+__device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum, double lp,
+                                 Terms* t, float* c) {
   *c = 0.f;
-  const double w = a.weight ? (double)a.weight[i] : 1.0 / a.n;
-  if (!live || w == 0.0) return t;
-  const double A = a.adv[i];
-  const double rho = a.old_lp ? exp(lp - (double)a.old_lp[i]) : 1.0;
+  *t = {0.0, 0.0, 0.0};
+  const double w = a.weight ? (double)r.w : 1.0 / a.n;
+  if (!r.chosen || sum == 0.0 || w == 0.0) return false;
+  const double A = r.adv, x = lp - (double)r.old_lp;
+  const double rho = !a.old_lp ? 1.0 : EXACT ? exp_exact(x) : exp_quick(x);
+  const bool near = a.old_lp && (fabs(rho - a.lo) <= 1e-5 * rho || fabs(rho - a.hi) <= 1e-5 * rho);
   const double ra = rho * A, ca = fmin(fmax(rho, a.lo), a.hi) * A;
   const bool cut = ra > ca;  // false for a NaN, which then shows in ra
-  double slope = cut ? 0.0 : -ra;
-  t.loss = -(cut ? ca : ra);
-  t.cut = cut ? w : 0.0;
+  double slope = cut ? 0.0 : -ra, loss = -(cut ? ca : ra);
   if (a.ref_lp) {
-    const double d = (double)a.ref_lp[i] - lp, e = exp(d);
-    const double kl = d == INFINITY ? d : e - d - 1.0;
-    t.kl = w * kl;
+    const double d = (double)r.ref_lp - lp, e = expm1_quick(d);
+    const double kl = d == INFINITY ? d : e - d;
+    t->kl = w * kl;
     if (a.beta != 0.0) {
-      t.loss += a.beta * kl;
-      slope += a.beta * (1.0 - e);
+      loss += a.beta * kl;
+      slope -= a.beta * e;
     }
   }
-  t.loss *= w;
+  t->loss = w * loss;
+  t->cut = cut ? w : 0.0;
   *c = (float)(w * slope);
+  return near;
+}
+
+// ------------------------------------------------------------- reductions
+
+template <int G>
+__device__ inline float group_max(float v) {
+#pragma unroll
+  for (int d = G / 2; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
+  return v;
+}
+template <int G, typename T>
+__device__ inline T group_sum(T v) {
+#pragma unroll
+  for (int d = G / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+  return v;
+}
+
+// The block's sum of terms in thread 0, in a fixed order.
+template <int T>
+__device__ inline Terms block_terms(Terms t) {
+  __shared__ Terms s[T / 64];
+  t.loss = group_sum<64>(t.loss);
+  t.kl = group_sum<64>(t.kl);
+  t.cut = group_sum<64>(t.cut);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = t;
+  __syncthreads();
+  t = s[0];
+  for (int k = 1; k < T / 64; ++k) {
+    t.loss += s[k].loss;
+    t.kl += s[k].kl;
+    t.cut += s[k].cut;
+  }
   return t;
 }
 
-template <typename T, typename F>
-__device__ inline T block_reduce(T v, T* s, F op) {
-  __syncthreads();
-  s[threadIdx.x] = v;
-  __syncthreads();
-  for (int d = THREADS / 2; d > 0; d >>= 1) {
-    if ((int)threadIdx.x < d) s[threadIdx.x] = op(s[threadIdx.x], s[threadIdx.x + d]);
-    __syncthreads();
-  }
-  return s[0];
+__device__ inline void store_out(float* out, const Terms& t) {
+  out[0] = (float)t.loss;
+  out[1] = (float)t.kl;
+  out[2] = (float)t.cut;
 }
 
-// One workgroup per row, three passes over it.
-__global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a) {
-  __shared__ float s_top[THREADS];
-  __shared__ double s_sum[THREADS];
-  const int32_t i = blockIdx.x;
-  const float* z = a.Z + (int64_t)i * a.ld_z;
-  const int32_t act = a.action[i];
-  const bool chosen = act >= 0 && act < a.C;
-  float top = -INFINITY, c = 0.f;
+// The block's share of `out`, or `out` itself where it is the only block.
+__device__ inline void store_terms(const PolicyArgs& a, const Terms& t) {
+  if (threadIdx.x) return;
+  if (a.blocks == 1) store_out(a.out, t);
+  else a.part[a.block0 + blockIdx.x] = t;
+}
+
+// Sum of exp(z - top) of one row by a wavefront, in doubles.
+__device__ inline double exact_sum(const float* z, int32_t C, float top) {
+  const double shift = shift_of(top);
   double sum = 0.0;
-  if (chosen) {
-    for (int32_t j = threadIdx.x; j < a.C; j += THREADS) top = fmaxf(top, z[j]);
-    top = block_reduce(top, s_top, [](float x, float y) { return fmaxf(x, y); });
-    for (int32_t j = threadIdx.x; j < a.C; j += THREADS) sum += exp((double)z[j] - (top == -INFINITY ? 0.0 : (double)top));
-    sum = block_reduce(sum, s_sum, [](double x, double y) { return x + y; });
-  }
-  const bool live = chosen && sum != 0.0;
-  const double lp = live ? (double)z[act] - top - log(sum) : chosen ? -INFINITY : 0.0;
-  if (threadIdx.x == 0 && a.logp) a.logp[i] = (float)lp;
-  if (!a.part) return;
-  const Terms t = row_terms(a, i, live, lp, &c);
-  if (threadIdx.x == 0) a.part[i] = t;
-  if (!a.dZ) return;
-  float* dz = a.dZ + (int64_t)i * a.ld_dz;
-  const float inv = (float)(1.0 / sum);
-  for (int32_t j = threadIdx.x; j < a.C; j += THREADS)
-    dz[j] = c == 0.f ? 0.f : c * ((j == act ? 1.f : 0.f) - exp_from(z[j], top) * inv);
+#pragma unroll 1
+  for (int32_t j = threadIdx.x & 63; j < C; j += 64) sum += exp_exact((double)z[j] - shift);
+  return group_sum<64>(sum);
 }
 
-// out = the sums of `count` partial terms, in a fixed order.
-__global__ __launch_bounds__(THREADS) void policy_final_kernel(int32_t count,
-                                                               const Terms* __restrict__ part,
-                                                               float* __restrict__ out) {
-  __shared__ double s[THREADS];
+// ---------------------------------------------------------- four at a time
+
+// Rows start at any multiple of 4 bytes, so the vector accesses claim no more
+// (global memory instructions of 16 bytes need no more).
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef f4 f4u __attribute__((aligned(4)));
+
+// Columns [col, col + 4) of a row of C, -inf past its end.
+__device__ inline f4 load_cols(const float* row, int32_t col, int32_t C) {
+  if (col + 4 <= C) return *reinterpret_cast<const f4u*>(row + col);
+  f4 r = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  if (col < C) r.x = row[col];
+  if (col + 1 < C) r.y = row[col + 1];
+  if (col + 2 < C) r.z = row[col + 2];
+  return r;
+}
+__device__ inline void store_cols(float* row, int32_t col, int32_t C, f4 v) {
+  if (col + 4 <= C) {
+    *reinterpret_cast<f4u*>(row + col) = v;
+    return;
+  }
+  if (col < C) row[col] = v.x;
+  if (col + 1 < C) row[col + 1] = v.y;
+  if (col + 2 < C) row[col + 2] = v.z;
+}
+
+__device__ inline float max4(f4 v) { return fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)); }
+__device__ inline f4 exp4(f4 v, float shift) {
+  return {expf(v.x - shift), expf(v.y - shift), expf(v.z - shift), expf(v.w - shift)};
+}
+__device__ inline float sum4(f4 v) { return (v.x + v.y) + (v.z + v.w); }
+
+// c (1[j = act] - e_j inv) for columns col .. col + 3; 0 where c is 0,
+// whatever the logits.
+__device__ inline f4 grad4(f4 e, int32_t col, int32_t act, float c, float inv) {
+  f4 g = {0.f, 0.f, 0.f, 0.f};
+  if (c == 0.f) return g;
+  g.x = c * ((col == act ? 1.f : 0.f) - e.x * inv);
+  g.y = c * ((col + 1 == act ? 1.f : 0.f) - e.y * inv);
+  g.z = c * ((col + 2 == act ? 1.f : 0.f) - e.z * inv);
+  g.w = c * ((col + 3 == act ? 1.f : 0.f) - e.w * inv);
+  return g;
+}
+
+// ------------------------------------------------ several rows a wavefront
+
+// G lanes to a row of at most 4 G V columns, U rows to each group of lanes:
+// R = 256 U / G <= 256 rows a block, read once into registers.  Between the
+// sums and the gradient one thread computes each row's scalars, so that they
+// cost a wavefront's time once for 64 rows instead of once for each 64 / G.
+template <int G, int V, int U, bool LOSS>
+__global__ __launch_bounds__(THREADS) void rows_kernel(PolicyArgs a) {
+  constexpr int NG = THREADS / G, R = NG * U;
+  static_assert(R <= THREADS, "a thread for each row");
+  __shared__ float s_top[R], s_sum[R], s_c[R], s_inv[R];
+  __shared__ int32_t s_act[R];
+  __shared__ double s_exact[R];
+  const int lane = threadIdx.x % G, grp = threadIdx.x / G, t = threadIdx.x;
+  const int32_t first = (int32_t)(a.block0 + blockIdx.x) * R;
+  f4 z[U][V];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = (int64_t)first + u * NG + grp;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      z[u][k] = load_cols(a.Z + i * a.ld_z, (k * G + lane) * 4, i < a.n ? a.C : 0);
+  }
+  const int32_t rows = min(R, a.n - first);
+  const bool mine = t < rows;
+  RowIn r = {};
+  if (mine) r = row_in(a, first + t, LOSS);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    float top = max4(z[u][0]);
+#pragma unroll
+    for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[u][k]));
+    top = group_max<G>(top);
+    const float shift = shift_of(top);
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      z[u][k] = exp4(z[u][k], shift);
+      sum += sum4(z[u][k]);
+    }
+    sum = group_sum<G>(sum);
+    if (lane == 0) {
+      s_top[u * NG + grp] = top;
+      s_sum[u * NG + grp] = sum;
+    }
+  }
+  __syncthreads();
+  double sum = mine ? (double)s_sum[t] : 1.0;
+  if (!LOSS) {
+    if (mine) a.logp[first + t] = (float)log_prob<false>(r, s_top[t], sum);
+  } else {
+    float c = 0.f;
+    Terms terms = {0.0, 0.0, 0.0};
+    bool near = false;
+    if (mine) {
+      const double lp = log_prob<false>(r, s_top[t], sum);
+      near = row_terms<false>(a, r, sum, lp, &terms, &c);
+      if (a.logp) a.logp[first + t] = (float)lp;
+      s_exact[t] = near ? -1.0 : 0.0;
+    }
+    if (__syncthreads_or(near)) {
+      for (int q = t >> 6; q < rows; q += THREADS / 64)
+        if (s_exact[q] < 0.0) {
+          const double s = exact_sum(a.Z + ((int64_t)first + q) * a.ld_z, a.C, s_top[q]);
+          if ((t & 63) == 0) s_exact[q] = s;
+        }
+      __syncthreads();
+      if (near) {
+        sum = s_exact[t];
+        row_terms<true>(a, r, sum, log_prob<true>(r, s_top[t], sum), &terms, &c);
+      }
+    }
+    if (mine) {
+      s_c[t] = c;
+      s_inv[t] = (float)(1.0 / sum);
+      s_act[t] = r.act;
+    }
+    __syncthreads();
+    if (a.dZ) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int q = u * NG + grp;
+        if (q >= rows) break;
+        float* to = a.dZ + ((int64_t)first + q) * a.ld_dz;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          const int32_t col = (k * G + lane) * 4;
+          store_cols(to, col, a.C, grad4(z[u][k], col, s_act[q], s_c[q], s_inv[q]));
+        }
+      }
+    }
+    store_terms(a, block_terms<THREADS>(terms));
+  }
+}
+
+// ---------------------------------------------------------- one row a block
+
+// T threads to a row of at most 4 T V columns, in registers.
+template <int T, int V, bool LOSS>
+__global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
+  __shared__ float s_top[T / 64], s_c, s_inv;
+  __shared__ double s_sum[T / 64];
+  const int t = threadIdx.x, wave = t >> 6;
+  const int32_t i = (int32_t)(a.block0 + blockIdx.x);
+  const float* row = a.Z + (int64_t)i * a.ld_z;
+  f4 z[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) z[k] = load_cols(row, (k * T + t) * 4, a.C);
+  const RowIn r = row_in(a, i, LOSS);
+  float top = max4(z[0]);
+#pragma unroll
+  for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
+  top = group_max<64>(top);
+  if ((t & 63) == 0) s_top[wave] = top;
+  __syncthreads();
+  top = s_top[0];
+#pragma unroll
+  for (int k = 1; k < T / 64; ++k) top = fmaxf(top, s_top[k]);
+  const float shift = shift_of(top);
+  float part = 0.f;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    z[k] = exp4(z[k], shift);
+    part += sum4(z[k]);
+  }
+  part = group_sum<64>(part);
+  if ((t & 63) == 0) s_sum[wave] = part;
+  __syncthreads();
+  if (wave == 0) {
+    double sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < T / 64; ++k) sum += s_sum[k];
+    const double lp = log_prob<false>(r, top, sum);
+    if (t == 0 && a.logp) a.logp[i] = (float)lp;
+    if (LOSS) {
+      Terms terms;
+      float c;
+      if (row_terms<false>(a, r, sum, lp, &terms, &c)) {  // the same in all lanes
+        sum = exact_sum(row, a.C, top);
+        row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &c);
+      }
+      store_terms(a, terms);
+      if (t == 0) {
+        s_c = c;
+        s_inv = (float)(1.0 / sum);
+      }
+    }
+  }
+  if (!LOSS || !a.dZ) return;
+  __syncthreads();
+  float* to = a.dZ + (int64_t)i * a.ld_dz;
+  const float c = s_c, inv = s_inv;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int32_t col = (k * T + t) * 4;
+    store_cols(to, col, a.C, grad4(z[k], col, r.act, c, inv));
+  }
+}
+
+// -------------------------------------------------------- several blocks a row
+
+// Rows longer than a block's registers are cut into chunks, a block each:
+// one launch for the chunks' sums, one that joins a row's sums, computes its
+// scalars in every block of the row alike, and writes the chunk's gradient
+// from a second reading (out of the caches, for the few rows that are so long).
+constexpr int SPLIT_V = 8;
+constexpr int SPLIT_COLS = 4 * THREADS * SPLIT_V;
+__host__ __device__ inline int32_t chunks_of(int32_t C) {
+  return (int32_t)ceil_div(C, SPLIT_COLS);
+}
+
+__global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
+  __shared__ float s_top[THREADS / 64];
+  __shared__ double s_sum[THREADS / 64];
+  const int t = threadIdx.x, wave = t >> 6;
+  const int64_t b = a.block0 + blockIdx.x;
+  const int32_t i = (int32_t)(b / a.per_row), first = (int32_t)(b % a.per_row) * SPLIT_COLS;
+  const float* row = a.Z + (int64_t)i * a.ld_z;
+  f4 z[SPLIT_V];
+#pragma unroll
+  for (int k = 0; k < SPLIT_V; ++k) z[k] = load_cols(row, first + (k * THREADS + t) * 4, a.C);
+  float top = max4(z[0]);
+#pragma unroll
+  for (int k = 1; k < SPLIT_V; ++k) top = fmaxf(top, max4(z[k]));
+  top = group_max<64>(top);
+  if ((t & 63) == 0) s_top[wave] = top;
+  __syncthreads();
+  top = s_top[0];
+#pragma unroll
+  for (int k = 1; k < THREADS / 64; ++k) top = fmaxf(top, s_top[k]);
+  const float shift = shift_of(top);
+  float part = 0.f;
+#pragma unroll
+  for (int k = 0; k < SPLIT_V; ++k) part += sum4(exp4(z[k], shift));
+  part = group_sum<64>(part);
+  if ((t & 63) == 0) s_sum[wave] = part;
+  __syncthreads();
+  if (t == 0) {
+    double sum = 0.0;
+    for (int k = 0; k < THREADS / 64; ++k) sum += s_sum[k];
+    a.chunks[b] = {sum, top, 0.f};
+  }
+}
+
+// a.blocks blocks: those of a row's chunks, or one a row without a gradient.
+template <bool LOSS>
+__global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
+  const int t = threadIdx.x, lane = t & 63;
+  const int32_t todo = LOSS && a.dZ ? a.per_row : 1;
+  const int64_t b = a.block0 + blockIdx.x;
+  const int32_t i = (int32_t)(b / todo), chunk = (int32_t)(b % todo);
+  const float* row = a.Z + (int64_t)i * a.ld_z;
+  const RowIn r = row_in(a, i, LOSS);
+  // every wavefront joins the row's sums alike
+  const Chunk* at = a.chunks + (int64_t)i * a.per_row;
+  float top = -INFINITY;
+  for (int32_t k = lane; k < a.per_row; k += 64) top = fmaxf(top, at[k].top);
+  top = group_max<64>(top);
+  const float shift = shift_of(top);
+  double sum = 0.0;
+  for (int32_t k = lane; k < a.per_row; k += 64) {
+    const Chunk c = at[k];
+    sum += c.sum * exp_quick((double)shift_of(c.top) - shift);
+  }
+  sum = group_sum<64>(sum);
+  const double lp = log_prob<false>(r, top, sum);
+  if (t == 0 && chunk == 0 && a.logp) a.logp[i] = (float)lp;
+  if (!LOSS) return;
+  Terms terms;
+  float c;
+  if (row_terms<false>(a, r, sum, lp, &terms, &c)) {  // alike in all threads of a row
+    sum = exact_sum(row, a.C, top);
+    row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &c);
+  }
+  if (t == 0 && chunk == 0) a.part[i] = terms;
+  if (!a.dZ) return;
+  const float inv = (float)(1.0 / sum);
+  float* to = a.dZ + (int64_t)i * a.ld_dz;
+#pragma unroll
+  for (int k = 0; k < SPLIT_V; ++k) {
+    const int32_t col = chunk * SPLIT_COLS + (k * THREADS + t) * 4;
+    if (col < a.C)
+      store_cols(to, col, a.C, grad4(exp4(load_cols(row, col, a.C), shift), col, r.act, c, inv));
+  }
+}
+
+// One block: out = the sum of `count` partial terms.  More: each its share of
+// them, to `shares`.  In a fixed order either way.
+constexpr int FINAL_THREADS = 1024;
+__global__ __launch_bounds__(FINAL_THREADS) void policy_final_kernel(
+    int32_t count, const Terms* __restrict__ part, Terms* __restrict__ shares,
+    float* __restrict__ out) {
   Terms t = {0.0, 0.0, 0.0};
-  for (int32_t k = threadIdx.x; k < count; k += THREADS) {
+  for (int64_t k = (int64_t)blockIdx.x * FINAL_THREADS + threadIdx.x; k < count;
+       k += (int64_t)gridDim.x * FINAL_THREADS) {
     t.loss += part[k].loss;
     t.kl += part[k].kl;
     t.cut += part[k].cut;
   }
-  const auto add = [](double x, double y) { return x + y; };
-  const double loss = block_reduce(t.loss, s, add), kl = block_reduce(t.kl, s, add),
-               cut = block_reduce(t.cut, s, add);
-  if (threadIdx.x == 0) {
-    out[0] = (float)loss;
-    out[1] = (float)kl;
-    out[2] = (float)cut;
-  }
+  t = block_terms<FINAL_THREADS>(t);
+  if (threadIdx.x) return;
+  if (gridDim.x == 1) store_out(out, t);
+  else shares[blockIdx.x] = t;
 }
 
-size_t workspace_need(int32_t n, int32_t C) { return round_up((size_t)n * sizeof(Terms), 256); }
+// ---------------------------------------------------------------- launches
 
-gnn_status launch(const PolicyArgs& a, float* out, hipStream_t stream) {
+constexpr int32_t GROUP_COLS = 1024, BLOCK_COLS = 32768;
+
+struct Launch {
+  void (*rows)(PolicyArgs);  // rows_kernel or block_kernel; NULL: split rows
+  int32_t rows_per_block, threads;
+};
+template <bool LOSS>
+Launch choose(int32_t C) {
+  if (C <= 4) return {rows_kernel<1, 1, 1, LOSS>, 256, THREADS};
+  if (C <= 8) return {rows_kernel<2, 1, 2, LOSS>, 256, THREADS};
+  if (C <= 16) return {rows_kernel<4, 1, 4, LOSS>, 256, THREADS};
+  if (C <= 32) return {rows_kernel<8, 1, 8, LOSS>, 256, THREADS};
+  if (C <= 64) return {rows_kernel<16, 1, 8, LOSS>, 128, THREADS};
+  if (C <= 128) return {rows_kernel<32, 1, 8, LOSS>, 64, THREADS};
+  if (C <= 256) return {rows_kernel<64, 1, 8, LOSS>, 32, THREADS};
+  if (C <= 512) return {rows_kernel<64, 2, 4, LOSS>, 16, THREADS};
+  if (C <= GROUP_COLS) return {rows_kernel<64, 4, 2, LOSS>, 8, THREADS};
+  if (C <= 2048) return {block_kernel<256, 2, LOSS>, 1, 256};
+  if (C <= 4096) return {block_kernel<256, 4, LOSS>, 1, 256};
+  if (C <= 8192) return {block_kernel<256, 8, LOSS>, 1, 256};
+  if (C <= 16384) return {block_kernel<1024, 4, LOSS>, 1, 1024};
+  if (C <= BLOCK_COLS) return {block_kernel<1024, 8, LOSS>, 1, 1024};
+  return {nullptr, 0, 0};
+}
+
+// Partial terms that one block adds; more are added in SHARES blocks first.
+constexpr int32_t FINAL_MOST = 32768, SHARES = 256;
+// Blocks of one launch (2^32 threads are the most that a launch can have).
+constexpr int64_t LAUNCH_BLOCKS = 1 << 21;
+
+int32_t parts_of(int32_t n, const Launch& l) {
+  return l.rows ? (int32_t)ceil_div(n, l.rows_per_block) : n;
+}
+
+// [partial terms | shares of them | chunks' sums]
+struct Layout {
+  size_t shares, chunks, total;
+};
+Layout layout_of(int32_t n, int32_t C, bool loss) {
+  const Launch l = choose<true>(C);
+  Layout o;
+  const int32_t parts = loss ? parts_of(n, l) : 0;
+  o.shares = round_up((size_t)parts * sizeof(Terms), 256);
+  o.chunks = o.shares + (parts > FINAL_MOST ? SHARES * sizeof(Terms) : 0);
+  o.total = o.chunks + (l.rows ? 0 : round_up((size_t)n * chunks_of(C) * sizeof(Chunk), 256));
+  return o;
+}
+
+template <bool LOSS>
+gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
+  const Launch l = choose<LOSS>(a.C);
+  const Layout o = layout_of(a.n, a.C, LOSS);
+  char* ws = static_cast<char*>(workspace);
+  a.part = reinterpret_cast<Terms*>(ws);
+  a.chunks = reinterpret_cast<Chunk*>(ws + o.chunks);
+  a.per_row = chunks_of(a.C);
+  const auto run = [&](void (*kernel)(PolicyArgs), int32_t threads, int64_t blocks) {
+    a.blocks = blocks;
+    for (a.block0 = 0; a.block0 < blocks; a.block0 += LAUNCH_BLOCKS)
+      kernel<<<(unsigned)std::min(blocks - a.block0, LAUNCH_BLOCKS), threads, 0, stream>>>(a);
+  };
   timer_begin(GNN_K_LOSS, stream);
-  if (a.n > 0) policy_row_kernel<<<a.n, THREADS, 0, stream>>>(a);
-  if (out) policy_final_kernel<<<1, THREADS, 0, stream>>>(a.n, a.part, out);
+  const int32_t parts = parts_of(a.n, l);
+  if (l.rows) {
+    run(l.rows, l.threads, parts);
+  } else {
+    run(split_sums_kernel, THREADS, (int64_t)a.n * a.per_row);
+    run(split_grad_kernel<LOSS>, THREADS, LOSS && a.dZ ? (int64_t)a.n * a.per_row : a.n);
+  }
+  if (LOSS && !(l.rows && parts == 1)) {  // (one block of rows has written `out` itself)
+    Terms* shares = reinterpret_cast<Terms*>(ws + o.shares);
+    if (parts > FINAL_MOST)
+      policy_final_kernel<<<SHARES, FINAL_THREADS, 0, stream>>>(parts, a.part, shares, nullptr);
+    policy_final_kernel<<<1, FINAL_THREADS, 0, stream>>>(
+        parts > FINAL_MOST ? SHARES : parts, parts > FINAL_MOST ? shares : a.part, nullptr, a.out);
+  }
   timer_end(GNN_K_LOSS, (a.dZ ? 8.0 : 4.0) * a.n * a.C, stream);
   GNN_HIP(hipGetLastError());
   return GNN_OK;
@@ -144,7 +612,7 @@ extern "C" {
 
 size_t gnn_policy_workspace_bytes(int32_t n, int32_t C) {
   if (n < 0 || C <= 0) return 0;
-  return workspace_need(n, C);
+  return layout_of(n, C, true).total;
 }
 
 gnn_status gnn_action_logp(int32_t n, int32_t C, const float* Z, int64_t ld_z,
@@ -154,7 +622,7 @@ gnn_status gnn_action_logp(int32_t n, int32_t C, const float* Z, int64_t ld_z,
   if (n == 0) return GNN_OK;
   if (!Z || !action || !logp) return GNN_ERR_NULL;
   if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
-  const size_t need = workspace_need(n, C);
+  const size_t need = layout_of(n, C, false).total;
   if (workspace_bytes < need || (need > 0 && !workspace)) return GNN_ERR_WORKSPACE;
   const size_t rows = (size_t)n * 4;
   const void* ins[] = {Z, action};
@@ -171,7 +639,7 @@ gnn_status gnn_action_logp(int32_t n, int32_t C, const float* Z, int64_t ld_z,
   a.ld_z = ld_z;
   a.action = action;
   a.logp = logp;
-  return launch(a, nullptr, stream);
+  return launch<false>(a, workspace, stream);
 }
 
 gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
@@ -189,7 +657,7 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
   if (!out) return GNN_ERR_NULL;
   if (n > 0 && (!Z || !action || !advantage || (beta > 0.0 && !ref_logp))) return GNN_ERR_NULL;
   if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
-  const size_t need = workspace_need(n, C);
+  const size_t need = layout_of(n, C, true).total;
   if (workspace_bytes < need || (need > 0 && !workspace)) return GNN_ERR_WORKSPACE;
   {
     const size_t rows = (size_t)n * 4;
@@ -217,11 +685,11 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
   a.lo = 1.0 - clip_lo;
   a.hi = 1.0 + clip_hi;
   a.beta = beta;
+  a.out = out;
   a.logp = logp;
   a.dZ = dZ;
   a.ld_dz = ld_dz;
-  a.part = static_cast<Terms*>(workspace);
-  return launch(a, out, stream);
+  return launch<true>(a, workspace, stream);
 }
 
 }  // extern "C"
