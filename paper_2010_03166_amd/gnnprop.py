@@ -232,8 +232,24 @@ def _ptr(t) -> Optional[int]:
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
+    return _current_stream()
+
+
+def _current_stream() -> int:
+    """Handle of torch's current stream on the current device.  Where torch
+    gives the handle itself this costs 0.3 us of a call's 5 to 8; a Stream
+    object, made anew each time, costs 3."""
+    global _current_stream
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    device = torch.cuda.current_device
+    if raw is not None:
+        def _current_stream():
+            return raw(device())
+    else:
+        def _current_stream():
+            return torch.cuda.current_stream().cuda_stream
+    return _current_stream()
 
 
 def _ld(t) -> int:
