@@ -30,6 +30,7 @@ struct PolicyArgs {
   const int32_t* action;
   const float *adv, *old_lp, *ref_lp, *weight;
   double lo, hi, beta;  // clip to [lo, hi]
+  double mean;          // 1 / n
   float* out;
   float* logp;
   float* dZ;
@@ -136,7 +137,7 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
                                  Terms* t, float* c) {
   *c = 0.f;
   *t = {0.0, 0.0, 0.0};
-  const double w = a.weight ? (double)r.w : 1.0 / a.n;
+  const double w = a.weight ? (double)r.w : a.mean;
   if (!r.chosen || sum == 0.0 || w == 0.0) return false;
   const double A = r.adv, x = lp - (double)r.old_lp;
   const double rho = !a.old_lp ? 1.0 : EXACT ? exp_exact(x) : exp_quick(x);
@@ -260,97 +261,86 @@ __device__ inline f4 grad4(f4 e, int32_t col, int32_t act, float c, float inv) {
 
 // ------------------------------------------------ several rows a wavefront
 
-// G lanes to a row of at most 4 G V columns, U rows to each group of lanes:
-// R = 256 U / G <= 256 rows a block, read once into registers.  Between the
-// sums and the gradient one thread computes each row's scalars, so that they
-// cost a wavefront's time once for 64 rows instead of once for each 64 / G.
-template <int G, int V, int U, bool LOSS>
+// G lanes to a row of at most 4 G V columns, R = 256 / G rows a block, read
+// once into registers.  Between the sums and the gradient one thread computes
+// each row's scalars, so that they cost a wavefront's time once for up to 64
+// rows instead of once for each 64 / G.
+template <int G, int V, bool LOSS>
 __global__ __launch_bounds__(THREADS) void rows_kernel(PolicyArgs a) {
-  constexpr int NG = THREADS / G, R = NG * U;
-  static_assert(R <= THREADS, "a thread for each row");
+  constexpr int R = THREADS / G;
   __shared__ float s_top[R], s_sum[R], s_c[R], s_inv[R];
   __shared__ int32_t s_act[R];
   __shared__ double s_exact[R];
-  const int lane = threadIdx.x % G, grp = threadIdx.x / G, t = threadIdx.x;
+  const int t = threadIdx.x, lane = t % G, grp = t / G;
   const int32_t first = (int32_t)(a.block0 + blockIdx.x) * R;
-  f4 z[U][V];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int64_t i = (int64_t)first + u * NG + grp;
-#pragma unroll
-    for (int k = 0; k < V; ++k)
-      z[u][k] = load_cols(a.Z + i * a.ld_z, (k * G + lane) * 4, i < a.n ? a.C : 0);
-  }
   const int32_t rows = min(R, a.n - first);
   const bool mine = t < rows;
+  const float* row = a.Z + ((int64_t)first + grp) * a.ld_z;
+  f4 z[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) z[k] = load_cols(row, (k * G + lane) * 4, grp < rows ? a.C : 0);
   RowIn r = {};
   if (mine) r = row_in(a, first + t, LOSS);
+  float top = max4(z[0]);
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    float top = max4(z[u][0]);
+  for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
+  top = group_max<G>(top);
+  const float shift = shift_of(top);
+  float part = 0.f;
 #pragma unroll
-    for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[u][k]));
-    top = group_max<G>(top);
-    const float shift = shift_of(top);
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < V; ++k) {
-      z[u][k] = exp4(z[u][k], shift);
-      sum += sum4(z[u][k]);
-    }
-    sum = group_sum<G>(sum);
-    if (lane == 0) {
-      s_top[u * NG + grp] = top;
-      s_sum[u * NG + grp] = sum;
-    }
+  for (int k = 0; k < V; ++k) {
+    z[k] = exp4(z[k], shift);
+    part += sum4(z[k]);
+  }
+  part = group_sum<G>(part);
+  if (lane == 0) {
+    s_top[grp] = top;
+    s_sum[grp] = part;
   }
   __syncthreads();
   double sum = mine ? (double)s_sum[t] : 1.0;
   if (!LOSS) {
     if (mine) a.logp[first + t] = (float)log_prob<false>(r, s_top[t], sum);
-  } else {
-    float c = 0.f;
-    Terms terms = {0.0, 0.0, 0.0};
-    bool near = false;
-    if (mine) {
-      const double lp = log_prob<false>(r, s_top[t], sum);
-      near = row_terms<false>(a, r, sum, lp, &terms, &c);
-      if (a.logp) a.logp[first + t] = (float)lp;
-      s_exact[t] = near ? -1.0 : 0.0;
-    }
-    if (__syncthreads_or(near)) {
-      for (int q = t >> 6; q < rows; q += THREADS / 64)
-        if (s_exact[q] < 0.0) {
-          const double s = exact_sum(a.Z + ((int64_t)first + q) * a.ld_z, a.C, s_top[q]);
-          if ((t & 63) == 0) s_exact[q] = s;
-        }
-      __syncthreads();
-      if (near) {
-        sum = s_exact[t];
-        row_terms<true>(a, r, sum, log_prob<true>(r, s_top[t], sum), &terms, &c);
+    return;
+  }
+  float c = 0.f;
+  Terms terms = {0.0, 0.0, 0.0};
+  bool near = false;
+  if (mine) {
+    const double lp = log_prob<false>(r, s_top[t], sum);
+    near = row_terms<false>(a, r, sum, lp, &terms, &c);
+    if (a.logp) a.logp[first + t] = (float)lp;
+    s_exact[t] = near ? -1.0 : 0.0;
+  }
+  if (__syncthreads_or(near)) {
+    for (int q = t >> 6; q < rows; q += THREADS / 64)
+      if (s_exact[q] < 0.0) {
+        const double s = exact_sum(a.Z + ((int64_t)first + q) * a.ld_z, a.C, s_top[q]);
+        if ((t & 63) == 0) s_exact[q] = s;
       }
+    __syncthreads();
+    if (near) {
+      sum = s_exact[t];
+      row_terms<true>(a, r, sum, log_prob<true>(r, s_top[t], sum), &terms, &c);
     }
+  }
+  if (a.dZ) {
     if (mine) {
       s_c[t] = c;
-      s_inv[t] = (float)(1.0 / sum);
+      s_inv[t] = 1.f / (float)sum;
       s_act[t] = r.act;
     }
     __syncthreads();
-    if (a.dZ) {
+    if (grp < rows) {
+      float* to = a.dZ + ((int64_t)first + grp) * a.ld_dz;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int q = u * NG + grp;
-        if (q >= rows) break;
-        float* to = a.dZ + ((int64_t)first + q) * a.ld_dz;
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          const int32_t col = (k * G + lane) * 4;
-          store_cols(to, col, a.C, grad4(z[u][k], col, s_act[q], s_c[q], s_inv[q]));
-        }
+      for (int k = 0; k < V; ++k) {
+        const int32_t col = (k * G + lane) * 4;
+        store_cols(to, col, a.C, grad4(z[k], col, s_act[grp], s_c[grp], s_inv[grp]));
       }
     }
-    store_terms(a, block_terms<THREADS>(terms));
   }
+  store_terms(a, block_terms<THREADS>(terms));
 }
 
 // ---------------------------------------------------------- one row a block
@@ -402,7 +392,7 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
       store_terms(a, terms);
       if (t == 0) {
         s_c = c;
-        s_inv = (float)(1.0 / sum);
+        s_inv = 1.f / (float)sum;
       }
     }
   }
@@ -494,7 +484,7 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   }
   if (t == 0 && chunk == 0) a.part[i] = terms;
   if (!a.dZ) return;
-  const float inv = (float)(1.0 / sum);
+  const float inv = 1.f / (float)sum;
   float* to = a.dZ + (int64_t)i * a.ld_dz;
 #pragma unroll
   for (int k = 0; k < SPLIT_V; ++k) {
@@ -506,18 +496,18 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
 
 // One block: out = the sum of `count` partial terms.  More: each its share of
 // them, to `shares`.  In a fixed order either way.
-constexpr int FINAL_THREADS = 1024;
-__global__ __launch_bounds__(FINAL_THREADS) void policy_final_kernel(
+template <int T>
+__global__ __launch_bounds__(T) void policy_final_kernel(
     int32_t count, const Terms* __restrict__ part, Terms* __restrict__ shares,
     float* __restrict__ out) {
   Terms t = {0.0, 0.0, 0.0};
-  for (int64_t k = (int64_t)blockIdx.x * FINAL_THREADS + threadIdx.x; k < count;
-       k += (int64_t)gridDim.x * FINAL_THREADS) {
+  for (int64_t k = (int64_t)blockIdx.x * T + threadIdx.x; k < count;
+       k += (int64_t)gridDim.x * T) {
     t.loss += part[k].loss;
     t.kl += part[k].kl;
     t.cut += part[k].cut;
   }
-  t = block_terms<FINAL_THREADS>(t);
+  t = block_terms<T>(t);
   if (threadIdx.x) return;
   if (gridDim.x == 1) store_out(out, t);
   else shares[blockIdx.x] = t;
@@ -525,28 +515,49 @@ __global__ __launch_bounds__(FINAL_THREADS) void policy_final_kernel(
 
 // ---------------------------------------------------------------- launches
 
-constexpr int32_t GROUP_COLS = 1024, BLOCK_COLS = 32768;
-
 struct Launch {
   void (*rows)(PolicyArgs);  // rows_kernel or block_kernel; NULL: split rows
   int32_t rows_per_block, threads;
 };
+template <int G, bool LOSS>
+Launch rows_of(int v) {
+  return {v == 3 ? rows_kernel<G, 3, LOSS> : rows_kernel<G, 4, LOSS>, THREADS / G, THREADS};
+}
+template <int T, bool LOSS>
+Launch block_of(int v) {
+  return {v == 3 ? block_kernel<T, 3, LOSS> : block_kernel<T, 4, LOSS>, 1, T};
+}
+
+// Three or four chunks of four columns a lane where the row is long enough,
+// and as few lanes as that takes.
 template <bool LOSS>
 Launch choose(int32_t C) {
-  if (C <= 4) return {rows_kernel<1, 1, 1, LOSS>, 256, THREADS};
-  if (C <= 8) return {rows_kernel<2, 1, 2, LOSS>, 256, THREADS};
-  if (C <= 16) return {rows_kernel<4, 1, 4, LOSS>, 256, THREADS};
-  if (C <= 32) return {rows_kernel<8, 1, 8, LOSS>, 256, THREADS};
-  if (C <= 64) return {rows_kernel<16, 1, 8, LOSS>, 128, THREADS};
-  if (C <= 128) return {rows_kernel<32, 1, 8, LOSS>, 64, THREADS};
-  if (C <= 256) return {rows_kernel<64, 1, 8, LOSS>, 32, THREADS};
-  if (C <= 512) return {rows_kernel<64, 2, 4, LOSS>, 16, THREADS};
-  if (C <= GROUP_COLS) return {rows_kernel<64, 4, 2, LOSS>, 8, THREADS};
-  if (C <= 2048) return {block_kernel<256, 2, LOSS>, 1, 256};
-  if (C <= 4096) return {block_kernel<256, 4, LOSS>, 1, 256};
-  if (C <= 8192) return {block_kernel<256, 8, LOSS>, 1, 256};
-  if (C <= 16384) return {block_kernel<1024, 4, LOSS>, 1, 1024};
-  if (C <= BLOCK_COLS) return {block_kernel<1024, 8, LOSS>, 1, 1024};
+  const int64_t q = ceil_div(C, 4);
+  if (q == 1) return {rows_kernel<1, 1, LOSS>, THREADS, THREADS};
+  if (q == 2) return {rows_kernel<1, 2, LOSS>, THREADS, THREADS};
+  int64_t lanes = 1;
+  while (lanes < 1024 && 4 * lanes < q) lanes *= 2;
+  const int v = (int)ceil_div(q, lanes);
+  switch (lanes) {
+    case 1: return rows_of<1, LOSS>(v);
+    case 2: return rows_of<2, LOSS>(v);
+    case 4: return rows_of<4, LOSS>(v);
+    case 8: return rows_of<8, LOSS>(v);
+    case 16: return rows_of<16, LOSS>(v);
+    case 32: return rows_of<32, LOSS>(v);
+    case 64: return block_of<64, LOSS>(v);
+    case 128: return block_of<128, LOSS>(v);
+    case 256: return block_of<256, LOSS>(v);
+    case 512: return block_of<512, LOSS>(v);
+  }
+  switch (v) {
+    case 3:
+    case 4: return block_of<1024, LOSS>(v);
+    case 5: return {block_kernel<1024, 5, LOSS>, 1, 1024};
+    case 6: return {block_kernel<1024, 6, LOSS>, 1, 1024};
+    case 7: return {block_kernel<1024, 7, LOSS>, 1, 1024};
+    case 8: return {block_kernel<1024, 8, LOSS>, 1, 1024};
+  }
   return {nullptr, 0, 0};
 }
 
@@ -596,10 +607,14 @@ gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
   }
   if (LOSS && !(l.rows && parts == 1)) {  // (one block of rows has written `out` itself)
     Terms* shares = reinterpret_cast<Terms*>(ws + o.shares);
+    const Terms* from = parts > FINAL_MOST ? shares : a.part;
+    const int32_t count = parts > FINAL_MOST ? SHARES : parts;
     if (parts > FINAL_MOST)
-      policy_final_kernel<<<SHARES, FINAL_THREADS, 0, stream>>>(parts, a.part, shares, nullptr);
-    policy_final_kernel<<<1, FINAL_THREADS, 0, stream>>>(
-        parts > FINAL_MOST ? SHARES : parts, parts > FINAL_MOST ? shares : a.part, nullptr, a.out);
+      policy_final_kernel<1024><<<SHARES, 1024, 0, stream>>>(parts, a.part, shares, nullptr);
+    if (count <= 1024)
+      policy_final_kernel<256><<<1, 256, 0, stream>>>(count, from, nullptr, a.out);
+    else
+      policy_final_kernel<1024><<<1, 1024, 0, stream>>>(count, from, nullptr, a.out);
   }
   timer_end(GNN_K_LOSS, (a.dZ ? 8.0 : 4.0) * a.n * a.C, stream);
   GNN_HIP(hipGetLastError());
@@ -685,6 +700,7 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
   a.lo = 1.0 - clip_lo;
   a.hi = 1.0 + clip_hi;
   a.beta = beta;
+  a.mean = n > 0 ? 1.0 / n : 0.0;
   a.out = out;
   a.logp = logp;
   a.dZ = dZ;
