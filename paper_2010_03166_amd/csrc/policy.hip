@@ -68,24 +68,33 @@ __device__ inline RowIn row_in(const PolicyArgs& a, int32_t i, bool loss) {
 }
 
 // Scalar functions.  Sums of fp32 exponentials are good to (20 + ln C) 2^-24
-// at worst, 2e-6, so logarithms and exponentials as good as 2e-7 lose nothing
-// beside them, and library functions of doubles would hold a hundred registers
-// for their coefficients.  Where a ratio is as near to a border of the clip
-// as those errors (rows are rarely), everything is computed once more in
-// doubles, slowly.
+// at worst, below 2.5e-6 for any C, so logarithms and exponentials as good as
+// 2e-7 lose little beside them, and library functions of doubles would hold a
+// hundred registers for their coefficients.  A row whose ratio is as near to
+// a border of the clip as those errors, one in 1e5 or so, is computed once
+// more in doubles.
+constexpr double NEAR = 4e-6;
 
-// exp(x) to a few 2^-53 for |x| < 700: 2^k times the series of the remainder
-// (below 0.35, 15 terms), each term from the one before.
+// exp(x) to a few 2^-53 for |x| < 700: 2^k times the remainder's series
+// (|r| < 0.35: the first term left out, r^14 / 14!, is below 5e-18).
 __device__ inline double exp_exact(double x) {
   if (!(x > -700.0)) return x < 0.0 ? 0.0 : x;  // 0, or NaN
   const double k = rint(x * 1.4426950408889634);
   const double r = fma(-k, 2.3190468138462996e-17, fma(-k, 0.6931471805599453, x));
-  double term = 1.0, sum = 1.0;
-#pragma unroll 1
-  for (int i = 1; i < 16; ++i) {
-    term *= r / i;
-    sum += term;
-  }
+  double sum = 1.0 / 6227020800.0;
+  sum = fma(sum, r, 1.0 / 479001600.0);
+  sum = fma(sum, r, 1.0 / 39916800.0);
+  sum = fma(sum, r, 1.0 / 3628800.0);
+  sum = fma(sum, r, 1.0 / 362880.0);
+  sum = fma(sum, r, 1.0 / 40320.0);
+  sum = fma(sum, r, 1.0 / 5040.0);
+  sum = fma(sum, r, 1.0 / 720.0);
+  sum = fma(sum, r, 1.0 / 120.0);
+  sum = fma(sum, r, 1.0 / 24.0);
+  sum = fma(sum, r, 1.0 / 6.0);
+  sum = fma(sum, r, 0.5);
+  sum = fma(sum, r, 1.0);
+  sum = fma(sum, r, 1.0);
   return ldexp(sum, (int)fmin(k, 2000.0));
 }
 
@@ -141,7 +150,7 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
   if (!r.chosen || sum == 0.0 || w == 0.0) return false;
   const double A = r.adv, x = lp - (double)r.old_lp;
   const double rho = !a.old_lp ? 1.0 : EXACT ? exp_exact(x) : exp_quick(x);
-  const bool near = a.old_lp && (fabs(rho - a.lo) <= 1e-5 * rho || fabs(rho - a.hi) <= 1e-5 * rho);
+  const bool near = a.old_lp && (fabs(rho - a.lo) <= NEAR * rho || fabs(rho - a.hi) <= NEAR * rho);
   const double ra = rho * A, ca = fmin(fmax(rho, a.lo), a.hi) * A;
   const bool cut = ra > ca;  // false for a NaN, which then shows in ra
   double slope = cut ? 0.0 : -ra, loss = -(cut ? ca : ra);
@@ -266,10 +275,10 @@ __device__ inline f4 grad4(f4 e, int32_t col, int32_t act, float c, float inv) {
 // each row's scalars, so that they cost a wavefront's time once for up to 64
 // rows instead of once for each 64 / G.
 template <int G, int V, bool LOSS>
-__global__ __launch_bounds__(THREADS) void rows_kernel(PolicyArgs a) {
+__global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
   constexpr int R = THREADS / G;
   __shared__ float s_top[R], s_sum[R], s_c[R], s_inv[R];
-  __shared__ int32_t s_act[R];
+  __shared__ int32_t s_act[R], s_near;
   __shared__ double s_exact[R];
   const int t = threadIdx.x, lane = t % G, grp = t / G;
   const int32_t first = (int32_t)(a.block0 + blockIdx.x) * R;
@@ -297,47 +306,50 @@ __global__ __launch_bounds__(THREADS) void rows_kernel(PolicyArgs a) {
     s_top[grp] = top;
     s_sum[grp] = part;
   }
+  if (t == 0) s_near = 0;
   __syncthreads();
   double sum = mine ? (double)s_sum[t] : 1.0;
   if (!LOSS) {
     if (mine) a.logp[first + t] = (float)log_prob<false>(r, s_top[t], sum);
     return;
   }
-  float c = 0.f;
   Terms terms = {0.0, 0.0, 0.0};
   bool near = false;
   if (mine) {
     const double lp = log_prob<false>(r, s_top[t], sum);
-    near = row_terms<false>(a, r, sum, lp, &terms, &c);
+    near = row_terms<false>(a, r, sum, lp, &terms, &s_c[t]);
     if (a.logp) a.logp[first + t] = (float)lp;
+    s_inv[t] = 1.f / (float)sum;
+    s_act[t] = r.act;
     s_exact[t] = near ? -1.0 : 0.0;
+    if (near) s_near = 1;
   }
-  if (__syncthreads_or(near)) {
+  __syncthreads();
+  if (s_near) {
     for (int q = t >> 6; q < rows; q += THREADS / 64)
       if (s_exact[q] < 0.0) {
-        const double s = exact_sum(a.Z + ((int64_t)first + q) * a.ld_z, a.C, s_top[q]);
-        if ((t & 63) == 0) s_exact[q] = s;
+        const double exact = exact_sum(a.Z + ((int64_t)first + q) * a.ld_z, a.C, s_top[q]);
+        if ((t & 63) == 0) s_exact[q] = exact;
       }
     __syncthreads();
     if (near) {
       sum = s_exact[t];
-      row_terms<true>(a, r, sum, log_prob<true>(r, s_top[t], sum), &terms, &c);
-    }
-  }
-  if (a.dZ) {
-    if (mine) {
-      s_c[t] = c;
+      row_terms<true>(a, r, sum, log_prob<true>(r, s_top[t], sum), &terms, &s_c[t]);
       s_inv[t] = 1.f / (float)sum;
-      s_act[t] = r.act;
     }
     __syncthreads();
-    if (grp < rows) {
-      float* to = a.dZ + ((int64_t)first + grp) * a.ld_dz;
+    // read once more, so that this branch has the registers
+    const float again = shift_of(s_top[grp]);
 #pragma unroll
-      for (int k = 0; k < V; ++k) {
-        const int32_t col = (k * G + lane) * 4;
-        store_cols(to, col, a.C, grad4(z[k], col, s_act[grp], s_c[grp], s_inv[grp]));
-      }
+    for (int k = 0; k < V; ++k)
+      z[k] = exp4(load_cols(row, (k * G + lane) * 4, grp < rows ? a.C : 0), again);
+  }
+  if (a.dZ && grp < rows) {
+    float* to = a.dZ + ((int64_t)first + grp) * a.ld_dz;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      const int32_t col = (k * G + lane) * 4;
+      store_cols(to, col, a.C, grad4(z[k], col, s_act[grp], s_c[grp], s_inv[grp]));
     }
   }
   store_terms(a, block_terms<THREADS>(terms));
@@ -413,7 +425,7 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
 // one launch for the chunks' sums, one that joins a row's sums, computes its
 // scalars in every block of the row alike, and writes the chunk's gradient
 // from a second reading (out of the caches, for the few rows that are so long).
-constexpr int SPLIT_V = 8;
+constexpr int SPLIT_V = 4;
 constexpr int SPLIT_COLS = 4 * THREADS * SPLIT_V;
 __host__ __device__ inline int32_t chunks_of(int32_t C) {
   return (int32_t)ceil_div(C, SPLIT_COLS);
@@ -500,12 +512,20 @@ template <int T>
 __global__ __launch_bounds__(T) void policy_final_kernel(
     int32_t count, const Terms* __restrict__ part, Terms* __restrict__ shares,
     float* __restrict__ out) {
+  constexpr int AT_ONCE = 8;  // reads under way, each from another XCD's block
   Terms t = {0.0, 0.0, 0.0};
-  for (int64_t k = (int64_t)blockIdx.x * T + threadIdx.x; k < count;
-       k += (int64_t)gridDim.x * T) {
-    t.loss += part[k].loss;
-    t.kl += part[k].kl;
-    t.cut += part[k].cut;
+  const int64_t step = (int64_t)gridDim.x * T;
+  for (int64_t k = (int64_t)blockIdx.x * T + threadIdx.x; k < count; k += AT_ONCE * step) {
+    Terms x[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j)
+      x[j] = k + j * step < count ? part[k + j * step] : Terms{0.0, 0.0, 0.0};
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      t.loss += x[j].loss;
+      t.kl += x[j].kl;
+      t.cut += x[j].cut;
+    }
   }
   t = block_terms<T>(t);
   if (threadIdx.x) return;
