@@ -32,8 +32,6 @@ struct Tensor {
   int64_t count;
   int64_t first;  // blocks of BLOCK elements in the tensors before it
   double decay;
-  int32_t vec;    // aligned for 16-byte accesses (8-bit moments: 4-byte)
-  int32_t pad;
 };
 struct Piece {
   int32_t tensor, index;  // elements [index PIECE, (index + 1) PIECE)
@@ -79,26 +77,50 @@ __global__ __launch_bounds__(THREADS) void plan_kernel(PlanBatch b, void* plan) 
 
 // ------------------------------------------------------------------ norm
 
-template <bool VEC>
-__device__ inline float4 load4(const float* p, int64_t i, int64_t count) {
-  if (VEC && i + 4 <= count) return *reinterpret_cast<const float4*>(p + i);
-  float4 r;
-  r.x = i < count ? p[i] : 0.f;
-  r.y = i + 1 < count ? p[i + 1] : 0.f;
-  r.z = i + 2 < count ? p[i + 2] : 0.f;
-  r.w = i + 3 < count ? p[i + 3] : 0.f;
+// Four elements at a time from any multiple of 4 bytes (codes: from any byte),
+// which global memory instructions of 16 bytes allow: tensors in one flat
+// buffer need no padding.  FULL: all four exist.
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef f4 f4u __attribute__((aligned(4)));
+typedef uint32_t u32u __attribute__((aligned(1)));
+
+template <bool FULL>
+__device__ inline f4 load4(const float* p, int64_t i, int64_t count) {
+  if (FULL || i + 4 <= count) return *reinterpret_cast<const f4u*>(p + i);
+  f4 r = {0.f, 0.f, 0.f, 0.f};
+  if (i < count) r.x = p[i];
+  if (i + 1 < count) r.y = p[i + 1];
+  if (i + 2 < count) r.z = p[i + 2];
   return r;
 }
-template <bool VEC>
-__device__ inline void store4(float* p, int64_t i, int64_t count, float4 r) {
-  if (VEC && i + 4 <= count) {
-    *reinterpret_cast<float4*>(p + i) = r;
+template <bool FULL>
+__device__ inline void store4(float* p, int64_t i, int64_t count, f4 r) {
+  if (FULL || i + 4 <= count) {
+    *reinterpret_cast<f4u*>(p + i) = r;
     return;
   }
   if (i < count) p[i] = r.x;
   if (i + 1 < count) p[i + 1] = r.y;
   if (i + 2 < count) p[i + 2] = r.z;
-  if (i + 3 < count) p[i + 3] = r.w;
+}
+template <bool FULL>
+__device__ inline uint32_t load_codes(const uint8_t* p, int64_t i, int64_t count) {
+  if (FULL || i + 4 <= count) return *reinterpret_cast<const u32u*>(p + i);
+  uint32_t r = 0;
+  if (i < count) r = p[i];
+  if (i + 1 < count) r |= (uint32_t)p[i + 1] << 8;
+  if (i + 2 < count) r |= (uint32_t)p[i + 2] << 16;
+  return r;
+}
+template <bool FULL>
+__device__ inline void store_codes(uint8_t* p, int64_t i, int64_t count, uint32_t r) {
+  if (FULL || i + 4 <= count) {
+    *reinterpret_cast<u32u*>(p + i) = r;
+    return;
+  }
+  if (i < count) p[i] = (uint8_t)r;
+  if (i + 1 < count) p[i + 1] = (uint8_t)(r >> 8);
+  if (i + 2 < count) p[i + 2] = (uint8_t)(r >> 16);
 }
 
 __device__ inline double block_sum(double v) {
@@ -112,17 +134,19 @@ __device__ inline double block_sum(double v) {
   return s[0];
 }
 
-template <bool VEC>
+constexpr int AT_ONCE = PIECE / (4 * THREADS);  // accesses of a thread to a piece
+
+template <bool FULL>
 __device__ inline double squares(const Tensor& t, int64_t base) {
+  f4 g[AT_ONCE];
+#pragma unroll
+  for (int k = 0; k < AT_ONCE; ++k)
+    g[k] = load4<FULL>(t.G, base + (k * THREADS + threadIdx.x) * 4, t.count);
   double sum = 0.0;
 #pragma unroll
-  for (int k = 0; k < PIECE / (4 * THREADS); ++k) {
-    const float4 g = load4<VEC>(t.G, base + (k * THREADS + threadIdx.x) * 4, t.count);
-    sum = fma((double)g.x, (double)g.x, sum);
-    sum = fma((double)g.y, (double)g.y, sum);
-    sum = fma((double)g.z, (double)g.z, sum);
-    sum = fma((double)g.w, (double)g.w, sum);
-  }
+  for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum = fma((double)g[k][j], (double)g[k][j], sum);
   return sum;
 }
 
@@ -135,7 +159,7 @@ __global__ __launch_bounds__(THREADS) void norm_part_kernel(const void* plan, in
     const Piece at = p.pieces[c];
     const Tensor& t = p.tensors[at.tensor];
     const int64_t base = (int64_t)at.index * PIECE;
-    sum += t.vec ? squares<true>(t, base) : squares<false>(t, base);
+    sum += base + PIECE <= t.count ? squares<true>(t, base) : squares<false>(t, base);
   }
   sum = block_sum(sum);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -154,7 +178,7 @@ __global__ __launch_bounds__(THREADS) void norm_final_kernel(int32_t count,
 
 struct Coef {
   double lr, b1, omb1, b2, omb2;
-  float eps, c1, c2, lrf;
+  float eps, step, root;  // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   const float* norm;
   double max_norm;
   uint64_t base;  // output t of the generator started at the seed
@@ -170,8 +194,10 @@ __device__ inline bool clip_factor(const Coef& a, double* k) {
   return true;
 }
 
+// The bias corrections are in the coefficients, and the division is a
+// reciprocal good to 1 ulp: one quotient a weight instead of three.
 __device__ inline float updated(float w, float m, float v, float keep, const Coef& a) {
-  return keep * w - a.lrf * (m / a.c1) / (sqrtf(v / a.c2) + a.eps);
+  return keep * w - a.step * m * __builtin_amdgcn_rcpf(sqrtf(v) * a.root + a.eps);
 }
 
 // 8-bit values: MAN bits of mantissa, the exponent of the smallest normal
@@ -185,126 +211,163 @@ struct FormatV {  // OCP e5m2
   static constexpr double most = 57344.0;
 };
 
-template <class F>
-__device__ inline double decode(uint32_t code) {
-  const uint32_t mag = code & 127u, ex = mag >> F::MAN;
-  const int32_t man = (int32_t)(mag & ((1u << F::MAN) - 1)) + (ex ? 1 << F::MAN : 0);
-  const double x = ldexp((double)man, (int)(ex ? ex : 1u) - 1 + F::EMIN - F::MAN);
-  return code & 128u ? -x : x;
+__device__ inline uint32_t high_word(double x) {
+  return (uint32_t)((uint64_t)__double_as_longlong(x) >> 32);
 }
 
-// Code of y >= 0 in units of the scale, rounded up where r / 2^16 reaches
-// past the distance to the lower neighbour: with e the exponent of y (at
-// least EMIN) neighbours are 2^(e - MAN) apart.
+// Code of y >= 0 in units of the scale, rounded up where (r + 1/2) / 2^16
+// reaches past the distance to the lower neighbour.  A double's exponent and
+// mantissa, read as one number, count neighbours: MAN + 11 bits in, one step
+// of the code; below the smallest normal 2^EMIN is added first, which leaves
+// their even spacing in the mantissa.  The 16 bits of r and the half after
+// them end above bit 32, so the upper word decides alone.
 template <class F>
 __device__ inline uint32_t encode(double y, uint32_t r) {
-  const int e = max((int)((uint64_t)__double_as_longlong(y) >> 52) - 1023, F::EMIN);
-  const double k = ldexp(y, F::MAN - e) + ((double)r + 0.5) * (1.0 / 65536.0);
-  return min((uint32_t)((e - F::EMIN) << F::MAN) + (uint32_t)k, (uint32_t)F::TOP);
+  constexpr uint32_t base = (uint32_t)(1023 + F::EMIN) << 20;  // 2^EMIN
+  const bool small = y < __builtin_ldexp(1.0, F::EMIN);
+  const uint32_t hi = high_word(small ? y + __builtin_ldexp(1.0, F::EMIN) : y) -
+                      (small ? base : base - (1u << 20));
+  constexpr int SH = 20 - F::MAN;  // bits of the upper word after the code's
+  return min((hi + ((2 * r + 1) << (SH - 17))) >> SH, (uint32_t)F::TOP);
 }
 
-// Largest magnitude in the wavefront, ordered by bits: NaN above infinity.
-__device__ inline uint64_t wave_max_bits(uint64_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) x = max(x, (uint64_t)__shfl_xor((unsigned long long)x, d, 64));
-  return x;
-}
-__device__ inline uint64_t magnitude(double x) {
-  return (uint64_t)__double_as_longlong(x) & 0x7FFFFFFFFFFFFFFFull;
-}
-
-// Scale of a block whose largest magnitude is `top`.
+// A block's scale and its reciprocal (NaN, 0 where it has a NaN or an
+// infinity).  `top`: the lane's largest magnitude; the wavefront's is found
+// among their roundings to fp32, then read from its lane (all of those that
+// round alike): six steps of 32 bits instead of 64.
 template <class F>
-__device__ inline float scale_of(uint64_t top) {
-  const float s = (float)(__longlong_as_double((long long)top) / F::most);
-  return s < 0x1p-126f ? 0x1p-126f : s;
-}
-
-template <bool VEC>
-__device__ inline uint32_t load_codes(const uint8_t* p, int64_t i, int64_t count) {
-  if (VEC && i + 4 <= count) return *reinterpret_cast<const uint32_t*>(p + i);
-  uint32_t r = 0;
-  for (int k = 0; k < 4; ++k)
-    if (i + k < count) r |= (uint32_t)p[i + k] << (8 * k);
-  return r;
-}
-template <bool VEC>
-__device__ inline void store_codes(uint8_t* p, int64_t i, int64_t count, uint32_t r) {
-  if (VEC && i + 4 <= count) {
-    *reinterpret_cast<uint32_t*>(p + i) = r;
-    return;
+__device__ inline float block_scale(double top, bool bad, double* inverse) {
+  const float mine = (float)top;
+  float most = mine;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+  // doubles >= 0 are ordered as their bits; each turn finds a larger one, so
+  // lanes that are all alike take one turn
+  const uint64_t own = (uint64_t)__double_as_longlong(top);
+  uint64_t bits = 0;
+  for (uint64_t lanes = __ballot(mine == most && own > bits); lanes;
+       lanes = __ballot(mine == most && own > bits)) {
+    const int lane = __ffsll((unsigned long long)lanes) - 1;
+    bits = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(own >> 32), lane) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)own, lane);
   }
-  for (int k = 0; k < 4; ++k)
-    if (i + k < count) p[i + k] = (uint8_t)(r >> (8 * k));
+  const double scaled = __longlong_as_double((long long)bits) * (1.0 / F::most);
+  float s = (float)scaled;
+  if (s < 0x1p-126f) s = 0x1p-126f;
+  if (bad || !(s < INFINITY)) {
+    *inverse = 0.0;
+    return NAN;
+  }
+  const double x = __builtin_amdgcn_rcp((double)s);
+  const double x1 = fma(fma(-(double)s, x, 1.0), x, x);
+  *inverse = fma(fma(-(double)s, x1, 1.0), x1, x1);
+  return s;
 }
 
-// Four consecutive elements from i.
-template <bool VEC>
-__device__ inline void step32(const Tensor& t, int64_t i, float k, float keep, const Coef& a) {
+struct Raw32 {
+  f4 w, g, m, v;
+};
+struct Raw8 {
+  f4 w, g;
+  uint32_t m, v;
+  float ms, vs;
+};
+
+// A thread's accesses to a piece are all under way before the first is used.
+template <bool FULL>
+__device__ inline void piece32(const Tensor& t, int64_t base, double kd, float keep,
+                               const Coef& a) {
   float *m = static_cast<float*>(t.m), *v = static_cast<float*>(t.v);
-  float w4[4], g4[4], m4[4], v4[4];
-  *reinterpret_cast<float4*>(w4) = load4<VEC>(t.W, i, t.count);
-  *reinterpret_cast<float4*>(g4) = load4<VEC>(t.G, i, t.count);
-  *reinterpret_cast<float4*>(m4) = load4<VEC>(m, i, t.count);
-  *reinterpret_cast<float4*>(v4) = load4<VEC>(v, i, t.count);
+  Raw32 x[AT_ONCE];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float g = g4[j] * k;
-    m4[j] = (float)a.b1 * m4[j] + (float)a.omb1 * g;
-    v4[j] = (float)a.b2 * v4[j] + (float)a.omb2 * g * g;
-    w4[j] = updated(w4[j], m4[j], v4[j], keep, a);
+  for (int q = 0; q < AT_ONCE; ++q) {
+    const int64_t i = base + (q * THREADS + threadIdx.x) * 4;
+    x[q] = {load4<FULL>(t.W, i, t.count), load4<FULL>(t.G, i, t.count),
+            load4<FULL>(m, i, t.count), load4<FULL>(v, i, t.count)};
   }
-  store4<VEC>(t.W, i, t.count, *reinterpret_cast<float4*>(w4));
-  store4<VEC>(m, i, t.count, *reinterpret_cast<float4*>(m4));
-  store4<VEC>(v, i, t.count, *reinterpret_cast<float4*>(v4));
+  const float k = (float)kd, b1 = (float)a.b1, omb1 = (float)a.omb1, b2 = (float)a.b2,
+              omb2 = (float)a.omb2;
+#pragma unroll
+  for (int q = 0; q < AT_ONCE; ++q) {
+    const int64_t i = base + (q * THREADS + threadIdx.x) * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float g = x[q].g[j] * k;
+      x[q].m[j] = b1 * x[q].m[j] + omb1 * g;
+      x[q].v[j] = b2 * x[q].v[j] + omb2 * g * g;
+      x[q].w[j] = updated(x[q].w[j], x[q].m[j], x[q].v[j], keep, a);
+    }
+    store4<FULL>(t.W, i, t.count, x[q].w);
+    store4<FULL>(m, i, t.count, x[q].m);
+    store4<FULL>(v, i, t.count, x[q].v);
+  }
 }
 
-// The same with 8-bit moments; the wavefront's 64 lanes hold one block.
-template <bool VEC>
-__device__ inline void step8(const Tensor& t, int64_t i, double k, float keep, const Coef& a) {
+// 8-bit moments: the 64 lanes of a wavefront hold one block of 256.
+template <bool FULL>
+__device__ inline void piece8(const Tensor& t, int64_t base, double k, float keep,
+                              const Coef& a) {
   uint8_t *m = static_cast<uint8_t*>(t.m), *v = static_cast<uint8_t*>(t.v);
-  const int64_t block = i / BLOCK;  // the same in all lanes
-  float w4[4], g4[4];
-  *reinterpret_cast<float4*>(w4) = load4<VEC>(t.W, i, t.count);
-  *reinterpret_cast<float4*>(g4) = load4<VEC>(t.G, i, t.count);
-  const uint32_t mc = load_codes<VEC>(m, i, t.count), vc = load_codes<VEC>(v, i, t.count);
-  const double ms = t.m_scale[block], vs = t.v_scale[block];
-  double m4[4], v4[4];
-  uint64_t mtop = 0, vtop = 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Raw8 x[AT_ONCE];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const double g = (double)g4[j] * k;
-    m4[j] = a.b1 * (decode<FormatM>(mc >> (8 * j) & 255u) * ms) + a.omb1 * g;
-    v4[j] = a.b2 * (decode<FormatV>(vc >> (8 * j) & 255u) * vs) + a.omb2 * g * g;
-    mtop = max(mtop, magnitude(m4[j]));
-    vtop = max(vtop, magnitude(v4[j]));
-    w4[j] = updated(w4[j], (float)m4[j], (float)v4[j], keep, a);
+  for (int q = 0; q < AT_ONCE; ++q) {
+    const int64_t first = base + (q * (THREADS / 64) + wave) * BLOCK, i = first + lane * 4;
+    if (!FULL && first >= t.count) break;
+    x[q] = {load4<FULL>(t.W, i, t.count), load4<FULL>(t.G, i, t.count),
+            load_codes<FULL>(m, i, t.count), load_codes<FULL>(v, i, t.count),
+            t.m_scale[first / BLOCK], t.v_scale[first / BLOCK]};
   }
-  const float msn = scale_of<FormatM>(wave_max_bits(mtop));
-  const float vsn = scale_of<FormatV>(wave_max_bits(vtop));
-  uint32_t mo = 0, vo = 0;
+  const double gm = a.omb1 * k, gv = a.omb2 * k * k;
 #pragma unroll
-  for (int j = 0; j < 4; j += 2) {
-    const uint64_t r = splitmix(a.base, (uint64_t)(t.first * BLOCK + i + j) / 2);
+  for (int q = 0; q < AT_ONCE; ++q) {
+    const int64_t first = base + (q * (THREADS / 64) + wave) * BLOCK, i = first + lane * 4;
+    if (!FULL && first >= t.count) break;
+    const double ms = a.b1 * (double)x[q].ms, vs = a.b2 * (double)x[q].vs;
+    const float mo[4] = {__builtin_amdgcn_cvt_f32_fp8(x[q].m, 0),
+                         __builtin_amdgcn_cvt_f32_fp8(x[q].m, 1),
+                         __builtin_amdgcn_cvt_f32_fp8(x[q].m, 2),
+                         __builtin_amdgcn_cvt_f32_fp8(x[q].m, 3)};
+    const float vo[4] = {__builtin_amdgcn_cvt_f32_bf8(x[q].v, 0),
+                         __builtin_amdgcn_cvt_f32_bf8(x[q].v, 1),
+                         __builtin_amdgcn_cvt_f32_bf8(x[q].v, 2),
+                         __builtin_amdgcn_cvt_f32_bf8(x[q].v, 3)};
+    double m4[4], v4[4], mtop = 0.0, vtop = 0.0;
+    uint32_t gtop = 0;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const uint32_t rr = (uint32_t)(r >> (32 * q));
-      const double ym = fabs(m4[j + q]) / (double)msn, yv = v4[j + q] / (double)vsn;
-      // a block with a NaN or an infinity: its scale says so
-      uint32_t cm = msn < INFINITY ? encode<FormatM>(ym, rr & 0xFFFFu) : 0u;
-      uint32_t cv = vsn < INFINITY ? encode<FormatV>(yv, rr >> 16) : 0u;
-      if (m4[j + q] < 0.0) cm |= 128u;
-      if (yv > 0.0 && cv == 0u) cv = 1u;
-      mo |= cm << (8 * (j + q));
-      vo |= cv << (8 * (j + q));
+    for (int j = 0; j < 4; ++j) {
+      const double g = (double)x[q].g[j];
+      m4[j] = fma((double)mo[j], ms, g * gm);
+      v4[j] = fma((double)vo[j], vs, g * gv * g);
+      mtop = fmax(mtop, fabs(m4[j]));
+      vtop = fmax(vtop, v4[j]);
+      gtop = max(gtop, __float_as_uint(x[q].g[j]) & 0x7FFFFFFFu);
+      x[q].w[j] = updated(x[q].w[j], (float)m4[j], (float)v4[j], keep, a);
     }
-  }
-  store4<VEC>(t.W, i, t.count, *reinterpret_cast<float4*>(w4));
-  store_codes<VEC>(m, i, t.count, mo);
-  store_codes<VEC>(v, i, t.count, vo);
-  if ((threadIdx.x & 63) == 0) {
-    t.m_scale[block] = msn;
-    t.v_scale[block] = vsn;
+    store4<FULL>(t.W, i, t.count, x[q].w);
+    // a NaN or an infinity: the scales say so
+    const bool bad = __ballot(gtop >= 0x7F800000u) != 0;
+    double im, iv;
+    const float msn = block_scale<FormatM>(mtop, bad || !(x[q].ms < INFINITY), &im);
+    const float vsn = block_scale<FormatV>(vtop, bad || !(x[q].vs < INFINITY), &iv);
+    uint32_t mc = 0, vc = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint64_t both = splitmix(a.base, (uint64_t)(t.first * BLOCK + i + j) / 2);
+      const uint32_t r = (uint32_t)(both >> (32 * (j & 1)));
+      const uint32_t cm = encode<FormatM>(fabs(m4[j]) * im, r & 0xFFFFu) |
+                          (high_word(m4[j]) >> 24 & 128u);
+      uint32_t cv = encode<FormatV>(v4[j] * iv, r >> 16);
+      if (cv == 0 && v4[j] > 0.0) cv = 1;
+      mc |= cm << (8 * j);
+      vc |= cv << (8 * j);
+    }
+    store_codes<FULL>(m, i, t.count, mc);
+    store_codes<FULL>(v, i, t.count, vc);
+    if (lane == 0) {
+      t.m_scale[first / BLOCK] = msn;
+      t.v_scale[first / BLOCK] = vsn;
+    }
   }
 }
 
@@ -317,18 +380,14 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const void* plan, int32_
   const Piece at = p.pieces[blockIdx.x];
   const Tensor& t = p.tensors[at.tensor];
   const float keep = (float)(1.0 - a.lr * t.decay);
-#pragma unroll
-  for (int q = 0; q < PIECE / (4 * THREADS); ++q) {
-    const int64_t i = (int64_t)at.index * PIECE + (q * THREADS + threadIdx.x) * 4;
-    // whole blocks past the end: nothing (uniform in a wavefront)
-    if (i / BLOCK * BLOCK >= t.count) break;
-    if (BITS == 32) {
-      if (t.vec) step32<true>(t, i, (float)k, keep, a);
-      else step32<false>(t, i, (float)k, keep, a);
-    } else {
-      if (t.vec) step8<true>(t, i, k, keep, a);
-      else step8<false>(t, i, k, keep, a);
-    }
+  const int64_t base = (int64_t)at.index * PIECE;
+  const bool full = base + PIECE <= t.count;
+  if (BITS == 32) {
+    if (full) piece32<true>(t, base, k, keep, a);
+    else piece32<false>(t, base, k, keep, a);
+  } else {
+    if (full) piece8<true>(t, base, k, keep, a);
+    else piece8<false>(t, base, k, keep, a);
   }
 }
 
@@ -442,9 +501,7 @@ gnn_status gnn_params_build_plan(const gnn_params* params, void* plan, size_t pl
     int64_t most = 0;
     for (int32_t j = 0; j < b.count; ++j) {
       const gnn_param& q = params->p[k + j];
-      const uintptr_t al = params->state_bits == 8 ? 4 : 16;
-      const bool vec = aligned(q.W, 16) && aligned(q.G, 16) && aligned(q.m, al) && aligned(q.v, al);
-      b.t[j] = {q.W, q.G, q.m, q.v, q.m_scale, q.v_scale, q.count, first, q.weight_decay, vec, 0};
+      b.t[j] = {q.W, q.G, q.m, q.v, q.m_scale, q.v_scale, q.count, first, q.weight_decay};
       b.piece0[j] = piece0;
       piece0 += ceil_div(q.count, PIECE);
       first += ceil_div(q.count, BLOCK);
@@ -523,8 +580,9 @@ gnn_status gnn_adamw_step(const gnn_params* params, double lr, double beta1, dou
   }
   if (pieces == 0) return GNN_OK;
   const Coef a = {lr, beta1, 1.0 - beta1, beta2, 1.0 - beta2, (float)eps,
-                  (float)(1.0 - std::pow(beta1, t)), (float)(1.0 - std::pow(beta2, t)), (float)lr,
-                  norm, max_norm, splitmix(seed, (uint64_t)t)};
+                  (float)(lr / (1.0 - std::pow(beta1, t))),
+                  (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, t))), norm, max_norm,
+                  splitmix(seed, (uint64_t)t)};
   timer_begin(GNN_K_UPDATE, stream);
   if (params->state_bits == 32)
     adamw_kernel<32><<<(unsigned)pieces, THREADS, 0, stream>>>(params->plan, params->n, a);
