@@ -17,7 +17,7 @@ namespace {
 
 constexpr int THREADS = 256;
 constexpr int BLOCK = GNN_STATE_BLOCK;  // one wavefront, four elements a lane
-constexpr int PIECE = 2048;
+constexpr int PIECE = 1024;
 constexpr int NORM_BLOCKS = 2048;  // partial sums of the norm
 
 struct PlanHead {
@@ -194,20 +194,22 @@ __device__ inline bool clip_factor(const Coef& a, double* k) {
   return true;
 }
 
-// The bias corrections are in the coefficients, and the division is a
-// reciprocal good to 1 ulp: one quotient a weight instead of three.
-__device__ inline float updated(float w, float m, float v, float keep, const Coef& a) {
-  return keep * w - a.step * m * __builtin_amdgcn_rcpf(sqrtf(v) * a.root + a.eps);
+// The bias corrections are in the coefficients, the quotient is a product
+// with a reciprocal good to 1 ulp, and the root the hardware's of doubles
+// (good to 2^-25, and over the whole range of v), rounded.
+__device__ inline float updated(float w, float m, double v, float keep, const Coef& a) {
+  const float root = (float)__builtin_amdgcn_sqrt(v);
+  return keep * w - a.step * m * __builtin_amdgcn_rcpf(root * a.root + a.eps);
 }
 
 // 8-bit values: MAN bits of mantissa, the exponent of the smallest normal
-// EMIN, the largest code TOP of value `most`.
+// EMIN, the largest value `most`.
 struct FormatM {  // OCP e4m3
-  static constexpr int MAN = 3, EMIN = -6, TOP = 126;
+  static constexpr int MAN = 3, EMIN = -6;
   static constexpr double most = 448.0;
 };
 struct FormatV {  // OCP e5m2
-  static constexpr int MAN = 2, EMIN = -14, TOP = 123;
+  static constexpr int MAN = 2, EMIN = -14;
   static constexpr double most = 57344.0;
 };
 
@@ -215,20 +217,19 @@ __device__ inline uint32_t high_word(double x) {
   return (uint32_t)((uint64_t)__double_as_longlong(x) >> 32);
 }
 
-// Code of y >= 0 in units of the scale, rounded up where (r + 1/2) / 2^16
-// reaches past the distance to the lower neighbour.  A double's exponent and
-// mantissa, read as one number, count neighbours: MAN + 11 bits in, one step
-// of the code; below the smallest normal 2^EMIN is added first, which leaves
-// their even spacing in the mantissa.  The 16 bits of r and the half after
-// them end above bit 32, so the upper word decides alone.
+// Code of |y|, y in units of the scale, rounded up where (r + 1/2) / 2^16
+// reaches past the distance to the lower neighbour, with y's sign above it.
+// y is multiplied so that the format's smallest normal comes to lie at the
+// doubles' own: exponent and mantissa, read as one number, then count
+// neighbours below it as above, MAN + 11 bits in, one step of the code.  The
+// 16 bits of r and the half after them end above bit 32, so the upper word
+// decides alone.  |y| is at most the format's largest value and 2^-24 of it,
+// 2^-20 of a step: no r rounds that up.
 template <class F>
 __device__ inline uint32_t encode(double y, uint32_t r) {
-  constexpr uint32_t base = (uint32_t)(1023 + F::EMIN) << 20;  // 2^EMIN
-  const bool small = y < __builtin_ldexp(1.0, F::EMIN);
-  const uint32_t hi = high_word(small ? y + __builtin_ldexp(1.0, F::EMIN) : y) -
-                      (small ? base : base - (1u << 20));
   constexpr int SH = 20 - F::MAN;  // bits of the upper word after the code's
-  return min((hi + ((2 * r + 1) << (SH - 17))) >> SH, (uint32_t)F::TOP);
+  const uint32_t hi = high_word(y * __builtin_ldexp(1.0, -1022 - F::EMIN));
+  return ((hi & 0x7FFFFFFFu) + ((2 * r + 1) << (SH - 17))) >> SH | (hi >> 24 & 128u);
 }
 
 // A block's scale and its reciprocal (NaN, 0 where it has a NaN or an
@@ -295,7 +296,7 @@ __device__ inline void piece32(const Tensor& t, int64_t base, double kd, float k
       const float g = x[q].g[j] * k;
       x[q].m[j] = b1 * x[q].m[j] + omb1 * g;
       x[q].v[j] = b2 * x[q].v[j] + omb2 * g * g;
-      x[q].w[j] = updated(x[q].w[j], x[q].m[j], x[q].v[j], keep, a);
+      x[q].w[j] = updated(x[q].w[j], x[q].m[j], (double)x[q].v[j], keep, a);
     }
     store4<FULL>(t.W, i, t.count, x[q].w);
     store4<FULL>(m, i, t.count, x[q].m);
@@ -319,6 +320,7 @@ __device__ inline void piece8(const Tensor& t, int64_t base, double k, float kee
             t.m_scale[first / BLOCK], t.v_scale[first / BLOCK]};
   }
   const double gm = a.omb1 * k, gv = a.omb2 * k * k;
+  const uint64_t lane_state = (uint64_t)lane * (2 * GOLDEN);  // two draws a lane
 #pragma unroll
   for (int q = 0; q < AT_ONCE; ++q) {
     const int64_t first = base + (q * (THREADS / 64) + wave) * BLOCK, i = first + lane * 4;
@@ -342,7 +344,7 @@ __device__ inline void piece8(const Tensor& t, int64_t base, double k, float kee
       mtop = fmax(mtop, fabs(m4[j]));
       vtop = fmax(vtop, v4[j]);
       gtop = max(gtop, __float_as_uint(x[q].g[j]) & 0x7FFFFFFFu);
-      x[q].w[j] = updated(x[q].w[j], (float)m4[j], (float)v4[j], keep, a);
+      x[q].w[j] = updated(x[q].w[j], (float)m4[j], v4[j], keep, a);
     }
     store4<FULL>(t.W, i, t.count, x[q].w);
     // a NaN or an infinity: the scales say so
@@ -351,14 +353,15 @@ __device__ inline void piece8(const Tensor& t, int64_t base, double k, float kee
     const float msn = block_scale<FormatM>(mtop, bad || !(x[q].ms < INFINITY), &im);
     const float vsn = block_scale<FormatV>(vtop, bad || !(x[q].vs < INFINITY), &iv);
     uint32_t mc = 0, vc = 0;
+    const uint64_t state = a.base + (uint64_t)(t.first * BLOCK + first + 2) / 2 * GOLDEN + lane_state;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint64_t both = splitmix(a.base, (uint64_t)(t.first * BLOCK + i + j) / 2);
+      const uint64_t both = mix64(state + j / 2 * GOLDEN);
       const uint32_t r = (uint32_t)(both >> (32 * (j & 1)));
-      const uint32_t cm = encode<FormatM>(fabs(m4[j]) * im, r & 0xFFFFu) |
-                          (high_word(m4[j]) >> 24 & 128u);
-      uint32_t cv = encode<FormatV>(v4[j] * iv, r >> 16);
-      if (cv == 0 && v4[j] > 0.0) cv = 1;
+      const uint32_t cm = encode<FormatM>(m4[j] * im, r & 0xFFFFu);
+      // a second moment above 0 (its upper word is, too) is not stored as 0
+      const uint32_t cv = max(encode<FormatV>(v4[j] * iv, r >> 16),
+                              min(high_word(v4[j]), 1u));
       mc |= cm << (8 * j);
       vc |= cv << (8 * j);
     }
@@ -414,6 +417,10 @@ gnn_status check_params(const gnn_params* s, int64_t* pieces) {
 
 size_t plan_need(int32_t n, int64_t pieces) {
   return round_up(HEAD_BYTES + (size_t)n * sizeof(Tensor) + (size_t)pieces * sizeof(Piece), 256);
+}
+
+int32_t norm_blocks(int64_t pieces) {
+  return (int32_t)std::min<int64_t>(ceil_div(pieces, 2), NORM_BLOCKS);
 }
 
 inline bool aligned(const void* p, uintptr_t to) {
@@ -519,7 +526,7 @@ gnn_status gnn_params_build_plan(const gnn_params* params, void* plan, size_t pl
 size_t gnn_grad_norm_workspace_bytes(const gnn_params* params) {
   int64_t pieces;
   if (check_params(params, &pieces) != GNN_OK) return 0;
-  return round_up((size_t)std::min<int64_t>(pieces, NORM_BLOCKS) * 8, 256);
+  return round_up((size_t)norm_blocks(pieces) * 8, 256);
 }
 
 gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
@@ -544,7 +551,7 @@ gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
       return GNN_ERR_ALIAS;
   }
   double* part = static_cast<double*>(workspace);
-  const int32_t blocks = (int32_t)std::min<int64_t>(pieces, NORM_BLOCKS);
+  const int32_t blocks = norm_blocks(pieces);
   timer_begin(GNN_K_NORM, stream);
   if (blocks > 0)
     norm_part_kernel<<<blocks, THREADS, 0, stream>>>(params->plan, params->n, part);
