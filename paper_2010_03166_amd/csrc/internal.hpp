@@ -41,6 +41,33 @@ __host__ __device__ inline uint64_t splitmix(uint64_t state, uint64_t k) {
   return mix64(state + (k + 1) * GOLDEN);
 }
 
+// ------------------------------------------------------- lane exchanges
+
+// The value of lane (own number xor D), D a power of two below 64.  Within 16
+// lanes a data-parallel move does it in the vector unit, where lanes that
+// differ in the lower bits hold the same value already (a mirror stands for
+// the xor of 4 and of 8): in a butterfly over D = 1, 2, 4, ... in this order.
+template <int D>
+__device__ inline float butterfly(float v) {
+  const int x = __float_as_int(v);
+  if (D == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, true));
+  if (D == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, true));
+  if (D == 4) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, true));
+  if (D == 8) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x140, 0xF, 0xF, true));
+  return __shfl_xor(v, D, 64);
+}
+// Largest value and sum over groups of G consecutive lanes, in all of them.
+template <int G, int D = 1>
+__device__ inline float lanes_max(float v) {
+  if constexpr (D < G) return lanes_max<G, 2 * D>(fmaxf(v, butterfly<D>(v)));
+  else return v;
+}
+template <int G, int D = 1>
+__device__ inline float lanes_sum(float v) {
+  if constexpr (D < G) return lanes_sum<G, 2 * D>(v + butterfly<D>(v));
+  else return v;
+}
+
 // ------------------------------------------------------------ work plan
 
 // Layout of the aggregation plan buffer (device memory), at the offsets of

@@ -239,9 +239,7 @@ __device__ inline uint32_t encode(double y, uint32_t r) {
 template <class F>
 __device__ inline float block_scale(double top, bool bad, double* inverse) {
   const float mine = (float)top;
-  float most = mine;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+  const float most = lanes_max<64>(mine);
   // doubles >= 0 are ordered as their bits; each turn finds a larger one, so
   // lanes that are all alike take one turn
   const uint64_t own = (uint64_t)__double_as_longlong(top);

@@ -171,16 +171,9 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
 
 // ------------------------------------------------------------- reductions
 
-template <int G>
-__device__ inline float group_max(float v) {
+__device__ inline double wave_sum(double v) {
 #pragma unroll
-  for (int d = G / 2; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-  return v;
-}
-template <int G, typename T>
-__device__ inline T group_sum(T v) {
-#pragma unroll
-  for (int d = G / 2; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
   return v;
 }
 
@@ -188,9 +181,9 @@ __device__ inline T group_sum(T v) {
 template <int T>
 __device__ inline Terms block_terms(Terms t) {
   __shared__ Terms s[T / 64];
-  t.loss = group_sum<64>(t.loss);
-  t.kl = group_sum<64>(t.kl);
-  t.cut = group_sum<64>(t.cut);
+  t.loss = wave_sum(t.loss);
+  t.kl = wave_sum(t.kl);
+  t.cut = wave_sum(t.cut);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = t;
   __syncthreads();
   t = s[0];
@@ -221,7 +214,7 @@ __device__ inline double exact_sum(const float* z, int32_t C, float top) {
   double sum = 0.0;
 #pragma unroll 1
   for (int32_t j = threadIdx.x & 63; j < C; j += 64) sum += exp_exact((double)z[j] - shift);
-  return group_sum<64>(sum);
+  return wave_sum(sum);
 }
 
 // ---------------------------------------------------------- four at a time
@@ -293,7 +286,7 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
-  top = group_max<G>(top);
+  top = lanes_max<G>(top);
   const float shift = shift_of(top);
   float part = 0.f;
 #pragma unroll
@@ -301,7 +294,7 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
     z[k] = exp4(z[k], shift);
     part += sum4(z[k]);
   }
-  part = group_sum<G>(part);
+  part = lanes_sum<G>(part);
   if (lane == 0) {
     s_top[grp] = top;
     s_sum[grp] = part;
@@ -372,7 +365,7 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
-  top = group_max<64>(top);
+  top = lanes_max<64>(top);
   if ((t & 63) == 0) s_top[wave] = top;
   __syncthreads();
   top = s_top[0];
@@ -385,7 +378,7 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
     z[k] = exp4(z[k], shift);
     part += sum4(z[k]);
   }
-  part = group_sum<64>(part);
+  part = lanes_sum<64>(part);
   if ((t & 63) == 0) s_sum[wave] = part;
   __syncthreads();
   if (wave == 0) {
@@ -444,7 +437,7 @@ __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < SPLIT_V; ++k) top = fmaxf(top, max4(z[k]));
-  top = group_max<64>(top);
+  top = lanes_max<64>(top);
   if ((t & 63) == 0) s_top[wave] = top;
   __syncthreads();
   top = s_top[0];
@@ -454,7 +447,7 @@ __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
   float part = 0.f;
 #pragma unroll
   for (int k = 0; k < SPLIT_V; ++k) part += sum4(exp4(z[k], shift));
-  part = group_sum<64>(part);
+  part = lanes_sum<64>(part);
   if ((t & 63) == 0) s_sum[wave] = part;
   __syncthreads();
   if (t == 0) {
@@ -477,14 +470,14 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   const Chunk* at = a.chunks + (int64_t)i * a.per_row;
   float top = -INFINITY;
   for (int32_t k = lane; k < a.per_row; k += 64) top = fmaxf(top, at[k].top);
-  top = group_max<64>(top);
+  top = lanes_max<64>(top);
   const float shift = shift_of(top);
   double sum = 0.0;
   for (int32_t k = lane; k < a.per_row; k += 64) {
     const Chunk c = at[k];
     sum += c.sum * exp_quick((double)shift_of(c.top) - shift);
   }
-  sum = group_sum<64>(sum);
+  sum = wave_sum(sum);
   const double lp = log_prob<false>(r, top, sum);
   if (t == 0 && chunk == 0 && a.logp) a.logp[i] = (float)lp;
   if (!LOSS) return;
