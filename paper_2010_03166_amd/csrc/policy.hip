@@ -53,11 +53,13 @@ struct RowIn {
   float za, adv, old_lp, ref_lp, w;
   bool chosen;
 };
-__device__ inline RowIn row_in(const PolicyArgs& a, int32_t i, bool loss) {
+// The action is read before the row's logits and the rest after them, so that
+// the chosen logit's own read, which needs the action, waits for no other.
+__device__ inline RowIn row_in(const PolicyArgs& a, int32_t i, int32_t act, bool loss) {
   RowIn r = {};
-  r.act = a.action[i];
-  r.chosen = r.act >= 0 && r.act < a.C;
-  r.za = r.chosen ? a.Z[(int64_t)i * a.ld_z + r.act] : 0.f;
+  r.act = act;
+  r.chosen = act >= 0 && act < a.C;
+  r.za = r.chosen ? a.Z[(int64_t)i * a.ld_z + act] : 0.f;
   if (loss) {
     r.adv = a.adv[i];
     r.old_lp = a.old_lp ? a.old_lp[i] : 0.f;
@@ -98,22 +100,21 @@ __device__ inline double exp_exact(double x) {
   return ldexp(sum, (int)fmin(k, 2000.0));
 }
 
-// log(s) as k ln 2 + log(m), 0.7 < m < 1.42: good to 4e-8.
-__device__ inline double log_quick(double s) {
+// log(s) as k ln 2 + log(m), 0.7 < m < 1.42 (so that log(1) is 0): good to
+// 4e-8.
+__device__ inline double log_quick(float s) {
   int k;
-  double m = frexp(s, &k);
-  if (m < 0.70710678) {
-    m *= 2.0;
+  float m = frexpf(s, &k);
+  if (m < 0.70710678f) {
+    m *= 2.f;
     --k;
   }
-  const float f = (float)m;
-  const float more = (float)(m - f);  // a NaN or an infinity shows in logf(f)
-  return k * 0.6931471805599453 + (double)(logf(f) + (more == more ? more : 0.f) / f);
+  return fma((double)k, 0.6931471805599453, (double)logf(m));
 }
 
-// One step of third order from there (e^y is s but for 1e-7).
+// One step of third order from there (e^y is s but for 2e-7).
 __device__ inline double log_exact(double s) {
-  const double y = log_quick(s), e = exp_exact(y);
+  const double y = log_quick((float)s), e = exp_exact(y);
   return y + 2.0 * (s - e) / (s + e);
 }
 
@@ -124,19 +125,32 @@ __device__ inline double beyond(double x, float f) {
 }
 __device__ inline double exp_quick(double x) {
   const float f = (float)x;
-  return (double)expf(f) * (1.0 + beyond(x, f));
+  const double e = (double)expf(f);
+  return fma(e, beyond(x, f), e);
 }
+// e^x - 1: its series where the 1 would take digits (the first term left out,
+// x^9 / 9!, is below 1e-8 of the sum).
 __device__ inline double expm1_quick(double x) {
   const float f = (float)x;
-  const double e = (double)expm1f(f);
-  return e + (1.0 + e) * beyond(x, f);
+  float e = expf(f) - 1.f;
+  if (fabsf(f) < 0.5f) {
+    e = 1.f / 40320.f;
+    e = fmaf(e, f, 1.f / 5040.f);
+    e = fmaf(e, f, 1.f / 720.f);
+    e = fmaf(e, f, 1.f / 120.f);
+    e = fmaf(e, f, 1.f / 24.f);
+    e = fmaf(e, f, 1.f / 6.f);
+    e = fmaf(e, f, 0.5f);
+    e = fmaf(e * f, f, f);
+  }
+  return fma(1.0 + (double)e, beyond(x, f), (double)e);
 }
 
 template <bool EXACT>
 __device__ inline double log_prob(const RowIn& r, float top, double sum) {
   if (!r.chosen) return 0.0;
   if (sum == 0.0) return -INFINITY;
-  return (double)r.za - top - (EXACT ? log_exact(sum) : log_quick(sum));
+  return (double)r.za - top - (EXACT ? log_exact(sum) : log_quick((float)sum));
 }
 
 // The row's terms, and its slope c = w dl/dlp.  Returns whether the ratio is
@@ -278,11 +292,12 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
   const int32_t rows = min(R, a.n - first);
   const bool mine = t < rows;
   const float* row = a.Z + ((int64_t)first + grp) * a.ld_z;
+  const int32_t act = mine ? a.action[first + t] : -1;
   f4 z[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) z[k] = load_cols(row, (k * G + lane) * 4, grp < rows ? a.C : 0);
   RowIn r = {};
-  if (mine) r = row_in(a, first + t, LOSS);
+  if (mine) r = row_in(a, first + t, act, LOSS);
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
@@ -358,10 +373,11 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   const int t = threadIdx.x, wave = t >> 6;
   const int32_t i = (int32_t)(a.block0 + blockIdx.x);
   const float* row = a.Z + (int64_t)i * a.ld_z;
+  const int32_t act = a.action[i];
   f4 z[V];
 #pragma unroll
   for (int k = 0; k < V; ++k) z[k] = load_cols(row, (k * T + t) * 4, a.C);
-  const RowIn r = row_in(a, i, LOSS);
+  const RowIn r = row_in(a, i, act, LOSS);
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
@@ -465,7 +481,7 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   const int64_t b = a.block0 + blockIdx.x;
   const int32_t i = (int32_t)(b / todo), chunk = (int32_t)(b % todo);
   const float* row = a.Z + (int64_t)i * a.ld_z;
-  const RowIn r = row_in(a, i, LOSS);
+  const RowIn r = row_in(a, i, a.action[i], LOSS);
   // every wavefront joins the row's sums alike
   const Chunk* at = a.chunks + (int64_t)i * a.per_row;
   float top = -INFINITY;
