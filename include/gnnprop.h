@@ -412,7 +412,8 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
  * advantage A, old_logp, ref_logp and weight w are n floats; weight NULL:
  * 1/n.  A row of weight 0 adds nothing and has a gradient of 0, whatever its
  * logits.  A chosen action with a logit of -inf has lp = -inf: its kl is
- * infinite, and its gradient not finite where beta > 0.  0 <= clip_lo <= 1,
+ * infinite, and its gradient not finite where beta > 0.  1 <= C <= 2^24,
+ * 0 <= clip_lo <= 1,
  * clip_hi >= 0 (infinity: no upper clip), beta finite >= 0, needing ref_logp
  * where beta > 0 (else GNN_ERR_SHAPE / GNN_ERR_NULL).
  * out: three floats.  logp (n floats) and dZ (n x C, stride ld_dz) may be
@@ -468,7 +469,7 @@ typedef struct gnn_params {
 } gnn_params;
 
 /* Bytes of the plan, and its filling (a device buffer of at least that size,
- * 16-byte aligned): a table of the tensors and of the pieces of 2,048
+ * 16-byte aligned): a table of the tensors and of the pieces of 1,024
  * elements that one workgroup takes, so that one launch covers every tensor.
  * Nothing is read from the host after the call returns.  No W, m, v or scale
  * may overlap anything else in the set or the plan (GNN_ERR_ALIAS).
@@ -491,7 +492,8 @@ gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
  * k = max_norm / norm where norm > max_norm (max_norm > 0) and 1 elsewhere,
  * and a norm that is not finite skips the step: nothing is changed.
  * Without norm a NaN or infinite gradient makes its own weight and moments
- * non-finite, with 8-bit moments those of its whole block of 256.
+ * non-finite, with 8-bit moments those of its whole block of 256 (so does one
+ * whose square passes 1e43).
  * Hyperparameters are host values, taken at the call (a captured launch
  * replays with them): 0 <= beta1, beta2 < 1, eps >= 0, lr finite.
  *

@@ -19,6 +19,8 @@ constexpr int THREADS = 256;
 constexpr int BLOCK = GNN_STATE_BLOCK;  // one wavefront, four elements a lane
 constexpr int PIECE = 1024;
 constexpr int NORM_BLOCKS = 2048;  // partial sums of the norm
+// Pieces of one launch (2^32 threads are the most that a launch can have).
+constexpr int64_t LAUNCH_PIECES = 1 << 23;
 
 struct PlanHead {
   int64_t pieces;
@@ -373,13 +375,17 @@ __device__ inline void piece8(const Tensor& t, int64_t base, double k, float kee
 }
 
 template <int BITS>
-__global__ __launch_bounds__(THREADS) void adamw_kernel(const void* plan, int32_t n, Coef a) {
+__global__ __launch_bounds__(THREADS) void adamw_kernel(const void* plan, int32_t n,
+                                                        int64_t piece0, Coef a) {
   const Plan p = plan_at(plan, n);
-  if (blockIdx.x >= p.head->pieces || p.head->state_bits != BITS) return;
+  const int64_t piece = piece0 + blockIdx.x;
+  if (piece >= p.head->pieces || p.head->state_bits != BITS) return;
   double k;
   if (!clip_factor(a, &k)) return;
-  const Piece at = p.pieces[blockIdx.x];
+  const Piece at = p.pieces[piece];
   const Tensor& t = p.tensors[at.tensor];
+  // (a plan for the norm alone has no weights)
+  if (!t.W || !t.m || !t.v || (BITS == 8 && (!t.m_scale || !t.v_scale))) return;
   const float keep = (float)(1.0 - a.lr * t.decay);
   const int64_t base = (int64_t)at.index * PIECE;
   const bool full = base + PIECE <= t.count;
@@ -579,8 +585,10 @@ gnn_status gnn_adamw_step(const gnn_params* params, double lr, double beta1, dou
       return GNN_ERR_NULL;
     weights += q.count;
     const size_t w = (size_t)q.count * 4, s = params->state_bits == 8 ? (size_t)q.count : w;
+    const size_t sc = params->state_bits == 8 ? (size_t)ceil_div(q.count, BLOCK) * 4 : 0;
     if (ranges_overlap(norm, 4, q.W, w) || ranges_overlap(norm, 4, q.m, s) ||
-        ranges_overlap(norm, 4, q.v, s))
+        ranges_overlap(norm, 4, q.v, s) || ranges_overlap(norm, 4, q.m_scale, sc) ||
+        ranges_overlap(norm, 4, q.v_scale, sc))
       return GNN_ERR_ALIAS;
   }
   if (pieces == 0) return GNN_OK;
@@ -589,10 +597,13 @@ gnn_status gnn_adamw_step(const gnn_params* params, double lr, double beta1, dou
                   (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, t))), norm, max_norm,
                   splitmix(seed, (uint64_t)t)};
   timer_begin(GNN_K_UPDATE, stream);
-  if (params->state_bits == 32)
-    adamw_kernel<32><<<(unsigned)pieces, THREADS, 0, stream>>>(params->plan, params->n, a);
-  else
-    adamw_kernel<8><<<(unsigned)pieces, THREADS, 0, stream>>>(params->plan, params->n, a);
+  for (int64_t p0 = 0; p0 < pieces; p0 += LAUNCH_PIECES) {
+    const unsigned blocks = (unsigned)std::min(pieces - p0, LAUNCH_PIECES);
+    if (params->state_bits == 32)
+      adamw_kernel<32><<<blocks, THREADS, 0, stream>>>(params->plan, params->n, p0, a);
+    else
+      adamw_kernel<8><<<blocks, THREADS, 0, stream>>>(params->plan, params->n, p0, a);
+  }
   timer_end(GNN_K_UPDATE, (params->state_bits == 32 ? 28.0 : 16.0) * weights, stream);
   GNN_HIP(hipGetLastError());
   return GNN_OK;

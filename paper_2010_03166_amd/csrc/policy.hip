@@ -13,6 +13,7 @@ using namespace gnnprop;
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int32_t MOST_COLS = 1 << 24;  // (a long row's chunks are joined by each of its blocks)
 
 struct Terms {  // a row's share of `out`
   double loss, kl, cut;
@@ -81,6 +82,7 @@ constexpr double NEAR = 4e-6;
 // (|r| < 0.35: the first term left out, r^14 / 14!, is below 5e-18).
 __device__ inline double exp_exact(double x) {
   if (!(x > -700.0)) return x < 0.0 ? 0.0 : x;  // 0, or NaN
+  if (x > 709.8) return INFINITY;
   const double k = rint(x * 1.4426950408889634);
   const double r = fma(-k, 2.3190468138462996e-17, fma(-k, 0.6931471805599453, x));
   double sum = 1.0 / 6227020800.0;
@@ -97,7 +99,7 @@ __device__ inline double exp_exact(double x) {
   sum = fma(sum, r, 0.5);
   sum = fma(sum, r, 1.0);
   sum = fma(sum, r, 1.0);
-  return ldexp(sum, (int)fmin(k, 2000.0));
+  return ldexp(sum, (int)k);
 }
 
 // log(s) as k ln 2 + log(m), 0.7 < m < 1.42 (so that log(1) is 0): good to
@@ -118,32 +120,40 @@ __device__ inline double log_exact(double s) {
   return y + 2.0 * (s - e) / (s + e);
 }
 
-// The part of x beyond its rounding to fp32 (0 for infinities).
-__device__ inline double beyond(double x, float f) {
-  const double d = x - (double)f;
-  return fabs(d) < INFINITY ? d : 0.0;
+// e = exp(f) made exp(x), f being x rounded to fp32 (0 and infinity stay).
+__device__ inline double refined(double e, double x, float f) {
+  return e > 0.0 && e < INFINITY ? fma(e, x - (double)f, e) : e;
+}
+// exp(f) where fp32 would overflow too (as the eighth power of exp(f / 8)).
+__device__ inline double exp_wide(float f) {
+  if (!(f > 80.f)) return (double)expf(f);
+  double e = (double)expf(0.125f * f);
+  e *= e;
+  e *= e;
+  return e * e;
 }
 __device__ inline double exp_quick(double x) {
   const float f = (float)x;
-  const double e = (double)expf(f);
-  return fma(e, beyond(x, f), e);
+  return refined(exp_wide(f), x, f);
 }
-// e^x - 1: its series where the 1 would take digits (the first term left out,
-// x^9 / 9!, is below 1e-8 of the sum).
-__device__ inline double expm1_quick(double x) {
+// e^x - 1, and e^x - 1 - x, from the series x^2 (1/2 + x/6 + ...) where the
+// difference would lose digits (its first term left out is below 1e-7 of it).
+__device__ inline double expm1_quick(double x, double* less_x) {
   const float f = (float)x;
-  float e = expf(f) - 1.f;
   if (fabsf(f) < 0.5f) {
-    e = 1.f / 40320.f;
-    e = fmaf(e, f, 1.f / 5040.f);
-    e = fmaf(e, f, 1.f / 720.f);
-    e = fmaf(e, f, 1.f / 120.f);
-    e = fmaf(e, f, 1.f / 24.f);
-    e = fmaf(e, f, 1.f / 6.f);
-    e = fmaf(e, f, 0.5f);
-    e = fmaf(e * f, f, f);
+    float p = 1.f / 40320.f;
+    p = fmaf(p, f, 1.f / 5040.f);
+    p = fmaf(p, f, 1.f / 720.f);
+    p = fmaf(p, f, 1.f / 120.f);
+    p = fmaf(p, f, 1.f / 24.f);
+    p = fmaf(p, f, 1.f / 6.f);
+    p = fmaf(p, f, 0.5f);
+    *less_x = (double)p * x * x;
+    return x + *less_x;
   }
-  return fma(1.0 + (double)e, beyond(x, f), (double)e);
+  const double e = refined(exp_wide(f), x, f) - 1.0;
+  *less_x = x == INFINITY ? x : e - x;
+  return e;
 }
 
 template <bool EXACT>
@@ -164,13 +174,14 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
   if (!r.chosen || sum == 0.0 || w == 0.0) return false;
   const double A = r.adv, x = lp - (double)r.old_lp;
   const double rho = !a.old_lp ? 1.0 : EXACT ? exp_exact(x) : exp_quick(x);
-  const bool near = a.old_lp && (fabs(rho - a.lo) <= NEAR * rho || fabs(rho - a.hi) <= NEAR * rho);
+  const bool near = a.old_lp && rho < INFINITY &&
+                    (fabs(rho - a.lo) <= NEAR * rho || fabs(rho - a.hi) <= NEAR * rho);
   const double ra = rho * A, ca = fmin(fmax(rho, a.lo), a.hi) * A;
   const bool cut = ra > ca;  // false for a NaN, which then shows in ra
   double slope = cut ? 0.0 : -ra, loss = -(cut ? ca : ra);
   if (a.ref_lp) {
-    const double d = (double)r.ref_lp - lp, e = expm1_quick(d);
-    const double kl = d == INFINITY ? d : e - d;
+    double kl;
+    const double e = expm1_quick((double)r.ref_lp - lp, &kl);
     t->kl = w * kl;
     if (a.beta != 0.0) {
       loss += a.beta * kl;
@@ -222,13 +233,28 @@ __device__ inline void store_terms(const PolicyArgs& a, const Terms& t) {
   else a.part[a.block0 + blockIdx.x] = t;
 }
 
-// Sum of exp(z - top) of one row by a wavefront, in doubles.
-__device__ inline double exact_sum(const float* z, int32_t C, float top) {
+// Sum of exp(z - top) of one row in doubles, by a wavefront or by a block of T
+// threads (in all of them).
+__device__ inline double exact_part(const float* z, int32_t C, float top, int32_t at, int32_t step) {
   const double shift = shift_of(top);
   double sum = 0.0;
 #pragma unroll 1
-  for (int32_t j = threadIdx.x & 63; j < C; j += 64) sum += exp_exact((double)z[j] - shift);
+  for (int32_t j = at; j < C; j += step) sum += exp_exact((double)z[j] - shift);
   return wave_sum(sum);
+}
+__device__ inline double exact_sum(const float* z, int32_t C, float top) {
+  return exact_part(z, C, top, threadIdx.x & 63, 64);
+}
+template <int T>
+__device__ inline double exact_sum_block(const float* z, int32_t C, float top) {
+  __shared__ double s[T / 64];
+  const double part = exact_part(z, C, top, threadIdx.x, T);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = part;
+  __syncthreads();
+  double sum = s[0];
+#pragma unroll 1
+  for (int k = 1; k < T / 64; ++k) sum += s[k];
+  return sum;
 }
 
 // ---------------------------------------------------------- four at a time
@@ -370,6 +396,7 @@ template <int T, int V, bool LOSS>
 __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   __shared__ float s_top[T / 64], s_c, s_inv;
   __shared__ double s_sum[T / 64];
+  __shared__ int32_t s_near;
   const int t = threadIdx.x, wave = t >> 6;
   const int32_t i = (int32_t)(a.block0 + blockIdx.x);
   const float* row = a.Z + (int64_t)i * a.ld_z;
@@ -397,28 +424,38 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   part = lanes_sum<64>(part);
   if ((t & 63) == 0) s_sum[wave] = part;
   __syncthreads();
+  double sum = 0.0;
+  Terms terms;
   if (wave == 0) {
-    double sum = 0.0;
 #pragma unroll
     for (int k = 0; k < T / 64; ++k) sum += s_sum[k];
     const double lp = log_prob<false>(r, top, sum);
     if (t == 0 && a.logp) a.logp[i] = (float)lp;
     if (LOSS) {
-      Terms terms;
       float c;
-      if (row_terms<false>(a, r, sum, lp, &terms, &c)) {  // the same in all lanes
-        sum = exact_sum(row, a.C, top);
-        row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &c);
-      }
-      store_terms(a, terms);
+      const bool near = row_terms<false>(a, r, sum, lp, &terms, &c);  // the same in all lanes
       if (t == 0) {
         s_c = c;
         s_inv = 1.f / (float)sum;
+        s_near = near;
       }
     }
   }
-  if (!LOSS || !a.dZ) return;
+  if (!LOSS) return;
   __syncthreads();
+  if (s_near) {
+    sum = exact_sum_block<T>(row, a.C, top);
+    if (t == 0) {
+      row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &s_c);
+      s_inv = 1.f / (float)sum;
+    }
+    __syncthreads();
+    // read once more, so that this branch has the registers
+#pragma unroll
+    for (int k = 0; k < V; ++k) z[k] = exp4(load_cols(row, (k * T + t) * 4, a.C), shift);
+  }
+  store_terms(a, terms);
+  if (!a.dZ) return;
   float* to = a.dZ + (int64_t)i * a.ld_dz;
   const float c = s_c, inv = s_inv;
 #pragma unroll
@@ -500,7 +537,7 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   Terms terms;
   float c;
   if (row_terms<false>(a, r, sum, lp, &terms, &c)) {  // alike in all threads of a row
-    sum = exact_sum(row, a.C, top);
+    sum = exact_sum_block<THREADS>(row, a.C, top);
     row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &c);
   }
   if (t == 0 && chunk == 0) a.part[i] = terms;
@@ -655,14 +692,14 @@ gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
 extern "C" {
 
 size_t gnn_policy_workspace_bytes(int32_t n, int32_t C) {
-  if (n < 0 || C <= 0) return 0;
+  if (n < 0 || C <= 0 || C > MOST_COLS) return 0;
   return layout_of(n, C, true).total;
 }
 
 gnn_status gnn_action_logp(int32_t n, int32_t C, const float* Z, int64_t ld_z,
                            const int32_t* action, float* logp, void* workspace,
                            size_t workspace_bytes, hipStream_t stream) {
-  if (n < 0 || C <= 0 || ld_z < C) return GNN_ERR_SHAPE;
+  if (n < 0 || C <= 0 || C > MOST_COLS || ld_z < C) return GNN_ERR_SHAPE;
   if (n == 0) return GNN_OK;
   if (!Z || !action || !logp) return GNN_ERR_NULL;
   if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
@@ -693,7 +730,7 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
                            double beta, float* out, float* logp, float* dZ,
                            int64_t ld_dz, void* workspace, size_t workspace_bytes,
                            hipStream_t stream) {
-  if (n < 0 || C <= 0 || ld_z < C || (dZ && ld_dz < C)) return GNN_ERR_SHAPE;
+  if (n < 0 || C <= 0 || C > MOST_COLS || ld_z < C || (dZ && ld_dz < C)) return GNN_ERR_SHAPE;
   // written so that a NaN is refused
   if (!(clip_lo >= 0.0 && clip_lo <= 1.0) || !(clip_hi >= 0.0) ||
       !(beta >= 0.0 && beta < INFINITY))

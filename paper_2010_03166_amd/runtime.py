@@ -371,6 +371,10 @@ class SageStack:
         return self.layers[0]["dX"] if want_dx_first else None
 
 
+def _on_current(t: torch.Tensor) -> bool:
+    return t.is_cuda and t.get_device() == torch.cuda.current_device()
+
+
 class ParamSet:
     """AdamW on a set of tensors, one launch a step: their moments (in 32
     bits, or in 8 with a scale for each 256 elements), the plan that lists
@@ -384,9 +388,9 @@ class ParamSet:
         if not len(weights) == len(grads) == len(weight_decay):
             raise ValueError("as many gradients and decays as weights")
         for t in list(weights) + list(grads):
-            if t.dtype != torch.float32 or not t.is_contiguous() or not t.is_cuda:
+            if t.dtype != torch.float32 or not t.is_contiguous() or not _on_current(t):
                 raise ValueError("weights and gradients must be contiguous float32 tensors on "
-                                 "the device")
+                                 "the current device")
         for w, g in zip(weights, grads):
             if w.shape != g.shape or w.device != g.device:
                 raise ValueError("a weight and its gradient differ in shape or device")
@@ -569,8 +573,8 @@ class Trainer:
 
     def _per_row(self, name: str, t: Optional[torch.Tensor], dtype=torch.float32):
         if t is not None and (t.dtype != dtype or t.shape != (self.n,) or
-                              not t.is_contiguous() or not t.is_cuda):
-            raise ValueError("%s must be %d contiguous values of %s on the device" %
+                              not t.is_contiguous() or not _on_current(t)):
+            raise ValueError("%s must be %d contiguous values of %s on the current device" %
                              (name, self.n, dtype))
         return t
 

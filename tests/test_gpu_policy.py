@@ -243,6 +243,50 @@ def test_policy_not_finite_rows_stay_alone(n, C):
     assert r["out"][0] == np.inf and r["out"][1] == np.inf
 
 
+@pytest.mark.parametrize("n,C", SHAPES)
+def test_policy_ratios_without_bound(n, C):
+    """Old log-probabilities of -inf and far below: a ratio that is infinite,
+    or beyond fp32, is clipped for a positive advantage, counts for nothing
+    with an advantage of 0 and shows for a negative one."""
+    z, a, adv, old, ref, w = _case(n, C, 9)
+    lp, _ = P.action_logp(z, a)
+    w[:] = 1.0 / n
+    old[:2] = [-np.inf, lp[1] - 120.0][: 2]
+    adv[:2] = 1.0
+    want = P.policy_loss(z, a, adv, old, ref, w, 0.2, 0.3, 0.05)
+    assert want["cut"][:2].all() and np.isfinite(want["out"]).all()
+    r = run_loss(z, a, adv, old, ref, w, beta=0.05)
+    with np.errstate(all="ignore"):
+        want["rho"][:2] = 1.3  # clipped there: that is what the loss depends on
+    check_loss(r, want, z, a, adv, np.where(np.isinf(old), 0, old), ref, 0.05)
+    adv[1] = 0.0  # e^120 times nothing
+    r = run_loss(z, a, adv, old, ref, w, beta=0.0)
+    assert np.isfinite(r["out"]).all() and np.all(r["dZ"][1] == 0)
+    adv[0] = -1.0
+    r = run_loss(z, a, adv, old, ref, w, beta=0.0)
+    assert r["out"][0] == np.inf and not np.isfinite(r["dZ"][0]).all()
+    assert np.isfinite(r["dZ"][1:]).all()
+
+
+@pytest.mark.parametrize("n,C", SHAPES + [(5000, 41)])
+def test_policy_clip_of_nothing(n, C):
+    """clip = (0, 0) at the old policy: every ratio is next to both borders."""
+    z, a, adv, old, ref, w = _case(n, C, 10)
+    lp, _ = P.action_logp(z, a)
+    old = lp.astype(np.float32)
+    r = run_loss(z, a, adv, old, ref, w, lo=0.0, hi=0.0, beta=0.05)
+    want = P.policy_loss(z, a, adv, old, ref, w, 0.0, 0.0, 0.05)
+    near = np.abs(want["rho"] - 1) < 1e-10
+    assert near.mean() < 0.2 or n < 10
+    if not near.any():
+        check_loss(r, want, z, a, adv, old, ref, 0.05)
+    # by rows: those that are decided, on their side
+    keep = np.where(near, -1, a)
+    want = P.policy_loss(z, keep, adv, old, ref, w, 0.0, 0.0, 0.05)
+    r = run_loss(z, keep, adv, old, ref, w, lo=0.0, hi=0.0, beta=0.05)
+    check_loss(r, want, z, keep, adv, old, ref, 0.05)
+
+
 @pytest.mark.parametrize("n,C", [(4096, 41), (600, 1000), (40, 20000), (2, 131072)])
 def test_policy_next_to_the_border(n, C):
     """Ratios that round to the clip's border, just inside and just outside:

@@ -136,10 +136,14 @@ def _loss(n=4, C=3, Z=0x1000, ld=3, action=0x2000, adv=0x2100, old=0x2200, ref=0
 def test_policy_refusals():
     for f in (_logp, _loss):
         assert f(n=-1) == -2 and f(C=0) == -2 and f(ld=2) == -2
+        assert f(C=2 ** 24 + 1, ld=2 ** 24 + 1) == -2
         assert f(Z=None) == -1 and f(action=None) == -1
         assert f(ws=0x4004) == -4
-        assert f(n=4000, ld=3, bytes_=8) == -5 or G.gnn_policy_workspace_bytes(4000, 3) <= 8
         assert f(logp=0x1004) == -7 and f(logp=0x2000) == -7
+    assert _loss(bytes_=8) == -5 and _loss(ws=None) == -5
+    # log-probabilities need a workspace for rows that are cut into chunks
+    long = dict(n=1, C=40000, ld=40000, Z=0x100000, action=0x2000)
+    assert _logp(bytes_=8, **long) == -5 and _logp(ws=None, **long) == -5
     assert _logp(logp=None) == -1
     assert _logp(n=0, Z=None) == 0
     assert _loss(adv=None) == -1 and _loss(out=None) == -1
@@ -153,8 +157,8 @@ def test_policy_refusals():
                dict(logp=0x3008), dict(dZ=0x3100), dict(ws=0x2200)):
         assert _loss(**kw) == -7, kw
     assert G.gnn_policy_workspace_bytes(-1, 3) == 0 == G.gnn_policy_workspace_bytes(3, 0)
-    top = 2 ** 31 - 1
-    assert G.gnn_policy_workspace_bytes(top, top) >= 0
+    assert G.gnn_policy_workspace_bytes(3, 2 ** 24 + 1) == 0
+    assert G.gnn_policy_workspace_bytes(2 ** 31 - 1, 2 ** 24) > 2 ** 31 * 4096
 
 
 def _set(bits=32, n=1, count=1000, **kw):
@@ -233,6 +237,8 @@ def test_norm_and_step_refusals(bits):
     if bits == 8:
         assert step(_set(bits, m_scale=None)) == -1 and step(_set(bits, v_scale=None)) == -1
     assert step(s, nrm=0x10000000) == -7 and step(s, nrm=0x10200000) == -7
+    if bits == 8:
+        assert step(s, nrm=0x10500000) == -7  # a scale
     s.plan = None
     assert norm(s) == -1 and step(s) == -1
     s.plan = 0x8000004
