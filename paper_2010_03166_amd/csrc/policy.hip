@@ -29,7 +29,8 @@ struct PolicyArgs {
   const float* Z;
   int64_t ld_z;
   const int32_t* action;
-  const float *adv, *old_lp, *ref_lp, *weight;
+  const float *adv, *old_lp, *ref_lp, *weight;  // adv in the place of those left out
+  bool has_old, has_ref, has_weight;
   double lo, hi, beta;  // clip to [lo, hi]
   double mean;          // 1 / n
   float* out;
@@ -56,16 +57,18 @@ struct RowIn {
 };
 // The action is read before the row's logits and the rest after them, so that
 // the chosen logit's own read, which needs the action, waits for no other.
+// (No branches here either: arrays that the caller left out are some other
+// array of the row's, and not used.)
 __device__ inline RowIn row_in(const PolicyArgs& a, int32_t i, int32_t act, bool loss) {
   RowIn r = {};
   r.act = act;
   r.chosen = act >= 0 && act < a.C;
-  r.za = r.chosen ? a.Z[(int64_t)i * a.ld_z + act] : 0.f;
+  r.za = a.Z[(int64_t)i * a.ld_z + (r.chosen ? act : 0)];
   if (loss) {
     r.adv = a.adv[i];
-    r.old_lp = a.old_lp ? a.old_lp[i] : 0.f;
-    r.ref_lp = a.ref_lp ? a.ref_lp[i] : 0.f;
-    r.w = a.weight ? a.weight[i] : 0.f;
+    r.old_lp = a.old_lp[i];
+    r.ref_lp = a.ref_lp[i];
+    r.w = a.weight[i];
   }
   return r;
 }
@@ -170,16 +173,16 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
                                  Terms* t, float* c) {
   *c = 0.f;
   *t = {0.0, 0.0, 0.0};
-  const double w = a.weight ? (double)r.w : a.mean;
+  const double w = a.has_weight ? (double)r.w : a.mean;
   if (!r.chosen || sum == 0.0 || w == 0.0) return false;
   const double A = r.adv, x = lp - (double)r.old_lp;
-  const double rho = !a.old_lp ? 1.0 : EXACT ? exp_exact(x) : exp_quick(x);
-  const bool near = a.old_lp && rho < INFINITY &&
+  const double rho = !a.has_old ? 1.0 : EXACT ? exp_exact(x) : exp_quick(x);
+  const bool near = a.has_old && rho < INFINITY &&
                     (fabs(rho - a.lo) <= NEAR * rho || fabs(rho - a.hi) <= NEAR * rho);
   const double ra = rho * A, ca = fmin(fmax(rho, a.lo), a.hi) * A;
   const bool cut = ra > ca;  // false for a NaN, which then shows in ra
   double slope = cut ? 0.0 : -ra, loss = -(cut ? ca : ra);
-  if (a.ref_lp) {
+  if (a.has_ref) {
     double kl;
     const double e = expm1_quick((double)r.ref_lp - lp, &kl);
     t->kl = w * kl;
@@ -264,14 +267,34 @@ __device__ inline double exact_sum_block(const float* z, int32_t C, float top) {
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef f4 f4u __attribute__((aligned(4)));
 
-// Columns [col, col + 4) of a row of C, -inf past its end.
+// Reading columns [col, col + 4) of a row of C, in two steps.  First a load
+// without a branch (what is loaded in one is waited for where the branch ends,
+// and a row's loads would follow each other), of the row's last four columns
+// where its end cuts the chunk or lies before it; later, when the values are
+// there, those past the end made -inf.
 __device__ inline f4 load_cols(const float* row, int32_t col, int32_t C) {
-  if (col + 4 <= C) return *reinterpret_cast<const f4u*>(row + col);
-  f4 r = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-  if (col < C) r.x = row[col];
-  if (col + 1 < C) r.y = row[col + 1];
-  if (col + 2 < C) r.z = row[col + 2];
-  return r;
+  if (C >= 4) return *reinterpret_cast<const f4u*>(row + min(col, C - 4));
+  return {row[0], row[min(1, C - 1)], row[min(2, C - 1)], 0.f};
+}
+__device__ inline float pick(bool c, float x, float y) { return c ? x : y; }
+__device__ inline f4 cut_cols(f4 w, int32_t col, int32_t C) {
+  const float none = -INFINITY;
+  const int32_t left = C - col;  // columns from col on
+  if (C >= 4) {                  // w starts 4 - left columns before col
+    const bool one = left == 3 || left == 1, two = left == 2 || left == 1;
+    w = {pick(one, w.y, w.x), pick(one, w.z, w.y), pick(one, w.w, w.z), w.w};
+    w = {pick(two, w.z, w.x), pick(two, w.w, w.y), w.z, w.w};
+  }
+  return {pick(left > 0, w.x, none), pick(left > 1, w.y, none), pick(left > 2, w.z, none),
+          pick(left > 3, w.w, none)};
+}
+// Chunk k of V of a lane: those before the last are whole (V is the chunks of
+// the row over the lanes, rounded up, so the row has at least 4 V - 3 columns).
+template <int V>
+__device__ inline f4 load_chunk(const float* row, int k, int32_t col, int32_t C) {
+  if (k < V - 1) return *reinterpret_cast<const f4u*>(row + col);
+  if (V > 1) return *reinterpret_cast<const f4u*>(row + min(col, C - 4));
+  return load_cols(row, col, C);
 }
 __device__ inline void store_cols(float* row, int32_t col, int32_t C, f4 v) {
   if (col + 4 <= C) {
@@ -304,26 +327,22 @@ __device__ inline f4 grad4(f4 e, int32_t col, int32_t act, float c, float inv) {
 // ------------------------------------------------ several rows a wavefront
 
 // G lanes to a row of at most 4 G V columns, R = 256 / G rows a block, read
-// once into registers.  Between the sums and the gradient one thread computes
-// each row's scalars, so that they cost a wavefront's time once for up to 64
-// rows instead of once for each 64 / G.
+// once into registers.  Every lane computes its row's scalars: the same
+// instructions as for one lane, and no wavefront waits for another.
 template <int G, int V, bool LOSS>
 __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
   constexpr int R = THREADS / G;
-  __shared__ float s_top[R], s_sum[R], s_c[R], s_inv[R];
-  __shared__ int32_t s_act[R], s_near;
-  __shared__ double s_exact[R];
   const int t = threadIdx.x, lane = t % G, grp = t / G;
   const int32_t first = (int32_t)(a.block0 + blockIdx.x) * R;
-  const int32_t rows = min(R, a.n - first);
-  const bool mine = t < rows;
-  const float* row = a.Z + ((int64_t)first + grp) * a.ld_z;
-  const int32_t act = mine ? a.action[first + t] : -1;
+  const bool mine = grp < a.n - first;
+  const int32_t i = first + (mine ? grp : 0);
+  const float* row = a.Z + (int64_t)i * a.ld_z;
+  const int32_t act = a.action[i];
   f4 z[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) z[k] = load_cols(row, (k * G + lane) * 4, grp < rows ? a.C : 0);
-  RowIn r = {};
-  if (mine) r = row_in(a, first + t, act, LOSS);
+  for (int k = 0; k < V; ++k) z[k] = load_chunk<V>(row, k, (k * G + lane) * 4, a.C);
+  const RowIn r = row_in(a, i, act, LOSS);
+  z[V - 1] = cut_cols(z[V - 1], ((V - 1) * G + lane) * 4, a.C);
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
@@ -335,57 +354,39 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
     z[k] = exp4(z[k], shift);
     part += sum4(z[k]);
   }
-  part = lanes_sum<G>(part);
-  if (lane == 0) {
-    s_top[grp] = top;
-    s_sum[grp] = part;
-  }
-  if (t == 0) s_near = 0;
-  __syncthreads();
-  double sum = mine ? (double)s_sum[t] : 1.0;
-  if (!LOSS) {
-    if (mine) a.logp[first + t] = (float)log_prob<false>(r, s_top[t], sum);
-    return;
-  }
-  Terms terms = {0.0, 0.0, 0.0};
-  bool near = false;
-  if (mine) {
-    const double lp = log_prob<false>(r, s_top[t], sum);
-    near = row_terms<false>(a, r, sum, lp, &terms, &s_c[t]);
-    if (a.logp) a.logp[first + t] = (float)lp;
-    s_inv[t] = 1.f / (float)sum;
-    s_act[t] = r.act;
-    s_exact[t] = near ? -1.0 : 0.0;
-    if (near) s_near = 1;
-  }
-  __syncthreads();
-  if (s_near) {
-    for (int q = t >> 6; q < rows; q += THREADS / 64)
-      if (s_exact[q] < 0.0) {
-        const double exact = exact_sum(a.Z + ((int64_t)first + q) * a.ld_z, a.C, s_top[q]);
-        if ((t & 63) == 0) s_exact[q] = exact;
-      }
-    __syncthreads();
-    if (near) {
-      sum = s_exact[t];
-      row_terms<true>(a, r, sum, log_prob<true>(r, s_top[t], sum), &terms, &s_c[t]);
-      s_inv[t] = 1.f / (float)sum;
+  double sum = lanes_sum<G>(part);
+  const double lp = log_prob<false>(r, top, sum);
+  if (lane == 0 && mine && a.logp) a.logp[i] = (float)lp;
+  if (!LOSS) return;
+  Terms terms;
+  float c;
+  const bool near = row_terms<false>(a, r, sum, lp, &terms, &c);
+  if (__any(near)) {
+    // each such row by the whole wavefront
+    for (uint64_t rows = __ballot(near && lane == 0); rows; rows &= rows - 1) {
+      const int from = __ffsll((unsigned long long)rows) - 1;
+      const int32_t q = __shfl(i, from, 64);
+      const double s = exact_sum(a.Z + (int64_t)q * a.ld_z, a.C, __shfl(top, from, 64));
+      if ((t & 63) / G == from / G) sum = s;
     }
-    __syncthreads();
+    if (near) row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &c);
     // read once more, so that this branch has the registers
-    const float again = shift_of(s_top[grp]);
 #pragma unroll
-    for (int k = 0; k < V; ++k)
-      z[k] = exp4(load_cols(row, (k * G + lane) * 4, grp < rows ? a.C : 0), again);
+    for (int k = 0; k < V; ++k) z[k] = load_chunk<V>(row, k, (k * G + lane) * 4, a.C);
+    z[V - 1] = cut_cols(z[V - 1], ((V - 1) * G + lane) * 4, a.C);
+#pragma unroll
+    for (int k = 0; k < V; ++k) z[k] = exp4(z[k], shift);
   }
-  if (a.dZ && grp < rows) {
-    float* to = a.dZ + ((int64_t)first + grp) * a.ld_dz;
+  if (a.dZ && mine) {
+    float* to = a.dZ + (int64_t)i * a.ld_dz;
+    const float inv = 1.f / (float)sum;
 #pragma unroll
     for (int k = 0; k < V; ++k) {
       const int32_t col = (k * G + lane) * 4;
-      store_cols(to, col, a.C, grad4(z[k], col, s_act[grp], s_c[grp], s_inv[grp]));
+      store_cols(to, col, a.C, grad4(z[k], col, r.act, c, inv));
     }
   }
+  if (lane != 0 || !mine) terms = {0.0, 0.0, 0.0};
   store_terms(a, block_terms<THREADS>(terms));
 }
 
@@ -403,8 +404,9 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   const int32_t act = a.action[i];
   f4 z[V];
 #pragma unroll
-  for (int k = 0; k < V; ++k) z[k] = load_cols(row, (k * T + t) * 4, a.C);
+  for (int k = 0; k < V; ++k) z[k] = load_chunk<V>(row, k, (k * T + t) * 4, a.C);
   const RowIn r = row_in(a, i, act, LOSS);
+  z[V - 1] = cut_cols(z[V - 1], ((V - 1) * T + t) * 4, a.C);
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < V; ++k) top = fmaxf(top, max4(z[k]));
@@ -452,7 +454,10 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
     __syncthreads();
     // read once more, so that this branch has the registers
 #pragma unroll
-    for (int k = 0; k < V; ++k) z[k] = exp4(load_cols(row, (k * T + t) * 4, a.C), shift);
+    for (int k = 0; k < V; ++k) z[k] = load_chunk<V>(row, k, (k * T + t) * 4, a.C);
+    z[V - 1] = cut_cols(z[V - 1], ((V - 1) * T + t) * 4, a.C);
+#pragma unroll
+    for (int k = 0; k < V; ++k) z[k] = exp4(z[k], shift);
   }
   store_terms(a, terms);
   if (!a.dZ) return;
@@ -487,6 +492,8 @@ __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
   f4 z[SPLIT_V];
 #pragma unroll
   for (int k = 0; k < SPLIT_V; ++k) z[k] = load_cols(row, first + (k * THREADS + t) * 4, a.C);
+#pragma unroll
+  for (int k = 0; k < SPLIT_V; ++k) z[k] = cut_cols(z[k], first + (k * THREADS + t) * 4, a.C);
   float top = max4(z[0]);
 #pragma unroll
   for (int k = 1; k < SPLIT_V; ++k) top = fmaxf(top, max4(z[k]));
@@ -518,7 +525,13 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   const int64_t b = a.block0 + blockIdx.x;
   const int32_t i = (int32_t)(b / todo), chunk = (int32_t)(b % todo);
   const float* row = a.Z + (int64_t)i * a.ld_z;
-  const RowIn r = row_in(a, i, a.action[i], LOSS);
+  const int32_t act = a.action[i];
+  f4 z[SPLIT_V];
+  if (LOSS && a.dZ)
+#pragma unroll
+    for (int k = 0; k < SPLIT_V; ++k)
+      z[k] = load_cols(row, chunk * SPLIT_COLS + (k * THREADS + t) * 4, a.C);
+  const RowIn r = row_in(a, i, act, LOSS);
   // every wavefront joins the row's sums alike
   const Chunk* at = a.chunks + (int64_t)i * a.per_row;
   float top = -INFINITY;
@@ -547,8 +560,7 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
 #pragma unroll
   for (int k = 0; k < SPLIT_V; ++k) {
     const int32_t col = chunk * SPLIT_COLS + (k * THREADS + t) * 4;
-    if (col < a.C)
-      store_cols(to, col, a.C, grad4(exp4(load_cols(row, col, a.C), shift), col, r.act, c, inv));
+    store_cols(to, col, a.C, grad4(exp4(cut_cols(z[k], col, a.C), shift), col, r.act, c, inv));
   }
 }
 
@@ -760,9 +772,12 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
   a.ld_z = ld_z;
   a.action = action;
   a.adv = advantage;
-  a.old_lp = old_logp;
-  a.ref_lp = ref_logp;
-  a.weight = weight;
+  a.has_old = old_logp != nullptr;
+  a.has_ref = ref_logp != nullptr;
+  a.has_weight = weight != nullptr;
+  a.old_lp = old_logp ? old_logp : advantage;
+  a.ref_lp = ref_logp ? ref_logp : advantage;
+  a.weight = weight ? weight : advantage;
   a.lo = 1.0 - clip_lo;
   a.hi = 1.0 + clip_hi;
   a.beta = beta;
