@@ -186,14 +186,9 @@ struct Coef {
   uint64_t base;  // output t of the generator started at the seed
 };
 
-// The gradients' factor; false: the step is skipped.
-__device__ inline bool clip_factor(const Coef& a, double* k) {
-  *k = 1.0;
-  if (!a.norm) return true;
-  const float norm = *a.norm;
-  if (!(fabsf(norm) < INFINITY)) return false;
-  if ((double)norm > a.max_norm) *k = a.max_norm / (double)norm;
-  return true;
+// The gradients' factor from their norm (0 where there is none).
+__device__ inline double clip_factor(const Coef& a, float norm) {
+  return (double)norm > a.max_norm ? a.max_norm / (double)norm : 1.0;
 }
 
 // The bias corrections are in the coefficients, the quotient is a product
@@ -276,8 +271,7 @@ struct Raw8 {
 
 // A thread's accesses to a piece are all under way before the first is used.
 template <bool FULL>
-__device__ inline void piece32(const Tensor& t, int64_t base, double kd, float keep,
-                               const Coef& a) {
+__device__ inline void piece32(const Tensor& t, int64_t base, float norm, const Coef& a) {
   float *m = static_cast<float*>(t.m), *v = static_cast<float*>(t.v);
   Raw32 x[AT_ONCE];
 #pragma unroll
@@ -286,7 +280,9 @@ __device__ inline void piece32(const Tensor& t, int64_t base, double kd, float k
     x[q] = {load4<FULL>(t.W, i, t.count), load4<FULL>(t.G, i, t.count),
             load4<FULL>(m, i, t.count), load4<FULL>(v, i, t.count)};
   }
-  const float k = (float)kd, b1 = (float)a.b1, omb1 = (float)a.omb1, b2 = (float)a.b2,
+  if (!(fabsf(norm) < INFINITY)) return;  // (asked here, when the reads are under way)
+  const float keep = (float)(1.0 - a.lr * t.decay);
+  const float k = (float)clip_factor(a, norm), b1 = (float)a.b1, omb1 = (float)a.omb1, b2 = (float)a.b2,
               omb2 = (float)a.omb2;
 #pragma unroll
   for (int q = 0; q < AT_ONCE; ++q) {
@@ -306,8 +302,7 @@ __device__ inline void piece32(const Tensor& t, int64_t base, double kd, float k
 
 // 8-bit moments: the 64 lanes of a wavefront hold one block of 256.
 template <bool FULL>
-__device__ inline void piece8(const Tensor& t, int64_t base, double k, float keep,
-                              const Coef& a) {
+__device__ inline void piece8(const Tensor& t, int64_t base, float norm, const Coef& a) {
   uint8_t *m = static_cast<uint8_t*>(t.m), *v = static_cast<uint8_t*>(t.v);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   Raw8 x[AT_ONCE];
@@ -319,6 +314,9 @@ __device__ inline void piece8(const Tensor& t, int64_t base, double k, float kee
             load_codes<FULL>(m, i, t.count), load_codes<FULL>(v, i, t.count),
             t.m_scale[first / BLOCK], t.v_scale[first / BLOCK]};
   }
+  if (!(fabsf(norm) < INFINITY)) return;
+  const float keep = (float)(1.0 - a.lr * t.decay);
+  const double k = clip_factor(a, norm);
   const double gm = a.omb1 * k, gv = a.omb2 * k * k;
   const uint64_t lane_state = (uint64_t)lane * (2 * GOLDEN);  // two draws a lane
 #pragma unroll
@@ -379,22 +377,22 @@ __global__ __launch_bounds__(THREADS) void adamw_kernel(const void* plan, int32_
                                                         int64_t piece0, Coef a) {
   const Plan p = plan_at(plan, n);
   const int64_t piece = piece0 + blockIdx.x;
-  if (piece >= p.head->pieces || p.head->state_bits != BITS) return;
-  double k;
-  if (!clip_factor(a, &k)) return;
+  // three reads that do not wait for each other
+  const PlanHead head = *p.head;
   const Piece at = p.pieces[piece];
-  const Tensor& t = p.tensors[at.tensor];
+  const float norm = a.norm ? *a.norm : 0.f;
+  if (piece >= head.pieces || head.state_bits != BITS) return;
+  const Tensor t = p.tensors[at.tensor];
   // (a plan for the norm alone has no weights)
   if (!t.W || !t.m || !t.v || (BITS == 8 && (!t.m_scale || !t.v_scale))) return;
-  const float keep = (float)(1.0 - a.lr * t.decay);
   const int64_t base = (int64_t)at.index * PIECE;
   const bool full = base + PIECE <= t.count;
   if (BITS == 32) {
-    if (full) piece32<true>(t, base, k, keep, a);
-    else piece32<false>(t, base, k, keep, a);
+    if (full) piece32<true>(t, base, norm, a);
+    else piece32<false>(t, base, norm, a);
   } else {
-    if (full) piece8<true>(t, base, k, keep, a);
-    else piece8<false>(t, base, k, keep, a);
+    if (full) piece8<true>(t, base, norm, a);
+    else piece8<false>(t, base, norm, a);
   }
 }
 
