@@ -86,9 +86,18 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef f4 f4u __attribute__((aligned(4)));
 typedef uint32_t u32u __attribute__((aligned(1)));
 
+// Addresses out of the plan are known to the compiler as device memory only
+// where it is told.
+#define GLOBAL __attribute__((address_space(1)))
+template <class T>
+__device__ inline GLOBAL T* global(T* p) {
+  return (GLOBAL T*)p;
+}
+
 template <bool FULL>
-__device__ inline f4 load4(const float* p, int64_t i, int64_t count) {
-  if (FULL || i + 4 <= count) return *reinterpret_cast<const f4u*>(p + i);
+__device__ inline f4 load4(const float* q, int64_t i, int64_t count) {
+  const GLOBAL float* p = global(q);
+  if (FULL || i + 4 <= count) return *(const GLOBAL f4u*)(p + i);
   f4 r = {0.f, 0.f, 0.f, 0.f};
   if (i < count) r.x = p[i];
   if (i + 1 < count) r.y = p[i + 1];
@@ -96,9 +105,10 @@ __device__ inline f4 load4(const float* p, int64_t i, int64_t count) {
   return r;
 }
 template <bool FULL>
-__device__ inline void store4(float* p, int64_t i, int64_t count, f4 r) {
+__device__ inline void store4(float* q, int64_t i, int64_t count, f4 r) {
+  GLOBAL float* p = global(q);
   if (FULL || i + 4 <= count) {
-    *reinterpret_cast<f4u*>(p + i) = r;
+    *(GLOBAL f4u*)(p + i) = r;
     return;
   }
   if (i < count) p[i] = r.x;
@@ -106,8 +116,9 @@ __device__ inline void store4(float* p, int64_t i, int64_t count, f4 r) {
   if (i + 2 < count) p[i + 2] = r.z;
 }
 template <bool FULL>
-__device__ inline uint32_t load_codes(const uint8_t* p, int64_t i, int64_t count) {
-  if (FULL || i + 4 <= count) return *reinterpret_cast<const u32u*>(p + i);
+__device__ inline uint32_t load_codes(const uint8_t* q, int64_t i, int64_t count) {
+  const GLOBAL uint8_t* p = global(q);
+  if (FULL || i + 4 <= count) return *(const GLOBAL u32u*)(p + i);
   uint32_t r = 0;
   if (i < count) r = p[i];
   if (i + 1 < count) r |= (uint32_t)p[i + 1] << 8;
@@ -115,9 +126,10 @@ __device__ inline uint32_t load_codes(const uint8_t* p, int64_t i, int64_t count
   return r;
 }
 template <bool FULL>
-__device__ inline void store_codes(uint8_t* p, int64_t i, int64_t count, uint32_t r) {
+__device__ inline void store_codes(uint8_t* q, int64_t i, int64_t count, uint32_t r) {
+  GLOBAL uint8_t* p = global(q);
   if (FULL || i + 4 <= count) {
-    *reinterpret_cast<u32u*>(p + i) = r;
+    *(GLOBAL u32u*)(p + i) = r;
     return;
   }
   if (i < count) p[i] = (uint8_t)r;
@@ -312,7 +324,7 @@ __device__ inline void piece8(const Tensor& t, int64_t base, float norm, const C
     if (!FULL && first >= t.count) break;
     x[q] = {load4<FULL>(t.W, i, t.count), load4<FULL>(t.G, i, t.count),
             load_codes<FULL>(m, i, t.count), load_codes<FULL>(v, i, t.count),
-            t.m_scale[first / BLOCK], t.v_scale[first / BLOCK]};
+            global(t.m_scale)[first / BLOCK], global(t.v_scale)[first / BLOCK]};
   }
   if (!(fabsf(norm) < INFINITY)) return;
   const float keep = (float)(1.0 - a.lr * t.decay);
@@ -366,8 +378,8 @@ __device__ inline void piece8(const Tensor& t, int64_t base, float norm, const C
     store_codes<FULL>(m, i, t.count, mc);
     store_codes<FULL>(v, i, t.count, vc);
     if (lane == 0) {
-      t.m_scale[first / BLOCK] = msn;
-      t.v_scale[first / BLOCK] = vsn;
+      global(t.m_scale)[first / BLOCK] = msn;
+      global(t.v_scale)[first / BLOCK] = vsn;
     }
   }
 }
