@@ -48,13 +48,23 @@ __host__ __device__ inline uint64_t splitmix(uint64_t state, uint64_t k) {
 // differ in the lower bits hold the same value already (a mirror stands for
 // the xor of 4 and of 8): in a butterfly over D = 1, 2, 4, ... in this order.
 template <int D>
+__device__ inline int butterfly_word(int x) {
+  if (D == 1) return __builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, true);
+  if (D == 2) return __builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, true);
+  if (D == 4) return __builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, true);
+  if (D == 8) return __builtin_amdgcn_mov_dpp(x, 0x140, 0xF, 0xF, true);
+  return __shfl_xor(x, D, 64);
+}
+template <int D>
 __device__ inline float butterfly(float v) {
-  const int x = __float_as_int(v);
-  if (D == 1) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, true));
-  if (D == 2) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, true));
-  if (D == 4) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, true));
-  if (D == 8) return __int_as_float(__builtin_amdgcn_mov_dpp(x, 0x140, 0xF, 0xF, true));
-  return __shfl_xor(v, D, 64);
+  return __int_as_float(butterfly_word<D>(__float_as_int(v)));
+}
+template <int D>
+__device__ inline double butterfly(double v) {
+  const long long x = __double_as_longlong(v);
+  const uint32_t hi = (uint32_t)butterfly_word<D>((int)(x >> 32));
+  const uint32_t lo = (uint32_t)butterfly_word<D>((int)x);
+  return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
 // Largest value and sum over groups of G consecutive lanes, in all of them.
 template <int G, int D = 1>
@@ -62,8 +72,8 @@ __device__ inline float lanes_max(float v) {
   if constexpr (D < G) return lanes_max<G, 2 * D>(fmaxf(v, butterfly<D>(v)));
   else return v;
 }
-template <int G, int D = 1>
-__device__ inline float lanes_sum(float v) {
+template <int G, int D = 1, typename T>
+__device__ inline T lanes_sum(T v) {
   if constexpr (D < G) return lanes_sum<G, 2 * D>(v + butterfly<D>(v));
   else return v;
 }

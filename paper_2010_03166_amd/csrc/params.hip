@@ -137,15 +137,16 @@ __device__ inline void store_codes(uint8_t* q, int64_t i, int64_t count, uint32_
   if (i + 2 < count) p[i + 2] = (uint8_t)(r >> 16);
 }
 
+// The block's sum in all threads, in a fixed order.
 __device__ inline double block_sum(double v) {
-  __shared__ double s[THREADS];
-  s[threadIdx.x] = v;
+  __shared__ double s[THREADS / 64];
+  v = lanes_sum<64>(v);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int d = THREADS / 2; d > 0; d >>= 1) {
-    if ((int)threadIdx.x < d) s[threadIdx.x] += s[threadIdx.x + d];
-    __syncthreads();
-  }
-  return s[0];
+  v = s[0];
+#pragma unroll
+  for (int k = 1; k < THREADS / 64; ++k) v += s[k];
+  return v;
 }
 
 constexpr int AT_ONCE = PIECE / (4 * THREADS);  // accesses of a thread to a piece

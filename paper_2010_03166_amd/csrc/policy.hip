@@ -199,19 +199,13 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
 
 // ------------------------------------------------------------- reductions
 
-__device__ inline double wave_sum(double v) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d, 64);
-  return v;
-}
-
 // The block's sum of terms in thread 0, in a fixed order.
 template <int T>
 __device__ inline Terms block_terms(Terms t) {
   __shared__ Terms s[T / 64];
-  t.loss = wave_sum(t.loss);
-  t.kl = wave_sum(t.kl);
-  t.cut = wave_sum(t.cut);
+  t.loss = lanes_sum<64>(t.loss);
+  t.kl = lanes_sum<64>(t.kl);
+  t.cut = lanes_sum<64>(t.cut);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = t;
   __syncthreads();
   t = s[0];
@@ -243,7 +237,7 @@ __device__ inline double exact_part(const float* z, int32_t C, float top, int32_
   double sum = 0.0;
 #pragma unroll 1
   for (int32_t j = at; j < C; j += step) sum += exp_exact((double)z[j] - shift);
-  return wave_sum(sum);
+  return lanes_sum<64>(sum);
 }
 __device__ inline double exact_sum(const float* z, int32_t C, float top) {
   return exact_part(z, C, top, threadIdx.x & 63, 64);
@@ -543,7 +537,7 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
     const Chunk c = at[k];
     sum += c.sum * exp_quick((double)shift_of(c.top) - shift);
   }
-  sum = wave_sum(sum);
+  sum = lanes_sum<64>(sum);
   const double lp = log_prob<false>(r, top, sum);
   if (t == 0 && chunk == 0 && a.logp) a.logp[i] = (float)lp;
   if (!LOSS) return;
