@@ -633,8 +633,10 @@ Launch choose(int32_t C) {
   return {nullptr, 0, 0};
 }
 
-// Partial terms that one block adds; more are added in SHARES blocks first.
-constexpr int32_t FINAL_MOST = 32768, SHARES = 256;
+// Partial terms that one block adds; more are added in SHARES blocks first (us
+// a call with one launch and with two: 7,500 terms 52.1 and 52.4, 16,384 terms
+// 56.2 and 54.3, 30,000 terms 58.5 and 53.3).
+constexpr int32_t FINAL_MOST = 8192, SHARES = 64;
 // Blocks of one launch (2^32 threads are the most that a launch can have).
 constexpr int64_t LAUNCH_BLOCKS = 1 << 21;
 
@@ -682,7 +684,7 @@ gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
     const Terms* from = parts > FINAL_MOST ? shares : a.part;
     const int32_t count = parts > FINAL_MOST ? SHARES : parts;
     if (parts > FINAL_MOST)
-      policy_final_kernel<1024><<<SHARES, 1024, 0, stream>>>(parts, a.part, shares, nullptr);
+      policy_final_kernel<256><<<SHARES, 256, 0, stream>>>(parts, a.part, shares, nullptr);
     if (count <= 1024)
       policy_final_kernel<256><<<1, 256, 0, stream>>>(count, from, nullptr, a.out);
     else

@@ -154,7 +154,7 @@ def test_policy_widths(n, C):
 
 @pytest.mark.parametrize("n,C", [(1, 8191), (3, 8192), (40, 9000), (5, 16384), (2, 16385),
                                  (300, 16390), (1, 32768), (2, 32769), (70, 33000), (1, 100003),
-                                 (3, 131072), (1, 1000003), (6000, 300), (20000, 41), (70001, 7)])
+                                 (3, 131072), (1, 1000003), (6000, 300), (20000, 41), (70001, 7), (9001, 515)])
 @pytest.mark.parametrize("aligned", [True, False])
 def test_policy_long_rows_and_many(n, C, aligned):
     pad = -C % 4 if aligned else 1 + C % 2
