@@ -4,6 +4,20 @@
 // Per row: top = max z, sum = sum exp(z - top), lp = z[a] - top - log sum;
 // then the row's loss terms and the slope c = w dl/dlp, and the gradient
 // c (1[j = a] - exp(z_j - top) / sum).
+//
+// Bound by memory: 4 bytes a logit read, with a gradient 4 written.  So every
+// row is read once, held in registers from its sums to its gradient, by as
+// many lanes as its length takes (choose() below), and all of a row's reads
+// are under way before the first is waited for.  Only rows past 32,768 columns
+// are read twice.  Measured, us a call (and what of it are the final sums, a
+// launch of their own unless one block has all rows):
+//   50,001 x 121, rows off alignment   14.9 (2.5)   3.3 TB/s
+//   16,384 x 2,048                     52.9 (6)     5.1 TB/s, a large copy 5.05
+//   64 x 131,071                       23.1 (2.5)   2.9 TB/s
+//   2,000 x 20,011, log-probabilities  29.8         5.4 TB/s
+// What the same accesses take with nothing computed: 10.6 us for the first.
+// Stores past the caches (non-temporal) take 3 to 15 % off the rows of whole
+// cache lines, but the product that reads dZ next loses more than that.
 #include <cmath>
 
 #include "abi.hpp"
@@ -320,9 +334,11 @@ __device__ inline f4 grad4(f4 e, int32_t col, int32_t act, float c, float inv) {
 
 // ------------------------------------------------ several rows a wavefront
 
-// G lanes to a row of at most 4 G V columns, R = 256 / G rows a block, read
-// once into registers.  Every lane computes its row's scalars: the same
-// instructions as for one lane, and no wavefront waits for another.
+// G lanes to a row of at most 4 G V columns, R = 256 / G rows a block.  Every
+// lane computes its row's scalars: the same instructions as for one lane, and
+// no wavefront waits for another.  (One thread a row, between two barriers:
+// 60,000 x 500 58.6 -> 63.5 us.)  72 registers let seven blocks share a CU:
+// six and eight, with spills, are slower for some widths and faster for none.
 template <int G, int V, bool LOSS>
 __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
   constexpr int R = THREADS / G;
@@ -386,7 +402,7 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
 
 // ---------------------------------------------------------- one row a block
 
-// T threads to a row of at most 4 T V columns, in registers.
+// T threads to a row of at most 4 T V columns.
 template <int T, int V, bool LOSS>
 __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   __shared__ float s_top[T / 64], s_c, s_inv;
@@ -466,10 +482,15 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
 
 // -------------------------------------------------------- several blocks a row
 
-// Rows longer than a block's registers are cut into chunks, a block each:
-// one launch for the chunks' sums, one that joins a row's sums, computes its
+// Rows longer than 32,768 columns are cut into chunks, a block each: one
+// launch for the chunks' sums, one that joins a row's sums, computes its
 // scalars in every block of the row alike, and writes the chunk's gradient
-// from a second reading (out of the caches, for the few rows that are so long).
+// from a second reading (out of the caches, for the few rows that are so
+// long).  Blocks of 1,024 threads with up to 16 chunks a thread would take
+// rows of up to 65,536 once: 600 x 40,000 56 us instead of 60, 500 x 65,536 66
+// instead of 82, but 1 x 65,536 13.3 instead of 9.9 and its log-probabilities
+// 9.7 instead of 5.3.  Chunks of 2,048 / 4,096 / 8,192: 64 x 131,071 28.3 /
+// 26.6 / 26.9 us, 1 x 131,071 9.4 / 10.4 / 12.5.
 constexpr int SPLIT_V = 4;
 constexpr int SPLIT_COLS = 4 * THREADS * SPLIT_V;
 __host__ __device__ inline int32_t chunks_of(int32_t C) {
@@ -601,7 +622,11 @@ Launch block_of(int v) {
 }
 
 // Three or four chunks of four columns a lane where the row is long enough,
-// and as few lanes as that takes.
+// and as few lanes as that takes: few exchanges between lanes, few lanes past
+// the row's end.  Measured with one chunk a lane and with this rule, us:
+// 200,000 x 41 37 and 27, 200,000 x 121 82 and 58, 30,000 x 1,000 88 and 66,
+// 16,384 x 2,048 87 and 66, 2,000 x 20,011 (five chunks, eight before) 104 and
+// 83; two and eight chunks lie between.
 template <bool LOSS>
 Launch choose(int32_t C) {
   const int64_t q = ceil_div(C, 4);
