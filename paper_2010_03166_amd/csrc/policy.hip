@@ -370,7 +370,7 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
   if (!LOSS) return;
   Terms terms;
   float c;
-  const bool near = row_terms<false>(a, r, sum, lp, &terms, &c);
+  const bool near = row_terms<false>(a, r, sum, lp, &terms, &c) && mine;
   if (__any(near)) {
     // each such row by the whole wavefront
     for (uint64_t rows = __ballot(near && lane == 0); rows; rows &= rows - 1) {

@@ -818,3 +818,81 @@ def test_policy_step_checks_and_no_rows():
     assert torch.all(out == 0) and tr.action_logp(X[:0], none.int()).numel() == 0
     assert all(torch.all(g == 0) for _, g in tr.pairs)
     assert torch.isfinite(tr.flat_w).all() and not torch.equal(tr.flat_w, w0)  # decay alone
+
+
+def test_policy_iteration_replayed():
+    """A policy iteration captured (with SGD: AdamW's t is a host value) and
+    replayed between eager ones, every replay against them."""
+    cap, d, _, X, _ = _trainer("sgd", lr=1e-3)
+    eager, _, _, _, _ = _trainer("sgd", lr=1e-3)
+    n = cap.n
+    act = torch.arange(n, device="cuda", dtype=torch.int32) % (cap.C + 1)  # C: left out
+    adv = torch.randn(n, device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    old = eager.action_logp(X, act)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    cap.policy_step(X, act, adv, old, old, beta=0.1, stream=s.cuda_stream)  # grows the buffers
+    torch.cuda.synchronize()
+    eager.policy_step(X, act, adv, old, old, beta=0.1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        cap.policy_step(X, act, adv, old, old, beta=0.1, stream=s.cuda_stream)
+    for it in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        eager.policy_step(X, act, adv, old, old, beta=0.1)
+        torch.cuda.synchronize()
+        assert torch.equal(cap.policy_out, eager.policy_out), it
+        for (w, _), (v, _) in zip(cap.pairs, eager.pairs):
+            assert torch.equal(w, v), it
+
+
+def test_policy_iteration_on_other_subgraphs():
+    """The trainer moved to a larger and back to a smaller subgraph between
+    steps gives what trainers made for each give."""
+    graphs = [prepared(synth.power_law_graph(k, 2.1, 8.0, seed=k)) for k in (300, 900, 200)]
+    rng = np.random.default_rng(0)
+    f, h, C = 24, 16, 5
+    params = [synth.LayerParams(synth.glorot(f, h, rng), synth.glorot(f, h, rng))]
+    w_mlp = synth.glorot(2 * h, C, rng)
+    one = runtime.Trainer(graphs[0], params, f, w_mlp, False, "sgd", lr=0.0)
+    for g in graphs:
+        x = to_dev(rng.standard_normal((g.n, f)).astype(np.float32), 32)
+        act = torch.from_numpy(rng.integers(0, C, g.n).astype(np.int32)).cuda()
+        adv = _f(rng.standard_normal(g.n))
+        one.bind(g)
+        fresh = runtime.Trainer(g, params, f, w_mlp, False, "sgd", lr=0.0)
+        a, b = one.policy_step(x, act, adv), fresh.policy_step(x, act, adv)
+        torch.cuda.synchronize()
+        assert torch.equal(a, b)
+        for (_, p), (_, q) in zip(one.pairs, fresh.pairs):
+            assert torch.equal(p, q)
+
+
+def test_current_stream_and_timer():
+    """Calls without a stream go to torch's current one; the event timer
+    counts the launches under their kernels."""
+    assert G._stream(None) == torch.cuda.current_stream().cuda_stream
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        assert G._stream(None) == s.cuda_stream
+    assert G._stream(None) == torch.cuda.current_stream().cuda_stream
+    z, a, adv, old, ref, w = _case(50, 9, 1)
+    ts = _tensors([3000], 8, 1)
+    ps, _ = _params(ts, 8)
+    norm = torch.zeros(1, device="cuda")
+    ws = _ws(G.gnn_grad_norm_workspace_bytes(ps))
+    torch.cuda.synchronize()
+    G.gnn_timer_reset()
+    G.gnn_timer_enable(True)
+    try:
+        run_loss(z, a, adv, old, ref, w)
+        G.gnn_grad_norm(ps, norm, ws)
+        G.gnn_adamw_step(ps, 1e-3, 0.9, 0.99, 1e-8, 1, norm)
+        for name, work in (("loss", 8.0 * 50 * 9), ("norm", 12000.0), ("update", 48000.0)):
+            ms, launches, got = G.gnn_timer_read(name)
+            assert launches == 1 and ms > 0 and got == work, name
+    finally:
+        G.gnn_timer_enable(False)
+        G.gnn_timer_reset()
