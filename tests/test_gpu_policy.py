@@ -352,6 +352,65 @@ def test_policy_offsets_past_32_bits():
         assert torch.equal(x, y)
 
 
+def _room(nbytes):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < nbytes:
+        pytest.skip("needs %d GB of free device memory" % (nbytes >> 30))
+
+
+def test_policy_more_blocks_than_one_launch():
+    """2^21 + 50 rows of a block each (two launches): the same rows in calls
+    of one launch give the same bits."""
+    n, C, cut = 2 ** 21 + 50, 520, 2 ** 21 - 100
+    _room(30 << 30)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    Z = torch.randn((n, C), device="cuda", generator=g)
+    act = torch.randint(0, C, (n,), device="cuda", generator=g, dtype=torch.int32)
+    adv, old, w = (torch.randn(n, device="cuda", generator=g) for _ in range(3))
+    old.sub_(7.0)
+    w.abs_().div_(n)
+    ws = _ws(G.gnn_policy_workspace_bytes(n, C))
+    dZ = torch.empty_like(Z)
+    res = []
+    for parts in ([(0, n)], [(0, cut), (cut, n)]):
+        dZ.fill_(SENTINEL)
+        logp = torch.empty(n, device="cuda")
+        outs = []
+        for b, e in parts:
+            out = torch.empty(3, device="cuda")
+            G.gnn_policy_loss(e - b, C, Z[b:e], C, act[b:e], adv[b:e], old[b:e], old[b:e], w[b:e],
+                              0.2, 0.2, 0.1, out, logp[b:e], dZ[b:e], C, ws)
+            outs.append(out)
+        torch.cuda.synchronize()
+        res.append((torch.stack(outs).double().sum(0), logp, dZ[::7].clone(), dZ[-2000:].clone()))
+    # one rounding of each output, of two in the second case
+    assert bool(((res[0][0] - res[1][0]).abs() <= 4 * U * res[0][0].abs().clamp(min=1e-3)).all())
+    for x, y in zip(res[0][1:], res[1][1:]):
+        assert torch.equal(x, y)
+
+
+def test_policy_two_calls_at_once():
+    """Two streams, each with its own workspace, call after call."""
+    cases = [_case(3000, 121, 20), _case(40, 20000, 21), _case(3, 70000, 22), _case(9000, 7, 23)]
+    alone = [run_loss(*c, beta=0.05) for c in cases]
+    args, streams = [], [torch.cuda.Stream() for _ in cases]
+    for z, a, adv, old, ref, w in cases:
+        n, C = z.shape
+        args.append([n, C, to_dev(z), C, torch.from_numpy(a.astype(np.int32)).cuda(), _f(adv),
+                     _f(old), _f(ref), _f(w), 0.2, 0.3, 0.05, torch.zeros(3, device="cuda"),
+                     torch.zeros(n, device="cuda"), torch.zeros((n, C), device="cuda"), C,
+                     _ws(G.gnn_policy_workspace_bytes(n, C))])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, s in zip(args, streams):
+            G.gnn_policy_loss(*x, stream=s)
+    torch.cuda.synchronize()
+    for x, one in zip(args, alone):
+        assert np.array_equal(x[12].cpu().numpy(), one["out"])
+        assert np.array_equal(x[13].cpu().numpy(), one["logp"])
+        assert np.array_equal(x[14].cpu().numpy(), one["dZ"])
+
+
 @pytest.mark.parametrize("n,C", SHAPES)
 def test_policy_graph_replay(n, C):
     """Captured and replayed between eager calls, its inputs changed."""
@@ -639,6 +698,29 @@ def test_adamw_past_32_bit_offsets(bits):
     assert bool((m[c:] == 0).all()) and bool((v[c:] == 0).all())
     if bits == 8:  # every element the block's largest: the top code
         assert bool((m[:c] == 126).all()) and bool((v[:c] == 123).all())
+
+
+def test_adamw_more_pieces_than_one_launch():
+    """2^33 + 5,000 weights: more pieces than a launch has blocks."""
+    c = 2 ** 33 + 5000
+    _room(120 << 30)
+    W, g = torch.empty(c + 64, device="cuda"), torch.empty(c + 64, device="cuda")
+    m, v = (torch.zeros(c + 64, dtype=torch.uint8, device="cuda") for _ in range(2))
+    sc = [torch.zeros(-(-c // 256), device="cuda") for _ in range(2)]
+    W.fill_(0.5)
+    g.fill_(2.0 ** -10)
+    ps = G.make_params([(W[:c], g[:c], m[:c], v[:c]) + tuple(sc) + (0.1,)], 8)
+    plan = torch.empty(G.gnn_params_plan_bytes(ps), dtype=torch.uint8, device="cuda")
+    ps.plan = plan.data_ptr()
+    G.gnn_params_build_plan(ps, plan)
+    G.gnn_adamw_step(ps, 1e-2, 0.9, 0.99, 1e-8, 1, seed=7)
+    torch.cuda.synchronize()
+    first = W[0].item()
+    w, _, _ = P.adamw([0.5], [2.0 ** -10], [0.0], [0.0], 1e-2, 0.9, 0.99, 1e-8, 1, 0.1)
+    assert abs(first - w[0]) <= 8 * U
+    assert float(W[:c].min()) == first == float(W[:c].max()) and bool((W[c:] == 0.5).all())
+    assert int(m[:c].min()) == 126 == int(m[:c].max()) and bool((m[c:] == 0).all())
+    assert int(v[:c].min()) == 123 == int(v[:c].max()) and bool((v[c:] == 0).all())
 
 
 @pytest.mark.parametrize("bits", [32, 8])
