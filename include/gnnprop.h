@@ -392,8 +392,9 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
  * action: n int32.  A row whose action lies outside [0, C) is left out: its
  * logits are not used (they may hold anything), its lp is written as 0 and
  * its gradient as 0.  Logits of -inf take an action out of a row's choice; a
- * row with every logit -inf is left out too, with lp = -inf.  Sums of
- * exponentials, logarithms and the loss are formed in double.
+ * row with every logit -inf is left out too, with lp = -inf.  Exponentials
+ * are fp32's, added in fp32 within a few lanes and in double beyond: lp is off
+ * by less than (20 + ln C) 2^-24 before its own rounding.
  *
  * gnn_action_logp writes lp (n floats): what acting needs, and the old_logp /
  * ref_logp that gnn_policy_loss takes.
@@ -408,7 +409,8 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
  *   out   = [ sum_i w_i l_i,  sum_i w_i kl_i,  sum_i w_i 1[i is clipped] ]
  *   dZ[i, j] = w_i (dl_i / dlp_i) (1[j = a_i] - exp(Z[i, j]) / sum exp)
  *   dl_i / dlp_i = -A_i rho_i 1[i is not clipped] + beta (1 - exp(d_i))
- * where i is clipped if rho_i A_i > clip(rho_i, ...) A_i (decided in double).
+ * where i is clipped if rho_i A_i > clip(rho_i, ...) A_i: decided as sums of
+ * double exponentials decide it.  The three sums are formed in double.
  * advantage A, old_logp, ref_logp and weight w are n floats; weight NULL:
  * 1/n.  A row of weight 0 adds nothing and has a gradient of 0, whatever its
  * logits.  A chosen action with a logit of -inf has lp = -inf: its kl is
@@ -443,9 +445,9 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  *   m_scale, v_scale  state_bits 8: ceil(count / 256) floats each; state_bits
  *            32: not used
  *   weight_decay      of this tensor (0 for biases, say)
- * Moments start as zeros (scales too).  16-byte aligned W, G, m, v (8-bit
- * moments: 4-byte) enable the vector paths.  gnn_grad_norm alone needs only
- * count and G: W, m, v and the scales may then be NULL. */
+ * Moments start as zeros (scales too).  Any such alignment takes the vector
+ * path.  gnn_grad_norm alone needs only count and G: W, m, v and the scales
+ * may then be NULL. */
 typedef struct gnn_param {
   int64_t count;
   float* W;
