@@ -234,6 +234,8 @@ def test_policy_not_finite_rows_stay_alone(n, C):
     assert np.isnan(r["dZ"][1]).any() and not np.isfinite(r["logp"][0])
     assert np.array_equal(r["dZ"][2:], clean["dZ"][2:])
     assert np.array_equal(r["logp"][2:], clean["logp"][2:])
+    r = run_loss(z, a, adv, None, None, w)  # on-policy: a NaN shows as well
+    assert np.isnan(r["out"][0]) and np.isnan(r["dZ"][0]).all()
     # a chosen action without probability: lp = -inf, no slope without beta
     z, a, adv, old, ref, w = _case(n, C, 4)
     z[0, a[0]] = -np.inf
