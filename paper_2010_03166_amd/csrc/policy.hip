@@ -402,9 +402,15 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
 
 // ---------------------------------------------------------- one row a block
 
-// T threads to a row of at most 4 T V columns.
+// T threads to a row of at most 4 T V columns.  Of more than four chunks a
+// thread the rest waits in LDS from the sums to the gradient (each thread
+// reads what it wrote), so that 64 registers do and two blocks of 1,024
+// threads share a CU: 2,000 x 20,011 79 -> 68 us, 1,000 x 32,768 67 -> 60.5
+// (64 rows of 32,768, a block a CU either way: 11.5 -> 12.3).
 template <int T, int V, bool LOSS>
-__global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
+__global__ __launch_bounds__(T, T == 1024 ? 8 : 1) void block_kernel(PolicyArgs a) {
+  constexpr int KEPT = V < 4 || !LOSS ? V : 4, AWAY = V - KEPT;
+  __shared__ f4 s_away[AWAY > 0 ? AWAY * T : 1];
   __shared__ float s_top[T / 64], s_c, s_inv;
   __shared__ double s_sum[T / 64];
   __shared__ int32_t s_near;
@@ -432,6 +438,7 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
   for (int k = 0; k < V; ++k) {
     z[k] = exp4(z[k], shift);
     part += sum4(z[k]);
+    if (k >= KEPT) s_away[(k - KEPT) * T + t] = z[k];
   }
   part = lanes_sum<64>(part);
   if ((t & 63) == 0) s_sum[wave] = part;
@@ -464,10 +471,10 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
     __syncthreads();
     // read once more, so that this branch has the registers
 #pragma unroll
-    for (int k = 0; k < V; ++k) z[k] = load_chunk<V>(row, k, (k * T + t) * 4, a.C);
-    z[V - 1] = cut_cols(z[V - 1], ((V - 1) * T + t) * 4, a.C);
+    for (int k = 0; k < KEPT; ++k) z[k] = load_chunk<V>(row, k, (k * T + t) * 4, a.C);
+    if (AWAY == 0) z[V - 1] = cut_cols(z[V - 1], ((V - 1) * T + t) * 4, a.C);
 #pragma unroll
-    for (int k = 0; k < V; ++k) z[k] = exp4(z[k], shift);
+    for (int k = 0; k < KEPT; ++k) z[k] = exp4(z[k], shift);
   }
   store_terms(a, terms);
   if (!a.dZ) return;
@@ -476,7 +483,8 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
 #pragma unroll
   for (int k = 0; k < V; ++k) {
     const int32_t col = (k * T + t) * 4;
-    store_cols(to, col, a.C, grad4(z[k], col, r.act, c, inv));
+    const f4 e = k < KEPT ? z[k] : s_away[(k - KEPT) * T + t];
+    store_cols(to, col, a.C, grad4(e, col, r.act, c, inv));
   }
 }
 
@@ -486,8 +494,8 @@ __global__ __launch_bounds__(T) void block_kernel(PolicyArgs a) {
 // launch for the chunks' sums, one that joins a row's sums, computes its
 // scalars in every block of the row alike, and writes the chunk's gradient
 // from a second reading (out of the caches, for the few rows that are so
-// long).  Blocks of 1,024 threads with up to 16 chunks a thread would take
-// rows of up to 65,536 once: 600 x 40,000 56 us instead of 60, 500 x 65,536 66
+// long).  Blocks of 1,024 threads with up to 16 chunks a thread in registers
+// would take rows of up to 65,536 once: 600 x 40,000 56 us instead of 60, 500 x 65,536 66
 // instead of 82, but 1 x 65,536 13.3 instead of 9.9 and its log-probabilities
 // 9.7 instead of 5.3.  Chunks of 2,048 / 4,096 / 8,192: 64 x 131,071 28.3 /
 // 26.6 / 26.9 us, 1 x 131,071 9.4 / 10.4 / 12.5.
