@@ -354,6 +354,35 @@ def test_policy_offsets_past_32_bits():
         assert torch.equal(x, y)
 
 
+def _random_cases(count=60, seed=77):
+    rng = np.random.default_rng(seed)
+    out = []
+    for i in range(count):
+        C = int(round(2.0 ** rng.uniform(0, 15.6)))
+        n = int(round(2.0 ** rng.uniform(0, np.log2(min(4000, max(2, 600000 // C))))))
+        out.append((i, n, C, int(rng.integers(0, 9)), int(rng.integers(0, 4)),
+                    float(rng.choice([0.0, 0.4])), float(rng.choice([0.0, 0.3])),
+                    tuple(bool(b) for b in rng.integers(0, 2, 3)),
+                    float(rng.choice([0.0, 0.02, 1.0])),
+                    float(rng.choice([0.0, 0.1, 1.0])), float(rng.choice([0.0, 0.3, 10.0]))))
+    return out
+
+
+@pytest.mark.parametrize("case", _random_cases(), ids=lambda c: "case%d" % c[0])
+def test_policy_random_calls(case):
+    """Seeded random rows, columns, strides, alignments, masks, optional
+    arrays, clips and KL weights."""
+    i, n, C, pad, shift, mask, skip, has, beta, lo, hi = case
+    z, a, adv, old, ref, w = _case(n, C, 1000 + i, mask=mask, skip=skip)
+    old, w = old if has[0] else None, w if has[1] else None
+    if not has[2] and beta == 0.0:
+        ref = None
+    want = P.policy_loss(z, a, adv, old, ref, w, lo, hi, beta)
+    r = run_loss(z, a, adv, old, ref, w, lo=lo, hi=hi, beta=beta, pad=pad, shift=shift)
+    check_loss(r, want, z, a, adv, old, ref, beta)
+    check_logp(run_logp(z, a, pad, shift), want["logp"], C)
+
+
 def _room(nbytes):
     torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < nbytes:
@@ -561,6 +590,31 @@ def test_adamw_steps(case, shift, bits):
         G.gnn_adamw_step(ps, 1e-2, 0.9, 0.99, 1e-8, t, seed=99)
         torch.cuda.synchronize()
         check_step(before, ts, bits, decays, 1e-2, 0.9, 0.99, 1e-8, t, 1.0, 99)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_adamw_random_sets(seed):
+    """Seeded random sets: tensors of any length at any alignment, random
+    hyperparameters, steps and clipping."""
+    rng = np.random.default_rng(500 + seed)
+    bits = 8 if seed % 2 else 32
+    counts = [int(2.0 ** rng.uniform(0, 15)) for _ in range(int(rng.integers(1, 40)))]
+    ts = _tensors(counts, bits, seed, int(rng.integers(0, 5)))
+    ps, decays = _params(ts, bits)
+    norm = torch.zeros(1, device="cuda")
+    b1, b2 = float(rng.choice([0.0, 0.5, 0.9])), float(rng.choice([0.0, 0.95, 0.999]))
+    lr, eps = float(rng.choice([0.0, 1e-4, 0.1])), float(rng.choice([1e-12, 1e-8, 1e-3]))
+    for _ in range(2):
+        t = int(rng.integers(1, 100000))
+        G.gnn_grad_norm(ps, norm, _ws(G.gnn_grad_norm_workspace_bytes(ps)))
+        n = float(norm)
+        want = P.grad_norm([x["G"][0].cpu().numpy() for x in ts])
+        assert abs(n - want) <= U * want * (1 + 1e-6)
+        top = n * float(rng.choice([0.01, 0.9, 5.0]))
+        before = [_host(x) for x in ts]
+        G.gnn_adamw_step(ps, lr, b1, b2, eps, t, norm, top, seed * 7919)
+        torch.cuda.synchronize()
+        check_step(before, ts, bits, decays, lr, b1, b2, eps, t, min(1.0, top / n), seed * 7919)
 
 
 @pytest.mark.parametrize("bits", [32, 8])
