@@ -11,10 +11,10 @@
 // are under way before the first is waited for.  Only rows past 32,768 columns
 // are read twice.  Measured, us a call (and what of it are the final sums, a
 // launch of their own unless one block has all rows):
-//   50,001 x 121, rows off alignment   14.9 (2.5)   3.3 TB/s
-//   16,384 x 2,048                     52.9 (6)     5.1 TB/s, a large copy 5.05
+//   50,001 x 121, rows off alignment   15.0 (2.5)   3.3 TB/s
+//   16,384 x 2,048                     53.3 (4)     5.0 TB/s, a large copy 5.05
 //   64 x 131,071                       23.1 (2.5)   2.9 TB/s
-//   2,000 x 20,011, log-probabilities  29.8         5.4 TB/s
+//   2,000 x 20,011, log-probabilities  30.2         5.3 TB/s
 // What the same accesses take with nothing computed: 10.6 us for the first.
 // Stores past the caches (non-temporal) take 3 to 15 % off the rows of whole
 // cache lines, but the product that reads dZ next loses more than that.
