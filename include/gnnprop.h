@@ -415,9 +415,8 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
  * 1/n.  A row of weight 0 adds nothing and has a gradient of 0, whatever its
  * logits.  A chosen action with a logit of -inf has lp = -inf: its kl is
  * infinite, and its gradient not finite where beta > 0.  1 <= C <= 2^24,
- * 0 <= clip_lo <= 1,
- * clip_hi >= 0 (infinity: no upper clip), beta finite >= 0, needing ref_logp
- * where beta > 0 (else GNN_ERR_SHAPE / GNN_ERR_NULL).
+ * 0 <= clip_lo <= 1, clip_hi >= 0 (infinity: no upper clip), beta finite >= 0,
+ * needing ref_logp where beta > 0 (else GNN_ERR_SHAPE / GNN_ERR_NULL).
  * out: three floats.  logp (n floats) and dZ (n x C, stride ld_dz) may be
  * NULL.  Columns of dZ's rows past C are not written.  Everything is summed
  * in a fixed order (bit-reproducible).  n = 0 gives out = 0.  No output may
@@ -497,7 +496,8 @@ gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
  * non-finite, with 8-bit moments those of its whole block of 256 (so does one
  * whose square passes 1e43).
  * Hyperparameters are host values, taken at the call (a captured launch
- * replays with them): 0 <= beta1, beta2 < 1, eps >= 0, lr finite.
+ * replays with them): 0 <= beta1, beta2 < 1, eps >= 0 (with 0 a weight whose
+ * v is 0 becomes NaN, as the formula says), lr finite.
  *
  * 8-bit moments: m, v and the update are formed from unrounded new moments
  * (in double), which are then stored with scale = max over the block / 448

@@ -250,7 +250,7 @@ __device__ inline uint32_t encode(double y, uint32_t r) {
 // A block's scale and its reciprocal (NaN, 0 where it has a NaN or an
 // infinity).  `top`: the lane's largest magnitude; the wavefront's is found
 // among their roundings to fp32, then read from its lane (all of those that
-// round alike): six steps of 32 bits instead of 64.
+// round alike): six steps of 32 bits instead of 64.  `top` is no NaN.
 template <class F>
 __device__ inline float block_scale(double top, bool bad, double* inverse) {
   const float mine = (float)top;
@@ -300,8 +300,8 @@ __device__ inline void piece32(const Tensor& t, int64_t base, float norm, const 
   }
   if (!(fabsf(norm) < INFINITY)) return;  // (asked here, when the reads are under way)
   const float keep = (float)(1.0 - a.lr * t.decay);
-  const float k = (float)clip_factor(a, norm), b1 = (float)a.b1, omb1 = (float)a.omb1, b2 = (float)a.b2,
-              omb2 = (float)a.omb2;
+  const float k = (float)clip_factor(a, norm), b1 = (float)a.b1, omb1 = (float)a.omb1;
+  const float b2 = (float)a.b2, omb2 = (float)a.omb2;
 #pragma unroll
   for (int q = 0; q < AT_ONCE; ++q) {
     const int64_t i = base + (q * THREADS + threadIdx.x) * 4;
