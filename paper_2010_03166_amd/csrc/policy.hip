@@ -564,7 +564,9 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   double sum = 0.0;
   for (int32_t k = lane; k < a.per_row; k += 64) {
     const Chunk c = at[k];
-    sum += c.sum * exp_quick((double)shift_of(c.top) - shift);
+    // a chunk of nothing but -inf has no top to come from: the factor of its
+    // sum of 0 would be infinite where the row's logits are far below 0
+    if (c.sum != 0.0) sum += c.sum * exp_quick((double)shift_of(c.top) - shift);
   }
   sum = lanes_sum<64>(sum);
   const double lp = log_prob<false>(r, top, sum);
