@@ -489,7 +489,8 @@ gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
  *   g = k G;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2
  *   W = (1 - lr weight_decay) W
  *       - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
- * norm: device float (gnn_grad_norm's) or NULL.  NULL: k = 1.  Else
+ * norm: device float (gnn_grad_norm's) or NULL.  NULL: k = 1, whatever
+ * max_norm.  Else
  * k = max_norm / norm where norm > max_norm (max_norm > 0) and 1 elsewhere,
  * and a norm that is not finite skips the step: nothing is changed.
  * Without norm a NaN or infinite gradient makes its own weight and moments

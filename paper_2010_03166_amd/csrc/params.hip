@@ -204,7 +204,7 @@ struct Coef {
   uint64_t base;  // output t of the generator started at the seed
 };
 
-// The gradients' factor from their norm (0 where there is none).
+// The gradients' factor from their norm (without one: 0, and no limit to it).
 __device__ inline double clip_factor(const Coef& a, float norm) {
   return (double)norm > a.max_norm ? a.max_norm / (double)norm : 1.0;
 }
@@ -614,8 +614,8 @@ gnn_status gnn_adamw_step(const gnn_params* params, double lr, double beta1, dou
   if (pieces == 0) return GNN_OK;
   const Coef a = {lr, beta1, 1.0 - beta1, beta2, 1.0 - beta2, (float)eps,
                   (float)(lr / (1.0 - std::pow(beta1, t))),
-                  (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, t))), norm, max_norm,
-                  splitmix(seed, (uint64_t)t)};
+                  (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, t))), norm,
+                  norm ? max_norm : INFINITY, splitmix(seed, (uint64_t)t)};
   timer_begin(GNN_K_UPDATE, stream);
   for (int64_t p0 = 0; p0 < pieces; p0 += LAUNCH_PIECES) {
     const unsigned blocks = (unsigned)std::min(pieces - p0, LAUNCH_PIECES);

@@ -40,3 +40,22 @@ def test_masked_ranges_and_far_logits(n, C, top):
     assert np.isfinite(want["out"]).all() and np.isfinite(want["dZ"]).all()
     check_logp(run_logp(z, a), want["logp"], C)
     check_loss(run_loss(z, a, adv, old, ref, w, beta=0.05), want, z, a, adv, old, ref, 0.05)
+
+
+# ------------------------------------------------------------------- AdamW
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("top", [-1.0, 0.0, float("nan"), float("-inf"), float("inf")])
+def test_adamw_without_a_norm_has_no_clipping(bits, top):
+    sets = []
+    for _ in range(2):
+        ts = _tensors([5000, 41], bits, 12)
+        sets.append((ts,) + _params(ts, bits))
+    G.gnn_adamw_step(sets[0][1], 1e-3, 0.9, 0.999, 1e-8, 3, None, 1.0, 4)
+    G.gnn_adamw_step(sets[1][1], 1e-3, 0.9, 0.999, 1e-8, 3, None, top, 4)
+    torch.cuda.synchronize()
+    for x, y in zip(sets[0][0], sets[1][0]):
+        hx, hy = _host(x), _host(y)
+        for k in hx:
+            assert np.array_equal(hx[k], hy[k]), k
+        assert np.isfinite(hx["W"]).all()
