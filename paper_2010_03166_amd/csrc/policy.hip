@@ -191,7 +191,8 @@ __device__ inline bool row_terms(const PolicyArgs& a, const RowIn& r, double sum
   if (!r.chosen || sum == 0.0 || w == 0.0) return false;
   const double A = r.adv, x = lp - (double)r.old_lp;
   const double rho = !a.has_old ? (lp == lp ? 1.0 : lp) : EXACT ? exp_exact(x) : exp_quick(x);
-  const bool near = a.has_old && rho < INFINITY &&
+  // (a border at 0 cuts nothing, and a ratio that underflows is no nearer to it)
+  const bool near = a.has_old && rho > 0.0 && rho < INFINITY &&
                     (fabs(rho - a.lo) <= NEAR * rho || fabs(rho - a.hi) <= NEAR * rho);
   const double ra = rho * A, ca = fmin(fmax(rho, a.lo), a.hi) * A;
   const bool cut = ra > ca;  // false for a NaN, which then shows in ra

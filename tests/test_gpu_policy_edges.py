@@ -42,6 +42,21 @@ def test_masked_ranges_and_far_logits(n, C, top):
     check_loss(run_loss(z, a, adv, old, ref, w, beta=0.05), want, z, a, adv, old, ref, 0.05)
 
 
+# ------------------------------------------------------- borders of the clip
+
+@pytest.mark.parametrize("n,C", SHAPES)
+def test_ratio_of_zero_is_not_at_a_border(n, C):
+    """clip_lo = 1 puts the lower border at 0, where a ratio that underflows
+    lies: such rows are as those of a border that no ratio is near."""
+    z, a, adv, old, ref, w = _case(n, C, 40)
+    old = (P.action_logp(z, a)[0] + 800.0).astype(np.float32)
+    at = run_loss(z, a, adv, old, ref, w, lo=1.0, beta=0.05)
+    off = run_loss(z, a, adv, old, ref, w, lo=1.0 - 2.0 ** -20, beta=0.05)
+    assert np.array_equal(at["dZ"], off["dZ"]) and np.array_equal(at["logp"], off["logp"])
+    want = P.policy_loss(z, a, adv, old, ref, w, 1.0, 0.3, 0.05)
+    check_loss(at, want, z, a, adv, old, ref, 0.05)
+
+
 # ------------------------------------------------------------------- AdamW
 
 @pytest.mark.parametrize("bits", [32, 8])
