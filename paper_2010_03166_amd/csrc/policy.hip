@@ -153,6 +153,14 @@ __device__ inline double exp_quick(double x) {
   const float f = (float)x;
   return refined(exp_wide(f), x, f);
 }
+// The factor from a chunk's top to its row's: exp(x), x <= 0.  A chunk of
+// nothing but -inf has no top to come from, and x may be anything; its sum is
+// 0, and a factor of at most 1 leaves it 0.
+__device__ inline double exp_down(double x) {
+  x = fmin(x, 0.0);
+  const float f = (float)x;
+  return refined((double)expf(f), x, f);
+}
 // e^x - 1, and e^x - 1 - x, from the series x^2 (1/2 + x/6 + ...) where the
 // difference would lose digits (its first term left out is below 1e-7 of it).
 __device__ inline double expm1_quick(double x, double* less_x) {
@@ -565,9 +573,7 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   double sum = 0.0;
   for (int32_t k = lane; k < a.per_row; k += 64) {
     const Chunk c = at[k];
-    // a chunk of nothing but -inf has no top to come from: the factor of its
-    // sum of 0 would be infinite where the row's logits are far below 0
-    if (c.sum != 0.0) sum += c.sum * exp_quick((double)shift_of(c.top) - shift);
+    sum += c.sum * exp_down((double)shift_of(c.top) - shift);
   }
   sum = lanes_sum<64>(sum);
   const double lp = log_prob<false>(r, top, sum);
