@@ -53,6 +53,7 @@ struct PolicyArgs {
   int64_t ld_dz;
   Terms* part;    // one per block (split rows: one per row)
   Chunk* chunks;  // split rows: per_row for each row
+  double* exact;  // and, of the rows next to a border of the clip, their sums in doubles
   int32_t per_row;
   int64_t blocks, block0;  // of all launches, and in the launches before
 };
@@ -253,22 +254,22 @@ __device__ inline void store_terms(const PolicyArgs& a, const Terms& t) {
   else a.part[a.block0 + blockIdx.x] = t;
 }
 
-// Sum of exp(z - top) of one row in doubles, by a wavefront or by a block of T
-// threads (in all of them).
-__device__ inline double exact_part(const float* z, int32_t C, float top, int32_t at, int32_t step) {
+// Sum of exp(z - top) over columns in doubles, by a wavefront (of a row) or by
+// a block of T threads (of columns [from, to)), in all of the threads.
+__device__ inline double exact_part(const float* z, int32_t at, int32_t to, int32_t step, float top) {
   const double shift = shift_of(top);
   double sum = 0.0;
 #pragma unroll 1
-  for (int32_t j = at; j < C; j += step) sum += exp_exact((double)z[j] - shift);
+  for (int32_t j = at; j < to; j += step) sum += exp_exact((double)z[j] - shift);
   return lanes_sum<64>(sum);
 }
 __device__ inline double exact_sum(const float* z, int32_t C, float top) {
-  return exact_part(z, C, top, threadIdx.x & 63, 64);
+  return exact_part(z, threadIdx.x & 63, C, 64, top);
 }
 template <int T>
-__device__ inline double exact_sum_block(const float* z, int32_t C, float top) {
+__device__ inline double exact_sum_block(const float* z, int32_t from, int32_t to, float top) {
   __shared__ double s[T / 64];
-  const double part = exact_part(z, C, top, threadIdx.x, T);
+  const double part = exact_part(z, from + threadIdx.x, to, T, top);
   if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = part;
   __syncthreads();
   double sum = s[0];
@@ -472,7 +473,7 @@ __global__ __launch_bounds__(T, T == 1024 ? 8 : 1) void block_kernel(PolicyArgs 
   if (!LOSS) return;
   __syncthreads();
   if (s_near) {
-    sum = exact_sum_block<T>(row, a.C, top);
+    sum = exact_sum_block<T>(row, 0, a.C, top);
     if (t == 0) {
       row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &s_c);
       s_inv = 1.f / (float)sum;
@@ -503,15 +504,35 @@ __global__ __launch_bounds__(T, T == 1024 ? 8 : 1) void block_kernel(PolicyArgs 
 // launch for the chunks' sums, one that joins a row's sums, computes its
 // scalars in every block of the row alike, and writes the chunk's gradient
 // from a second reading (out of the caches, for the few rows that are so
-// long).  Blocks of 1,024 threads with up to 16 chunks a thread in registers
-// would take rows of up to 65,536 once: 600 x 40,000 56 us instead of 60, 500 x 65,536 66
-// instead of 82, but 1 x 65,536 13.3 instead of 9.9 and its log-probabilities
-// 9.7 instead of 5.3.  Chunks of 2,048 / 4,096 / 8,192: 64 x 131,071 28.3 /
-// 26.6 / 26.9 us, 1 x 131,071 9.4 / 10.4 / 12.5.
+// long), one that adds the rows' terms.  Where a row's ratio is next to a
+// border of the clip, the second launch forms its chunks' sums in doubles
+// instead of their gradients, and the third joins those and writes them: a
+// row of 2^22 columns takes 44 us more than one away from the border (with
+// each of its 1,024 blocks summing the whole row 6,800).  Blocks of 1,024
+// threads with up to 16 chunks a thread in registers would take rows of up to
+// 65,536 once: 600 x 40,000 56 us instead of 60, 500 x 65,536 66 instead of
+// 82, but 1 x 65,536 13.3 instead of 9.9 and its log-probabilities 9.7 instead
+// of 5.3.  Chunks of 2,048 / 4,096 / 8,192: 64 x 131,071 28.3 / 26.6 / 26.9
+// us, 1 x 131,071 9.4 / 10.4 / 12.5.
 constexpr int SPLIT_V = 4;
 constexpr int SPLIT_COLS = 4 * THREADS * SPLIT_V;
 __host__ __device__ inline int32_t chunks_of(int32_t C) {
   return (int32_t)ceil_div(C, SPLIT_COLS);
+}
+
+__device__ inline void split_load(const float* row, int32_t first, int32_t C, f4 (&z)[SPLIT_V]) {
+#pragma unroll
+  for (int k = 0; k < SPLIT_V; ++k) z[k] = load_cols(row, first + (k * THREADS + threadIdx.x) * 4, C);
+}
+// The gradient of the chunk at column `first` from its logits.
+__device__ inline void split_store(const PolicyArgs& a, int32_t i, int32_t first, f4 (&z)[SPLIT_V],
+                                   float shift, int32_t act, float c, float inv) {
+  float* to = a.dZ + (int64_t)i * a.ld_dz;
+#pragma unroll
+  for (int k = 0; k < SPLIT_V; ++k) {
+    const int32_t col = first + (k * THREADS + threadIdx.x) * 4;
+    store_cols(to, col, a.C, grad4(exp4(cut_cols(z[k], col, a.C), shift), col, act, c, inv));
+  }
 }
 
 __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
@@ -522,8 +543,7 @@ __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
   const int32_t i = (int32_t)(b / a.per_row), first = (int32_t)(b % a.per_row) * SPLIT_COLS;
   const float* row = a.Z + (int64_t)i * a.ld_z;
   f4 z[SPLIT_V];
-#pragma unroll
-  for (int k = 0; k < SPLIT_V; ++k) z[k] = load_cols(row, first + (k * THREADS + t) * 4, a.C);
+  split_load(row, first, a.C, z);
 #pragma unroll
   for (int k = 0; k < SPLIT_V; ++k) z[k] = cut_cols(z[k], first + (k * THREADS + t) * 4, a.C);
   float top = max4(z[0]);
@@ -549,20 +569,24 @@ __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
   }
 }
 
+// Terms that stand for a row that is left to the last launch, and add nothing.
+// No other row's third one is a negative zero: it is 0 or a weight that is not.
+constexpr Terms LEFT = {0.0, 0.0, -0.0};
+__device__ inline bool is_left(const Terms& t) {
+  return (uint64_t)__double_as_longlong(t.cut) == 1ull << 63;
+}
+
 // a.blocks blocks: those of a row's chunks, or one a row without a gradient.
 template <bool LOSS>
 __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   const int t = threadIdx.x, lane = t & 63;
   const int32_t todo = LOSS && a.dZ ? a.per_row : 1;
   const int64_t b = a.block0 + blockIdx.x;
-  const int32_t i = (int32_t)(b / todo), chunk = (int32_t)(b % todo);
+  const int32_t i = (int32_t)(b / todo), first = (int32_t)(b % todo) * SPLIT_COLS;
   const float* row = a.Z + (int64_t)i * a.ld_z;
   const int32_t act = a.action[i];
   f4 z[SPLIT_V];
-  if (LOSS && a.dZ)
-#pragma unroll
-    for (int k = 0; k < SPLIT_V; ++k)
-      z[k] = load_cols(row, chunk * SPLIT_COLS + (k * THREADS + t) * 4, a.C);
+  if (LOSS && a.dZ) split_load(row, first, a.C, z);
   const RowIn r = row_in(a, i, act, LOSS);
   // every wavefront joins the row's sums alike
   const Chunk* at = a.chunks + (int64_t)i * a.per_row;
@@ -577,35 +601,35 @@ __global__ __launch_bounds__(THREADS) void split_grad_kernel(PolicyArgs a) {
   }
   sum = lanes_sum<64>(sum);
   const double lp = log_prob<false>(r, top, sum);
-  if (t == 0 && chunk == 0 && a.logp) a.logp[i] = (float)lp;
+  const bool writer = t == 0 && first == 0;  // of what there is one of a row
+  if (writer && a.logp) a.logp[i] = (float)lp;
   if (!LOSS) return;
   Terms terms;
   float c;
-  if (row_terms<false>(a, r, sum, lp, &terms, &c)) {  // alike in all threads of a row
-    sum = exact_sum_block<THREADS>(row, a.C, top);
-    row_terms<true>(a, r, sum, log_prob<true>(r, top, sum), &terms, &c);
+  const bool near = row_terms<false>(a, r, sum, lp, &terms, &c);  // alike in all threads of a row
+  if (near) {
+    const double part =
+        exact_sum_block<THREADS>(row, first, a.dZ ? min(first + SPLIT_COLS, a.C) : a.C, top);
+    if (a.dZ) {  // left to split_final_kernel
+      if (t == 0) a.exact[b] = part;
+      terms = LEFT;
+    } else {
+      row_terms<true>(a, r, part, log_prob<true>(r, top, part), &terms, &c);
+    }
   }
-  if (t == 0 && chunk == 0) a.part[i] = terms;
-  if (!a.dZ) return;
-  const float inv = 1.f / (float)sum;
-  float* to = a.dZ + (int64_t)i * a.ld_dz;
-#pragma unroll
-  for (int k = 0; k < SPLIT_V; ++k) {
-    const int32_t col = chunk * SPLIT_COLS + (k * THREADS + t) * 4;
-    store_cols(to, col, a.C, grad4(exp4(cut_cols(z[k], col, a.C), shift), col, r.act, c, inv));
-  }
+  if (writer) a.part[i] = terms;
+  if (a.dZ && !near) split_store(a, i, first, z, shift, r.act, c, 1.f / (float)sum);
 }
 
-// One block: out = the sum of `count` partial terms.  More: each its share of
-// them, to `shares`.  In a fixed order either way.
-template <int T>
-__global__ __launch_bounds__(T) void policy_final_kernel(
-    int32_t count, const Terms* __restrict__ part, Terms* __restrict__ shares,
-    float* __restrict__ out) {
-  constexpr int AT_ONCE = 8;  // reads under way, each from another XCD's block
+constexpr int AT_ONCE = 8;  // reads under way, each from another XCD's block
+
+// The sum of terms first, first + step, ... of `count`; left: whether one of
+// them is that of a row left.
+__device__ inline Terms sum_terms(const Terms* __restrict__ part, int64_t first, int64_t step,
+                                  int32_t count, bool* left) {
   Terms t = {0.0, 0.0, 0.0};
-  const int64_t step = (int64_t)gridDim.x * T;
-  for (int64_t k = (int64_t)blockIdx.x * T + threadIdx.x; k < count; k += AT_ONCE * step) {
+  *left = false;
+  for (int64_t k = first; k < count; k += AT_ONCE * step) {
     Terms x[AT_ONCE];
 #pragma unroll
     for (int j = 0; j < AT_ONCE; ++j)
@@ -615,9 +639,92 @@ __global__ __launch_bounds__(T) void policy_final_kernel(
       t.loss += x[j].loss;
       t.kl += x[j].kl;
       t.cut += x[j].cut;
+      *left |= is_left(x[j]);
     }
   }
-  t = block_terms<T>(t);
+  return t;
+}
+
+// A row that the launch before left, from its chunks' sums in doubles: by 16
+// lanes, so that a block takes the terms of 16 rows at once.
+struct Left {
+  RowIn r;
+  float top, c, inv;
+  Terms terms;
+};
+__device__ inline Left left_row(const PolicyArgs& a, int32_t i) {
+  Left x;
+  x.r = row_in(a, i, a.action[i], true);
+  const int64_t at = (int64_t)i * a.per_row;
+  float top = -INFINITY;
+  double sum = 0.0;
+  for (int32_t k = threadIdx.x & 15; k < a.per_row; k += 16) {
+    top = fmaxf(top, a.chunks[at + k].top);
+    sum += a.exact[at + k];
+  }
+  x.top = lanes_max<16>(top);
+  sum = lanes_sum<16>(sum);
+  row_terms<true>(a, x.r, sum, log_prob<true>(x.r, x.top, sum), &x.terms, &x.c);
+  x.inv = 1.f / (float)sum;
+  return x;
+}
+
+// out = the sum of all rows' terms, by block 0, and the gradients of the rows
+// left, a chunk of one to a block in turn.
+__global__ __launch_bounds__(THREADS) void split_final_kernel(int32_t n, const Terms* part,
+                                                              float* out, PolicyArgs a) {
+  __shared__ int32_t s_left[THREADS / 64];
+  const int t = threadIdx.x, lane = t & 63;
+  bool left;
+  Terms all = sum_terms(part, t, THREADS, n, &left);
+  left = __any(left);
+  if (lane == 0) s_left[t >> 6] = left;
+  __syncthreads();
+  left = false;
+  for (int k = 0; k < THREADS / 64; ++k) left |= s_left[k] != 0;
+  if (left) {
+    const int32_t blocks = (int32_t)gridDim.x;
+    int32_t chunk0 = (int32_t)blockIdx.x;  // of the next such row, the block's first
+    for (int64_t i0 = 0; i0 < n; i0 += 64) {
+      uint64_t rows = __ballot(i0 + lane < n && is_left(part[min(i0 + lane, (int64_t)n - 1)]));
+      for (; rows; rows &= rows - 1) {
+        int32_t chunk = chunk0;
+        chunk0 -= a.per_row % blocks;
+        if (chunk0 < 0) chunk0 += blocks;
+        if (chunk >= a.per_row) continue;
+        const int32_t i = (int32_t)i0 + __ffsll((unsigned long long)rows) - 1;
+        const Left x = left_row(a, i);
+        for (; chunk < a.per_row; chunk += blocks) {
+          f4 z[SPLIT_V];
+          split_load(a.Z + (int64_t)i * a.ld_z, chunk * SPLIT_COLS, a.C, z);
+          split_store(a, i, chunk * SPLIT_COLS, z, shift_of(x.top), x.r.act, x.c, x.inv);
+        }
+      }
+    }
+    if (blockIdx.x == 0)
+      for (int64_t i = t / 16; i < n; i += THREADS / 16) {
+        if (!is_left(part[i])) continue;
+        const Terms terms = left_row(a, (int32_t)i).terms;
+        if (t % 16) continue;
+        all.loss += terms.loss;
+        all.kl += terms.kl;
+        all.cut += terms.cut;
+      }
+  }
+  if (blockIdx.x) return;
+  all = block_terms<THREADS>(all);
+  if (t == 0) store_out(out, all);
+}
+
+// One block: out = the sum of `count` partial terms.  More: each its share of
+// them, to `shares`.  In a fixed order either way.
+template <int T>
+__global__ __launch_bounds__(T) void policy_final_kernel(
+    int32_t count, const Terms* __restrict__ part, Terms* __restrict__ shares,
+    float* __restrict__ out) {
+  bool left;
+  const Terms t = block_terms<T>(sum_terms(part, (int64_t)blockIdx.x * T + threadIdx.x,
+                                           (int64_t)gridDim.x * T, count, &left));
   if (threadIdx.x) return;
   if (gridDim.x == 1) store_out(out, t);
   else shares[blockIdx.x] = t;
@@ -679,6 +786,9 @@ Launch choose(int32_t C) {
 // a call with one launch and with two: 7,500 terms 52.1 and 52.4, 16,384 terms
 // 56.2 and 54.3, 30,000 terms 58.5 and 53.3).
 constexpr int32_t FINAL_MOST = 8192, SHARES = 64;
+// Blocks of the last launch of split rows: for the rows next to a border of the
+// clip (adding the terms takes one).
+constexpr int64_t SPLIT_LAST = 256;
 // Blocks of one launch (2^32 threads are the most that a launch can have).
 constexpr int64_t LAUNCH_BLOCKS = 1 << 21;
 
@@ -686,17 +796,19 @@ int32_t parts_of(int32_t n, const Launch& l) {
   return l.rows ? (int32_t)ceil_div(n, l.rows_per_block) : n;
 }
 
-// [partial terms | shares of them | chunks' sums]
+// [partial terms | shares of them | chunks' sums | those in doubles]
 struct Layout {
-  size_t shares, chunks, total;
+  size_t shares, chunks, exact, total;
 };
 Layout layout_of(int32_t n, int32_t C, bool loss) {
   const Launch l = choose<true>(C);
   Layout o;
   const int32_t parts = loss ? parts_of(n, l) : 0;
   o.shares = round_up((size_t)parts * sizeof(Terms), 256);
-  o.chunks = o.shares + (parts > FINAL_MOST ? SHARES * sizeof(Terms) : 0);
-  o.total = o.chunks + (l.rows ? 0 : round_up((size_t)n * chunks_of(C) * sizeof(Chunk), 256));
+  o.chunks = o.shares + (l.rows && parts > FINAL_MOST ? SHARES * sizeof(Terms) : 0);
+  const size_t chunks = l.rows ? 0 : (size_t)n * chunks_of(C);
+  o.exact = o.chunks + round_up(chunks * sizeof(Chunk), 256);
+  o.total = o.exact + (loss ? round_up(chunks * sizeof(double), 256) : 0);
   return o;
 }
 
@@ -707,6 +819,7 @@ gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
   char* ws = static_cast<char*>(workspace);
   a.part = reinterpret_cast<Terms*>(ws);
   a.chunks = reinterpret_cast<Chunk*>(ws + o.chunks);
+  a.exact = reinterpret_cast<double*>(ws + o.exact);
   a.per_row = chunks_of(a.C);
   const auto run = [&](void (*kernel)(PolicyArgs), int32_t threads, int64_t blocks) {
     a.blocks = blocks;
@@ -715,13 +828,19 @@ gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
   };
   timer_begin(GNN_K_LOSS, stream);
   const int32_t parts = parts_of(a.n, l);
+  bool done = !LOSS;
   if (l.rows) {
     run(l.rows, l.threads, parts);
+    done |= parts == 1;  // (one block has written `out` itself)
   } else {
-    run(split_sums_kernel, THREADS, (int64_t)a.n * a.per_row);
-    run(split_grad_kernel<LOSS>, THREADS, LOSS && a.dZ ? (int64_t)a.n * a.per_row : a.n);
+    const int64_t chunks = (int64_t)a.n * a.per_row;
+    run(split_sums_kernel, THREADS, chunks);
+    run(split_grad_kernel<LOSS>, THREADS, LOSS && a.dZ ? chunks : a.n);
+    const unsigned last = a.dZ ? (unsigned)std::max<int64_t>(1, std::min(chunks, SPLIT_LAST)) : 1;
+    if (LOSS) split_final_kernel<<<last, THREADS, 0, stream>>>(a.n, a.part, a.out, a);
+    done = true;
   }
-  if (LOSS && !(l.rows && parts == 1)) {  // (one block of rows has written `out` itself)
+  if (!done) {
     Terms* shares = reinterpret_cast<Terms*>(ws + o.shares);
     const Terms* from = parts > FINAL_MOST ? shares : a.part;
     const int32_t count = parts > FINAL_MOST ? SHARES : parts;

@@ -57,6 +57,116 @@ def test_ratio_of_zero_is_not_at_a_border(n, C):
     check_loss(at, want, z, a, adv, old, ref, 0.05)
 
 
+def _near(n, C, seed, share=1.0):
+    """Rows whose ratios round to a border of clip = (0.2, 0.3)."""
+    z, a, adv, old, ref, w = _case(n, C, seed)
+    lp, _ = P.action_logp(z, a)
+    rng = np.random.default_rng([seed, 8])
+    side = np.where(rng.random(n) < 0.5, 0.8, 1.3)
+    pick = rng.random(n) < share
+    old = np.where(pick, lp - np.log(side), old).astype(np.float32)
+    return z, a, adv, old, ref, w
+
+
+def _ms(call):
+    """Least time of five calls."""
+    call()
+    best = np.inf
+    for _ in range(5):
+        x, y = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        x.record()
+        call()
+        y.record()
+        y.synchronize()
+        best = min(best, x.elapsed_time(y))
+    return best
+
+
+def test_row_at_a_border_costs_no_multiple_of_itself():
+    """One row of 2^22 logits with its ratio at the clip's border and away
+    from it: the sums in doubles are formed once, not by each of the row's
+    1,024 chunks (which took 200 times the call's time)."""
+    C = 1 << 22
+    g = torch.Generator(device="cuda").manual_seed(5)
+    Z = torch.randn((1, C), device="cuda", generator=g)
+    act = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    lp = torch.log_softmax(Z.double(), 1)[:, 77]
+    adv, w = torch.ones(1, device="cuda"), torch.ones(1, device="cuda")
+    dZ, out, logp = torch.empty_like(Z), torch.empty(3, device="cuda"), torch.empty(1, device="cuda")
+    ws = _ws(G.gnn_policy_workspace_bytes(1, C))
+    ms = {}
+    for name, ratio in (("away", 1.0), ("at", 1.3)):
+        old = (lp - np.log(ratio)).float()
+        ms[name] = _ms(lambda: G.gnn_policy_loss(1, C, Z, C, act, adv, old, old, w, 0.2, 0.3, 0.05,
+                                                 out, logp, dZ, C, ws))
+    print(ms)
+    assert ms["at"] < 10 * ms["away"] + 0.1
+
+
+@pytest.mark.parametrize("n,C", [(3, 40000), (70, 33000), (1, 131072), (600, 32770)])
+@pytest.mark.parametrize("share", [1.0, 0.3])
+def test_long_rows_at_a_border(n, C, share):
+    """Rows at and away from a border of the clip in one call: decided as in
+    doubles, with the gradients and sums of their side."""
+    z, a, adv, old, ref, w = _near(n, C, 41, share)
+    first = P.policy_loss(z, a, adv, old, ref, w, 0.2, 0.3, 0.05)
+    with np.errstate(divide="ignore"):
+        unsure = np.minimum(np.abs(first["rho"] - 0.8), np.abs(first["rho"] - 1.3)) < 1e-10
+    keep = np.where(unsure, -1, a)
+    assert unsure.mean() < 0.1 or n < 10
+    want = P.policy_loss(z, keep, adv, old, ref, w, 0.2, 0.3, 0.05)
+    r = run_loss(z, keep, adv, old, ref, w, beta=0.05, pad=C % 3, shift=1)
+    check_loss(r, want, z, keep, adv, old, ref, 0.05)
+    again = run_loss(z, keep, adv, old, ref, w, beta=0.05, pad=C % 3, shift=1)
+    no_dz = run_loss(z, keep, adv, old, ref, w, beta=0.05, want_dz=False)
+    for k in r:
+        assert np.array_equal(r[k], again[k]), k
+    check_loss(dict(r, out=no_dz["out"], logp=no_dz["logp"]), want, z, keep, adv, old, ref, 0.05)
+    # without the KL term a cut row has no gradient at all
+    r = run_loss(z, keep, adv, old, None, w)
+    cut = np.all(r["dZ"] == 0, axis=1)
+    assert np.array_equal(cut, want["cut"] | (keep < 0))
+
+
+def test_many_long_rows_at_a_border():
+    """More rows than one block adds up, a fifth of them at a border: the same
+    bits as in two calls of fewer rows."""
+    n, C, cut = 8300, 32769, 4100
+    _room(8 << 30)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    Z = torch.randn((n, C), device="cuda", generator=g)
+    act = torch.randint(0, C, (n,), device="cuda", generator=g, dtype=torch.int32)
+    adv, w = (torch.randn(n, device="cuda", generator=g) for _ in range(2))
+    w.abs_().div_(n)
+    lp = torch.cat([torch.log_softmax(z.double(), 1).gather(1, a[:, None].long())[:, 0]
+                    for z, a in zip(Z.split(1000), act.split(1000))])
+    pick = torch.rand(n, device="cuda", generator=g)
+    ratio = torch.where(pick < 0.1, 0.8, torch.where(pick < 0.2, 1.3, 1.0)).double()
+    old = (lp - torch.log(ratio)).float()
+    ws = _ws(G.gnn_policy_workspace_bytes(n, C))
+    dZ = torch.empty_like(Z)
+    res = []
+    for parts in ([(0, n)], [(0, cut), (cut, n)]):
+        ws.fill_(255)
+        dZ.fill_(7.0)
+        logp, outs = torch.empty(n, device="cuda"), []
+        for b, e in parts:
+            out = torch.empty(3, device="cuda")
+            G.gnn_policy_loss(e - b, C, Z[b:e], C, act[b:e], adv[b:e], old[b:e], None, w[b:e], 0.2,
+                              0.3, 0.0, out, logp[b:e], dZ[b:e], C, ws)
+            outs.append(out)
+        torch.cuda.synchronize()
+        none = (dZ == 0).all(1)
+        res.append((torch.stack(outs).double().sum(0), logp, none, dZ[::7].clone()))
+    assert bool(((res[0][0] - res[1][0]).abs() <= 4 * U * res[0][0].abs().clamp(min=1e-3)).all())
+    for x, y in zip(res[0][1:], res[1][1:]):
+        assert torch.equal(x, y)
+    rho = (lp - old.double()).exp()
+    want = rho * adv.double() > rho.clamp(0.8, 1.3) * adv.double()
+    sure = ((rho - 0.8).abs() > 1e-10) & ((rho - 1.3).abs() > 1e-10)
+    assert torch.equal(res[0][2][sure], want[sure]) and int(want.sum()) > 100
+
+
 # ------------------------------------------------------------------- AdamW
 
 @pytest.mark.parametrize("bits", [32, 8])
