@@ -393,8 +393,8 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
  * logits are not used (they may hold anything), its lp is written as 0 and
  * its gradient as 0.  Logits of -inf take an action out of a row's choice; a
  * row with every logit -inf is left out too, with lp = -inf.  Exponentials
- * are fp32's, added in fp32 within a few lanes and in double beyond: lp is off
- * by less than (20 + ln C) 2^-24 before its own rounding.
+ * are fp32's, at most 16 of them added in fp32 and all beyond in double: lp is
+ * off by less than (20 + ln C) 2^-24 before its own rounding.
  *
  * gnn_action_logp writes lp (n floats): what acting needs, and the old_logp /
  * ref_logp that gnn_policy_loss takes.

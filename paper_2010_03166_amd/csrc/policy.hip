@@ -88,12 +88,16 @@ __device__ inline RowIn row_in(const PolicyArgs& a, int32_t i, int32_t act, bool
   return r;
 }
 
-// Scalar functions.  Sums of fp32 exponentials are good to (20 + ln C) 2^-24
-// at worst, below 2.5e-6 for any C, so logarithms and exponentials as good as
-// 2e-7 lose little beside them, and library functions of doubles would hold a
-// hundred registers for their coefficients.  A row whose ratio is as near to
-// a border of the clip as those errors, one in 1e5 or so, is computed once
-// more in doubles.
+// Scalar functions.  What is fp32 in a row's logarithm, in steps u = 2^-24:
+// the exponentials, 4 u each (doubles would bound the kernels by instructions)
+// and ln C u, the weighted mean of their rounded arguments; the sum of at most
+// 16 of a lane, five additions deep, 5 u (all beyond in doubles); a chunk's
+// factor of a split row, 4 u; the sum's own rounding before its logarithm, u,
+// and that, 0.7 u.  Together below (20 + ln C) u, 2.2e-6 for any C, beside
+// which fp32 logarithms and ratios lose little, and library functions of
+// doubles would hold a hundred registers for their coefficients.  A row whose
+// ratio is as near to a border of the clip as those errors, one in 1e5 or so,
+// is computed once more in doubles.
 constexpr double NEAR = 4e-6;
 
 // exp(x) to a few 2^-53 for |x| < 700: 2^k times the remainder's series
@@ -374,7 +378,7 @@ __global__ __launch_bounds__(THREADS, 7) void rows_kernel(PolicyArgs a) {
     z[k] = exp4(z[k], shift);
     part += sum4(z[k]);
   }
-  double sum = lanes_sum<G>(part);
+  double sum = lanes_sum<G>((double)part);
   const double lp = log_prob<false>(r, top, sum);
   if (lane == 0 && mine && a.logp) a.logp[i] = (float)lp;
   if (!LOSS) return;
@@ -443,11 +447,16 @@ __global__ __launch_bounds__(T, T == 1024 ? 8 : 1) void block_kernel(PolicyArgs 
 #pragma unroll
   for (int k = 1; k < T / 64; ++k) top = fmaxf(top, s_top[k]);
   const float shift = shift_of(top);
-  float part = 0.f;
+  float some = 0.f;  // of at most four chunks
+  double part = 0.0;
 #pragma unroll
   for (int k = 0; k < V; ++k) {
     z[k] = exp4(z[k], shift);
-    part += sum4(z[k]);
+    some += sum4(z[k]);
+    if (k % 4 == 3 || k == V - 1) {
+      part += some;
+      some = 0.f;
+    }
     if (k >= KEPT) s_away[(k - KEPT) * T + t] = z[k];
   }
   part = lanes_sum<64>(part);
@@ -559,8 +568,8 @@ __global__ __launch_bounds__(THREADS) void split_sums_kernel(PolicyArgs a) {
   float part = 0.f;
 #pragma unroll
   for (int k = 0; k < SPLIT_V; ++k) part += sum4(exp4(z[k], shift));
-  part = lanes_sum<64>(part);
-  if ((t & 63) == 0) s_sum[wave] = part;
+  const double all = lanes_sum<64>((double)part);
+  if ((t & 63) == 0) s_sum[wave] = all;
   __syncthreads();
   if (t == 0) {
     double sum = 0.0;
