@@ -300,14 +300,15 @@ __device__ inline void piece32(const Tensor& t, int64_t base, float norm, const 
   }
   if (!(fabsf(norm) < INFINITY)) return;  // (asked here, when the reads are under way)
   const float keep = (float)(1.0 - a.lr * t.decay);
-  const float k = (float)clip_factor(a, norm), b1 = (float)a.b1, omb1 = (float)a.omb1;
+  const double k = clip_factor(a, norm);  // (1e-42, say, has 10 bits in fp32)
+  const float b1 = (float)a.b1, omb1 = (float)a.omb1;
   const float b2 = (float)a.b2, omb2 = (float)a.omb2;
 #pragma unroll
   for (int q = 0; q < AT_ONCE; ++q) {
     const int64_t i = base + (q * THREADS + threadIdx.x) * 4;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float g = x[q].g[j] * k;
+      const float g = (float)((double)x[q].g[j] * k);
       x[q].m[j] = b1 * x[q].m[j] + omb1 * g;
       x[q].v[j] = b2 * x[q].v[j] + omb2 * g * g;
       x[q].w[j] = updated(x[q].w[j], x[q].m[j], (double)x[q].v[j], keep, a);

@@ -184,3 +184,22 @@ def test_adamw_without_a_norm_has_no_clipping(bits, top):
         for k in hx:
             assert np.array_equal(hx[k], hy[k]), k
         assert np.isfinite(hx["W"]).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("size,top", [(1e30, 1.0), (1e36, 1e-3), (1e37, 1e-4), (1e-30, 1e-38)])
+def test_adamw_clipping_factors_at_the_ends(bits, size, top):
+    """Factors down to 1e-42, which fp32 holds with a few bits only."""
+    ts = _tensors([600], bits, 13, zero_state=True)
+    rng = np.random.default_rng(2)
+    g = (size * rng.uniform(0.5, 2.0, 600) * rng.choice([-1.0, 1.0], 600)).astype(np.float32)
+    ts[0]["G"][0].copy_(torch.from_numpy(g))
+    ps, decays = _params(ts, bits, decay=0.0)
+    norm = torch.zeros(1, device="cuda")
+    G.gnn_grad_norm(ps, norm, _ws(G.gnn_grad_norm_workspace_bytes(ps)))
+    n = float(norm)
+    assert np.isfinite(n) and n > top
+    before = [_host(x) for x in ts]
+    G.gnn_adamw_step(ps, 1e-3, 0.9, 0.999, 1e-12, 1, norm, top, 4)
+    torch.cuda.synchronize()
+    check_step(before, ts, bits, decays, 1e-3, 0.9, 0.999, 1e-12, 1, top / n, 4)
