@@ -472,9 +472,10 @@ typedef struct gnn_params {
 /* Bytes of the plan, and its filling (a device buffer of at least that size,
  * 16-byte aligned): a table of the tensors and of the pieces of 1,024
  * elements that one workgroup takes, so that one launch covers every tensor.
- * Nothing is read from the host after the call returns.  No W, m, v or scale
- * may overlap anything else in the set or the plan (GNN_ERR_ALIAS).
- * params->plan is not read. */
+ * Nothing is read from the host after the call returns; the plan itself, a
+ * table of addresses, is written on `stream`, and a call on another stream has
+ * to wait for that.  No W, m, v or scale may overlap anything else in the set
+ * or the plan (GNN_ERR_ALIAS).  params->plan is not read. */
 size_t gnn_params_plan_bytes(const gnn_params* params);
 gnn_status gnn_params_build_plan(const gnn_params* params, void* plan,
                                  size_t plan_bytes, hipStream_t stream);

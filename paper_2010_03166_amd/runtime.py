@@ -379,7 +379,10 @@ class ParamSet:
     """AdamW on a set of tensors, one launch a step: their moments (in 32
     bits, or in 8 with a scale for each 256 elements), the plan that lists
     them and the norm of their gradients.  Weights and gradients are
-    contiguous float32 tensors that stay where they are."""
+    contiguous float32 tensors that stay where they are.  The constructor
+    returns when moments and plan are written, so that the first step may be on
+    any stream; later steps on another stream than the last one's have to wait
+    for it, as for whatever writes the gradients."""
 
     def __init__(self, weights: Sequence[torch.Tensor], grads: Sequence[torch.Tensor],
                  weight_decay: Sequence[float], state_bits: int = 32):
@@ -415,6 +418,8 @@ class ParamSet:
         self.ws = torch.empty(max(G.gnn_grad_norm_workspace_bytes(self.params), 256),
                               dtype=torch.uint8, device=device)
         G.gnn_params_build_plan(self.params, self.plan)
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
 
     def grad_norm(self, stream=None) -> torch.Tensor:
         """Norm of all gradients (one float, on the device)."""

@@ -203,3 +203,31 @@ def test_adamw_clipping_factors_at_the_ends(bits, size, top):
     G.gnn_adamw_step(ps, 1e-3, 0.9, 0.999, 1e-12, 1, norm, top, 4)
     torch.cuda.synchronize()
     check_step(before, ts, bits, decays, 1e-3, 0.9, 0.999, 1e-12, 1, top / n, 4)
+
+
+# ----------------------------------------------------------------- streams
+
+def _busy(stream=None, times=30):
+    """Work of some tens of ms on a stream."""
+    with torch.cuda.stream(stream or torch.cuda.current_stream()):
+        x = torch.randn((4096, 4096), device="cuda")
+        for _ in range(times):
+            x = (x @ x).mul_(1e-3)
+    return x
+
+
+def test_param_set_is_ready_for_any_stream():
+    """The plan and the moments are there when the constructor returns: a
+    first step may be on a stream that does not wait for the present one."""
+    _busy(times=1)
+    torch.cuda.synchronize()
+    keep = _busy()
+    w = [torch.randn(5000, device="cuda"), torch.randn((30, 41), device="cuda")]
+    ps = runtime.ParamSet(w, [torch.ones_like(x) for x in w], [0.1, 0.0], 8)
+    assert torch.cuda.current_stream().query()
+    s = torch.cuda.Stream()
+    before = [x.clone() for x in w]
+    torch.cuda.synchronize()
+    ps.step(1, 1e-2, max_norm=1.0, stream=s)
+    s.synchronize()
+    assert all(not torch.equal(x, y) for x, y in zip(w, before)) and keep is not None
