@@ -371,6 +371,13 @@ class SageStack:
         return self.layers[0]["dX"] if want_dx_first else None
 
 
+def _stream_object(stream):
+    """torch's object of a stream argument (None: the current stream)."""
+    if stream is None:
+        return torch.cuda.current_stream()
+    return torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream
+
+
 def _on_current(t: torch.Tensor) -> bool:
     return t.is_cuda and t.get_device() == torch.cuda.current_device()
 
@@ -530,11 +537,13 @@ class Trainer:
                                    state_bits)
             self.state = self.params.state
         self.t = 0
-        # the policy's logits and their gradient, grown when first used
+        # the policy's logits, their gradient, log-probabilities and workspace,
+        # made when first used
         self._Z, self._dZ = _Rows(self.C, ld_p, device), _Rows(self.C, ld_p, device)
         self.policy_out = torch.zeros(3, device=device)
         self.logp = torch.empty(0, device=device)
         self.policy_ws = None
+        self._policy_streams = set()  # handles of the streams they were used on
 
     def bind(self, graph: DeviceGraph, rebind_stack: bool = True):
         """Moves the iteration to another prepared subgraph (weights and
@@ -583,16 +592,34 @@ class Trainer:
                              (name, self.n, dtype))
         return t
 
+    def _policy_buffers(self, stream):
+        """Makes the policy's buffers, if the present ones are too small, in the
+        memory of the stream that they are used on, and keeps their memory from
+        other use, once they are replaced, until every stream that used them
+        is done."""
+        n, C, f = self.n, self.C, self.f_top
+        need = max(G.gnn_policy_workspace_bytes(n, C), G.gnn_gemm_workspace_bytes(n, C, f),
+                   G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C), 256)
+        if self.policy_ws is None or self.policy_ws.numel() < need or self._Z.buf.shape[0] < n:
+            with torch.cuda.stream(_stream_object(stream)):
+                self._Z = _Rows(C, self._Z.ld, self.device)
+                self._dZ = _Rows(C, self._dZ.ld, self.device)
+                for rows in (self._Z, self._dZ):
+                    rows.view(n)
+                self.logp = torch.empty(n, device=self.device)
+                self.policy_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+            self._policy_streams.clear()
+        handle = G._stream(stream)
+        if handle not in self._policy_streams:
+            for t in (self._Z.buf, self._dZ.buf, self.logp, self.policy_ws):
+                t.record_stream(_stream_object(stream))
+            self._policy_streams.add(handle)
+
     def _logits(self, X: torch.Tensor, stream):
         """(X^(L), its row stride, logits Z = X^(L) W_MLP, their row stride)."""
         n, C, f = self.n, self.C, self.f_top
-        top, Z = self.stack.forward(X, stream), self._Z.view(self.n)
-        if self.logp.numel() < n:
-            self.logp = torch.empty(n, device=self.device)
-        self.policy_ws = _grown(self.policy_ws, max(
-            G.gnn_policy_workspace_bytes(n, C), G.gnn_gemm_workspace_bytes(n, C, f),
-            G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C)),
-            self.device)
+        self._policy_buffers(stream)
+        top, Z = self.stack.forward(X, stream), self._Z.view(n)
         ld_top = top.stride(0) if n else f
         G.gnn_gemm(False, False, n, C, f, top, ld_top, self.W_mlp, C, Z, self._Z.ld, self.flags,
                    self.policy_ws, stream)
@@ -601,10 +628,16 @@ class Trainer:
     def action_logp(self, X: torch.Tensor, actions: torch.Tensor, stream=None) -> torch.Tensor:
         """Log-probability of each row's action (n int32; outside [0, C): 0)
         under the present weights: a new tensor, to be kept as old_logp or
-        ref_logp."""
+        ref_logp.  stream: where all of it runs (the current one unless given);
+        what the call reads has to be ready there, and what it gives is."""
         self._per_row("actions", actions, torch.int32)
         _, _, Z, ld = self._logits(X, stream)
-        logp = torch.empty(self.n, device=self.device)
+        if stream is None:
+            logp = torch.empty(self.n, device=self.device)
+        else:
+            with torch.cuda.stream(_stream_object(stream)):
+                logp = torch.empty(self.n, device=self.device)
+            logp.record_stream(torch.cuda.current_stream())
         G.gnn_action_logp(self.n, self.C, Z, ld, actions, logp, self.policy_ws, stream)
         return logp
 
@@ -618,7 +651,8 @@ class Trainer:
         (n int32; outside [0, C): the row is left out), advantage, old_logp
         (None: on-policy), ref_logp (with beta), weight (None: 1/n).  Returns
         three floats on the device: loss, KL and clipped share (weighted sums);
-        the rows' log-probabilities are in `logp`."""
+        the rows' log-probabilities are in `logp`.  stream: as in
+        action_logp."""
         for name, t in (("advantage", advantage), ("old_logp", old_logp),
                         ("ref_logp", ref_logp), ("weight", weight)):
             self._per_row(name, t)

@@ -8,8 +8,9 @@ import torch
 
 from oracle import policy as P
 from paper_2010_03166_amd import gnnprop as G
-from paper_2010_03166_amd import runtime
+from paper_2010_03166_amd import runtime, synth
 
+from gpu_helpers import prepared, to_dev
 from test_gpu_policy import (SHAPES, U, _case, _f, _host, _params, _room, _tensors, _trainer, _ws,
                              check_logp, check_loss, check_step, run_logp, run_loss)
 
@@ -231,3 +232,48 @@ def test_param_set_is_ready_for_any_stream():
     ps.step(1, 1e-2, max_norm=1.0, stream=s)
     s.synchronize()
     assert all(not torch.equal(x, y) for x, y in zip(w, before)) and keep is not None
+
+
+def test_trainer_allocates_on_the_stream_it_works_on():
+    """With stream= the tensors that a call makes come from that stream's
+    memory: not from a block that the present stream freed a moment ago and
+    may still be writing."""
+    tr, d, _, X, _ = _trainer("sgd", lr=0.0)
+    act = torch.zeros(tr.n, dtype=torch.int32, device="cuda")
+    want = tr.action_logp(X, act)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    freed = [torch.empty(tr.n, device="cuda") for _ in range(4)]
+    at = {x.data_ptr() for x in freed}
+    del freed
+    for stream in (s, s.cuda_stream):
+        lp = tr.action_logp(X, act, stream=stream)
+        assert lp.data_ptr() not in at
+        s.synchronize()
+        assert torch.equal(lp, want)
+
+
+def test_trainer_buffers_outlive_the_streams_that_use_them():
+    """Buffers that a larger subgraph replaces while another stream still
+    works in them are not handed out again before it is done."""
+    small, large = (prepared(synth.power_law_graph(k, 2.1, 8.0, seed=k)) for k in (900, 2000))
+    rng = np.random.default_rng(0)
+    f, h, C = 24, 16, 700
+    params = [synth.LayerParams(synth.glorot(f, h, rng), synth.glorot(f, h, rng))]
+    tr = runtime.Trainer(small, params, f, synth.glorot(2 * h, C, rng), False, "sgd", lr=0.0)
+    X = to_dev(rng.standard_normal((2000, f)).astype(np.float32), 32)
+    act = torch.zeros(2000, dtype=torch.int32, device="cuda")
+    tr.action_logp(X[:900], act[:900])  # made in the current stream's memory
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    keep = _busy(s, 100)
+    tr.action_logp(X[:900], act[:900], stream=s)
+    size = tr._Z.buf.numel()
+    old = {t.data_ptr() for t in (tr._Z.buf, tr._dZ.buf)}
+    tr.bind(large)
+    tr.action_logp(X, act)  # replaces them
+    more = [torch.empty(size, device="cuda") for _ in range(8)] + [tr._Z.buf, tr._dZ.buf]
+    if not s.query():  # (else they may well be)
+        assert not old & {t.data_ptr() for t in more}
+    torch.cuda.synchronize()
+    del keep
