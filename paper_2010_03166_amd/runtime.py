@@ -541,7 +541,7 @@ class Trainer:
         # made when first used
         self._Z, self._dZ = _Rows(self.C, ld_p, device), _Rows(self.C, ld_p, device)
         self.policy_out = torch.zeros(3, device=device)
-        self.logp = torch.empty(0, device=device)
+        self.logp = self._logp = torch.empty(0, device=device)
         self.policy_ws = None
         self._policy_streams = set()  # handles of the streams they were used on
 
@@ -606,12 +606,12 @@ class Trainer:
                 self._dZ = _Rows(C, self._dZ.ld, self.device)
                 for rows in (self._Z, self._dZ):
                     rows.view(n)
-                self.logp = torch.empty(n, device=self.device)
+                self._logp = torch.empty(n, device=self.device)
                 self.policy_ws = torch.empty(need, dtype=torch.uint8, device=self.device)
             self._policy_streams.clear()
         handle = G._stream(stream)
         if handle not in self._policy_streams:
-            for t in (self._Z.buf, self._dZ.buf, self.logp, self.policy_ws):
+            for t in (self._Z.buf, self._dZ.buf, self._logp, self.policy_ws):
                 t.record_stream(_stream_object(stream))
             self._policy_streams.add(handle)
 
@@ -651,7 +651,7 @@ class Trainer:
         (n int32; outside [0, C): the row is left out), advantage, old_logp
         (None: on-policy), ref_logp (with beta), weight (None: 1/n).  Returns
         three floats on the device: loss, KL and clipped share (weighted sums);
-        the rows' log-probabilities are in `logp`.  stream: as in
+        the n rows' log-probabilities are in `logp`.  stream: as in
         action_logp."""
         for name, t in (("advantage", advantage), ("old_logp", old_logp),
                         ("ref_logp", ref_logp), ("weight", weight)):
@@ -659,7 +659,7 @@ class Trainer:
         self._per_row("actions", actions, torch.int32)
         n, C, f = self.n, self.C, self.f_top
         top, ld_top, Z, ld = self._logits(X, stream)
-        dZ = self._dZ.view(n)
+        dZ, self.logp = self._dZ.view(n), self._logp[:n]
         G.gnn_policy_loss(n, C, Z, ld, actions, advantage, old_logp, ref_logp, weight, clip[0],
                           clip[1], beta, self.policy_out, self.logp, dZ, ld, self.policy_ws,
                           stream)

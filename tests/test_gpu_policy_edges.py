@@ -277,3 +277,20 @@ def test_trainer_buffers_outlive_the_streams_that_use_them():
         assert not old & {t.data_ptr() for t in more}
     torch.cuda.synchronize()
     del keep
+
+
+def test_trainer_logp_is_of_the_present_rows():
+    """`logp` after a step has the present subgraph's rows, whatever subgraphs
+    the trainer was on before."""
+    graphs = [prepared(synth.power_law_graph(k, 2.1, 8.0, seed=k)) for k in (900, 300)]
+    rng = np.random.default_rng(0)
+    f, h, C = 24, 16, 5
+    params = [synth.LayerParams(synth.glorot(f, h, rng), synth.glorot(f, h, rng))]
+    tr = runtime.Trainer(graphs[0], params, f, synth.glorot(2 * h, C, rng), False, "sgd", lr=0.0)
+    for g in graphs:
+        tr.bind(g)
+        X = to_dev(rng.standard_normal((g.n, f)).astype(np.float32), 32)
+        act = torch.from_numpy(rng.integers(0, C, g.n).astype(np.int32)).cuda()
+        tr.policy_step(X, act, torch.ones(g.n, device="cuda"))
+        assert tr.logp.shape == (g.n,)
+        assert torch.equal(tr.logp, tr.action_logp(X, act))
