@@ -168,6 +168,39 @@ def test_many_long_rows_at_a_border():
     assert torch.equal(res[0][2][sure], want[sure]) and int(want.sum()) > 100
 
 
+@pytest.mark.parametrize("n,C", [(300, 9), (40, 700), (6, 20000), (70, 33000)])
+def test_captured_away_from_borders_and_replayed_at_them(n, C):
+    """Which rows are at a border is decided on the device: a call captured
+    with none of them there, replayed with some, with all and with none, gives
+    an eager call's bits."""
+    z, a, adv, away, ref, w = _case(n, C, 42)
+    at = [_near(n, C, 42, share)[3] for share in (0.0, 0.4, 1.0, 0.0, 1.0)]
+    Z, act = to_dev(z), torch.from_numpy(a.astype(np.int32)).cuda()
+    A, o, rf, ww = _f(adv), _f(away), _f(ref), _f(w)
+    bufs = [[torch.zeros(3, device="cuda"), torch.zeros(n, device="cuda"),
+             torch.zeros((n, C), device="cuda"), _ws(G.gnn_policy_workspace_bytes(n, C))]
+            for _ in range(2)]
+
+    def call(b, stream=None):
+        G.gnn_policy_loss(n, C, Z, C, act, A, o, rf, ww, 0.2, 0.3, 0.05, b[0], b[1], b[2], C, b[3],
+                          stream)
+
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        call(bufs[0], s.cuda_stream)
+    for old in at:
+        o.copy_(_f(old))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        call(bufs[1])
+        torch.cuda.synchronize()
+        for x, y in zip(bufs[0][:3], bufs[1][:3]):
+            assert torch.equal(x, y)
+
+
 # ------------------------------------------------------------------- AdamW
 
 @pytest.mark.parametrize("bits", [32, 8])
@@ -204,6 +237,66 @@ def test_adamw_clipping_factors_at_the_ends(bits, size, top):
     G.gnn_adamw_step(ps, 1e-3, 0.9, 0.999, 1e-12, 1, norm, top, 4)
     torch.cuda.synchronize()
     check_step(before, ts, bits, decays, 1e-3, 0.9, 0.999, 1e-12, 1, top / n, 4)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("size", [2.0 ** -100, 1e-24, 1e-19, 1e-12, 1e-4])
+def test_adamw_tiny_gradients_from_weights_of_zero(bits, size):
+    """The update alone (weights 0, no decay), so that it is seen to its own
+    last bits.  Roundings, u each: m 5 of its size, v 8 of v and with 32-bit
+    moments half a step of 2^-149 for each of its three operations, which the
+    root carries into the update's bounds; 14 for the update's own."""
+    ts = _tensors([1000, 41], bits, 14, zero_state=True)
+    rng = np.random.default_rng(3)
+    for t in ts:
+        c = t["W"][0].numel()
+        t["W"][0].zero_()
+        t["G"][0].copy_(torch.from_numpy((size * rng.uniform(0.5, 2.0, c) *
+                                          rng.choice([-1.0, 1.0], c)).astype(np.float32)))
+    ps, _ = _params(ts, bits, decay=0.0)
+    before = [_host(x) for x in ts]
+    lr, b1, b2, eps = 1e-3, 0.9, 0.999, 0.1 * size
+    G.gnn_adamw_step(ps, lr, b1, b2, eps, 1, seed=8)
+    torch.cuda.synchronize()
+    for h, x in zip(before, ts):
+        _, m, v = P.adamw(h["W"], h["G"], 0 * h["W"], 0 * h["W"], lr, b1, b2, eps, 1, 0.0)
+        verr = 8 * U * v + (1.5 * 2.0 ** -149 if bits == 32 else 0.0)
+        now = -_host(x)["W"].astype(np.float64) * np.sign(m)
+        for err, side in ((verr, -1), (-verr, 1)):
+            den = np.sqrt(np.maximum(v + err, 0) / (1 - b2)) + eps
+            bound = lr * np.abs(m) / (1 - b1) / den
+            assert np.all(side * (now - bound) <= 20 * U * bound)
+
+
+def test_adamw8_neighbours_of_a_broken_block():
+    """A NaN and an infinity break their own blocks of 256; every other block,
+    in the same tensor and in others, is as if they were not there."""
+    ts = _tensors([256 * 6 + 100, 300], 8, 15)
+    ps, decays = _params(ts, 8)
+    sound = [_host(x) for x in ts]
+    ts[0]["G"][0][256 + 7] = float("nan")
+    ts[0]["G"][0][256 * 4 + 255] = float("inf")
+    G.gnn_adamw_step(ps, 1e-3, 0.9, 0.999, 1e-8, 3, seed=5)
+    torch.cuda.synchronize()
+    now = [_host(x) for x in ts]
+    other = _tensors([256 * 6 + 100, 300], 8, 15)
+    ps2, _ = _params(other, 8)
+    G.gnn_adamw_step(ps2, 1e-3, 0.9, 0.999, 1e-8, 3, seed=5)
+    torch.cuda.synchronize()
+    check_step(sound, other, 8, decays, 1e-3, 0.9, 0.999, 1e-8, 3, 1.0, 5)
+    want = [_host(x) for x in other]
+    broken = [1, 4]
+    fine = np.repeat([b not in broken for b in range(7)], 256)[: 256 * 6 + 100]
+    for k in ("W", "m", "v"):
+        assert np.array_equal(now[0][k][fine], want[0][k][fine]), k
+        assert np.array_equal(now[1][k], want[1][k]), k
+    for k in ("m_scale", "v_scale"):
+        ok = np.array([b not in broken for b in range(7)])
+        assert np.array_equal(now[0][k][ok], want[0][k][ok]) and np.isnan(now[0][k][~ok]).all()
+    at = np.zeros(256 * 6 + 100, bool)
+    at[[256 + 7, 256 * 4 + 255]] = True
+    assert np.array_equal(now[0]["W"][~at], want[0]["W"][~at])
+    assert not np.isfinite(now[0]["W"][at]).any()
 
 
 # ----------------------------------------------------------------- streams
@@ -251,6 +344,7 @@ def test_trainer_allocates_on_the_stream_it_works_on():
         assert lp.data_ptr() not in at
         s.synchronize()
         assert torch.equal(lp, want)
+    assert torch.equal(tr.action_logp(X, act, stream=0), want)  # the default stream
 
 
 def test_trainer_buffers_outlive_the_streams_that_use_them():
