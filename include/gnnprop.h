@@ -396,8 +396,8 @@ gnn_status gnn_adam_step(int64_t count, float* W, const float* G, float* m,
  * are fp32's, at most 16 of them added in fp32 and all beyond in double: lp is
  * off by less than (20 + ln C) 2^-24 before its own rounding.
  *
- * gnn_action_logp writes lp (n floats): what acting needs, and the old_logp /
- * ref_logp that gnn_policy_loss takes.
+ * gnn_action_logp writes lp (n floats): the old_logp / ref_logp that
+ * gnn_policy_loss takes, of actions that were drawn from the logits.
  *
  * gnn_policy_loss: the clipped surrogate loss with a KL term, and its
  * gradient, with
@@ -491,9 +491,13 @@ gnn_status gnn_grad_norm(const gnn_params* params, float* norm, void* workspace,
  *   W = (1 - lr weight_decay) W
  *       - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
  * norm: device float (gnn_grad_norm's) or NULL.  NULL: k = 1, whatever
- * max_norm.  Else
- * k = max_norm / norm where norm > max_norm (max_norm > 0) and 1 elsewhere,
- * and a norm that is not finite skips the step: nothing is changed.
+ * max_norm.  Else k = max_norm / norm where norm > max_norm (max_norm > 0) and
+ * 1 elsewhere, and a norm that is not finite skips the step: nothing is
+ * changed.  t is the caller's count: one that goes on over a skipped step has
+ * bias corrections for a step more than the moments hold, so that the updates
+ * after it are smaller than they might be (by (1 - b1) / (1 - b1^2) over the
+ * root of the same of b2, 0.74 for 0.9 and 0.999, where the first step of all
+ * is skipped; less and less later).
  * Without norm a NaN or infinite gradient makes its own weight and moments
  * non-finite, with 8-bit moments those of its whole block of 256 (so does one
  * whose square passes 1e43).

@@ -6,8 +6,8 @@
 // moments, plus 16 bytes for each block of 256).  The plan in device memory
 // lists the set's pieces of PIECE elements, so that one launch, one workgroup
 // a piece, covers tensors of any number and size.  Measured on 120 million
-// weights: norm 78 us (6.1 TB/s), update 616 us (5.5 TB/s; a large copy 5.05)
-// and with 8-bit moments 367 us (5.3 TB/s); on 1.7 million 7.8 and 8.9 us,
+// weights: norm 78 us (6.2 TB/s), update 613 us (5.5 TB/s; a large copy 5.05)
+// and with 8-bit moments 360 us (5.4 TB/s); on 1.7 million 7.8 and 8.9 us,
 // launches (the norm takes two) and their latency.  Pieces of 2,048: 86, 637
 // and 399 us where 1,024 take 82, 630 and 400; blocks of 128 threads 119 us
 // for the norm.
@@ -323,7 +323,9 @@ __device__ inline void piece32(const Tensor& t, int64_t base, float norm, const 
 // scale is a reduction within the wavefront.  Instructions bound this path
 // until they are few: about 90 a weight, 15 of them of doubles (as fast here
 // as fp32 ones); with library roots, quotients and ldexp 210, and 666 us in
-// the place of 367.
+// the place of 360.  Small sets are bound by latency: a block's reads follow
+// two reads of the plan, the piece's and then its tensor's (0.9 million
+// weights, a single round of blocks: 6.2 us, their bytes 2.8).
 template <bool FULL>
 __device__ inline void piece8(const Tensor& t, int64_t base, float norm, const Coef& a) {
   uint8_t *m = static_cast<uint8_t*>(t.m), *v = static_cast<uint8_t*>(t.v);

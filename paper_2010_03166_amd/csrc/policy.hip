@@ -11,11 +11,13 @@
 // are under way before the first is waited for.  Only rows past 32,768 columns
 // are read twice.  Measured, us a call (and what of it are the final sums, a
 // launch of their own unless one block has all rows):
-//   50,001 x 121, rows off alignment   15.0 (2.5)   3.3 TB/s
-//   16,384 x 2,048                     53.3 (4)     5.0 TB/s, a large copy 5.05
-//   64 x 131,071                       23.1 (2.5)   2.9 TB/s
-//   2,000 x 20,011, log-probabilities  30.2         5.3 TB/s
+//   50,001 x 121, rows off alignment   14.8 (2.5)   3.3 TB/s
+//   16,384 x 2,048                     52.8 (4)     5.1 TB/s, a large copy 5.05
+//   64 x 131,071                       23.5 (2.5)   2.9 TB/s
+//   2,000 x 20,011, log-probabilities  29.1         5.5 TB/s
 // What the same accesses take with nothing computed: 10.6 us for the first.
+// Up to 16 columns a lane has a row of its own, and its accesses are scattered:
+// 200,000 x 7 9.3 us, 200,000 x 16 12.5, where the bytes take 3.2 and 6.0.
 // Stores past the caches (non-temporal) take 3 to 15 % off the rows of whole
 // cache lines, but the product that reads dZ next loses more than that.
 #include <cmath>
@@ -517,7 +519,8 @@ __global__ __launch_bounds__(T, T == 1024 ? 8 : 1) void block_kernel(PolicyArgs 
 // border of the clip, the second launch forms its chunks' sums in doubles
 // instead of their gradients, and the third joins those and writes them: a
 // row of 2^22 columns takes 44 us more than one away from the border (with
-// each of its 1,024 blocks summing the whole row 6,800).  Blocks of 1,024
+// each of its 1,024 blocks summing the whole row 6,800), 64 x 131,071 with
+// every row there 68 us (443).  Blocks of 1,024
 // threads with up to 16 chunks a thread in registers would take rows of up to
 // 65,536 once: 600 x 40,000 56 us instead of 60, 500 x 65,536 66 instead of
 // 82, but 1 x 65,536 13.3 instead of 9.9 and its log-probabilities 9.7 instead

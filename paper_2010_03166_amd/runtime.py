@@ -437,7 +437,8 @@ class ParamSet:
              max_norm: Optional[float] = None, seed: int = 0, stream=None):
         """AdamW step t (from 1).  With max_norm the gradients are scaled down
         to that norm where theirs is larger, and a step whose norm is not
-        finite changes nothing.  seed: of the 8-bit moments' rounding."""
+        finite changes nothing (the device decides that: to count only steps
+        that were taken, read `norm`).  seed: of the 8-bit moments' rounding."""
         norm = self.grad_norm(stream) if max_norm is not None else None
         G.gnn_adamw_step(self.params, lr, betas[0], betas[1], eps, t, norm,
                          max_norm if max_norm is not None else 1.0, seed, stream)
@@ -465,7 +466,8 @@ class Trainer:
         With optimizer "adamw": weight_decay (0.01 unless given) of the weight
         matrices (biases do not decay), max_norm to clip the norm of all
         gradients, state_bits 8 for moments of one byte and the seed of their
-        rounding."""
+        rounding.  `t` counts the iterations, those too that change nothing
+        because their gradients' norm is not finite."""
         if optimizer not in ("sgd", "adam", "adamw"):
             raise ValueError("optimizer must be 'sgd', 'adam' or 'adamw'")
         if optimizer != "adamw" and (weight_decay is not None or max_norm is not None or
