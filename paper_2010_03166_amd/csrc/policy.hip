@@ -683,12 +683,11 @@ __device__ inline Left left_row(const PolicyArgs& a, int32_t i) {
 
 // out = the sum of all rows' terms, by block 0, and the gradients of the rows
 // left, a chunk of one to a block in turn.
-__global__ __launch_bounds__(THREADS) void split_final_kernel(int32_t n, const Terms* part,
-                                                              float* out, PolicyArgs a) {
+__global__ __launch_bounds__(THREADS) void split_final_kernel(PolicyArgs a) {
   __shared__ int32_t s_left[THREADS / 64];
   const int t = threadIdx.x, lane = t & 63;
   bool left;
-  Terms all = sum_terms(part, t, THREADS, n, &left);
+  Terms all = sum_terms(a.part, t, THREADS, a.n, &left);
   left = __any(left);
   if (lane == 0) s_left[t >> 6] = left;
   __syncthreads();
@@ -697,8 +696,8 @@ __global__ __launch_bounds__(THREADS) void split_final_kernel(int32_t n, const T
   if (left) {
     const int32_t blocks = (int32_t)gridDim.x;
     int32_t chunk0 = (int32_t)blockIdx.x;  // of the next such row, the block's first
-    for (int64_t i0 = 0; i0 < n; i0 += 64) {
-      uint64_t rows = __ballot(i0 + lane < n && is_left(part[min(i0 + lane, (int64_t)n - 1)]));
+    for (int64_t i0 = 0; i0 < a.n; i0 += 64) {
+      uint64_t rows = __ballot(i0 + lane < a.n && is_left(a.part[min(i0 + lane, (int64_t)a.n - 1)]));
       for (; rows; rows &= rows - 1) {
         int32_t chunk = chunk0;
         chunk0 -= a.per_row % blocks;
@@ -714,8 +713,8 @@ __global__ __launch_bounds__(THREADS) void split_final_kernel(int32_t n, const T
       }
     }
     if (blockIdx.x == 0)
-      for (int64_t i = t / 16; i < n; i += THREADS / 16) {
-        if (!is_left(part[i])) continue;
+      for (int64_t i = t / 16; i < a.n; i += THREADS / 16) {
+        if (!is_left(a.part[i])) continue;
         const Terms terms = left_row(a, (int32_t)i).terms;
         if (t % 16) continue;
         all.loss += terms.loss;
@@ -725,7 +724,7 @@ __global__ __launch_bounds__(THREADS) void split_final_kernel(int32_t n, const T
   }
   if (blockIdx.x) return;
   all = block_terms<THREADS>(all);
-  if (t == 0) store_out(out, all);
+  if (t == 0) store_out(a.out, all);
 }
 
 // One block: out = the sum of `count` partial terms.  More: each its share of
@@ -849,7 +848,7 @@ gnn_status launch(PolicyArgs a, void* workspace, hipStream_t stream) {
     run(split_sums_kernel, THREADS, chunks);
     run(split_grad_kernel<LOSS>, THREADS, LOSS && a.dZ ? chunks : a.n);
     const unsigned last = a.dZ ? (unsigned)std::max<int64_t>(1, std::min(chunks, SPLIT_LAST)) : 1;
-    if (LOSS) split_final_kernel<<<last, THREADS, 0, stream>>>(a.n, a.part, a.out, a);
+    if (LOSS) split_final_kernel<<<last, THREADS, 0, stream>>>(a);
     done = true;
   }
   if (!done) {

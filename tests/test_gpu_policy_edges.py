@@ -388,3 +388,41 @@ def test_trainer_logp_is_of_the_present_rows():
         tr.policy_step(X, act, torch.ones(g.n, device="cuda"))
         assert tr.logp.shape == (g.n,)
         assert torch.equal(tr.logp, tr.action_logp(X, act))
+
+
+def test_trainer_captured_on_a_stream_that_it_was_not_on():
+    """Buffers made on the current stream, then acting and a step captured on
+    another one and replayed between eager iterations of a second trainer."""
+    cap, d, _, X, _ = _trainer("sgd", lr=1e-3)
+    eager, _, _, _, _ = _trainer("sgd", lr=1e-3)
+    n = cap.n
+    act = torch.arange(n, device="cuda", dtype=torch.int32) % cap.C
+    adv = torch.randn(n, device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    cap.action_logp(X, act)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        old = cap.action_logp(X, act, stream=s.cuda_stream)
+        cap.policy_step(X, act, adv, old, old, beta=0.1, stream=s.cuda_stream)
+    for it in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        want = eager.action_logp(X, act)
+        eager.policy_step(X, act, adv, want, want, beta=0.1)
+        torch.cuda.synchronize()
+        assert torch.equal(old, want) and torch.equal(cap.policy_out, eager.policy_out), it
+        assert torch.equal(cap.logp, eager.logp)
+        for (w, _), (v, _) in zip(cap.pairs, eager.pairs):
+            assert torch.equal(w, v), it
+
+
+@pytest.mark.parametrize("C", [5, 700, 20000, 70000])
+def test_policy_of_no_rows_at_every_width(C):
+    out, dZ = torch.full((3,), 7.0, device="cuda"), torch.full((C,), 7.0, device="cuda")
+    for d in (None, dZ):
+        out.fill_(7.0)
+        G.gnn_policy_loss(0, C, None, C, None, None, None, None, None, 0.2, 0.2, 0.0, out, None, d,
+                          C, None)
+        torch.cuda.synchronize()
+        assert torch.all(out == 0) and torch.all(dZ == 7.0)
