@@ -434,6 +434,82 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
                            int64_t ld_dz, void* workspace, size_t workspace_bytes,
                            hipStream_t stream);
 
+/* Acting, and teaching one network by another.  Rows of logits Z (n x C,
+ * stride ld_z) as above; the order of a row's entries is: larger logits first,
+ * equal ones (0 and -0 are) by their columns.  Logits of -inf are not there.  A
+ * row whose largest logit is not a finite number, or with a NaN among them, is
+ * left out.  1 <= C <= 2^24; temperatures T are 0 or 1e-6 to 1e6 (else
+ * GNN_ERR_SHAPE).
+ *
+ * gnn_sample_actions: each row draws an action by its random number u.  With
+ *   e_j = exp((Z[i, j] - top) / T),  top the row's largest logit,
+ * it keeps the shortest of these beginnings of the row's order:
+ *   the first top_k                                     (0 or >= C: all)
+ *   the shortest whose sum of e reaches top_p times that of the first top_k
+ *                                                       (0 < top_p <= 1)
+ *   those with Z[i, j] - top >= T ln(min_p)             (0 <= min_p <= 1)
+ * and the action is the first of the kept entries, by columns, with which the
+ * sum of their e passes u times the sum of all kept.  T = 0: the first entry
+ * of the order, whatever the rest (u may be NULL).  Weights e are whole
+ * multiples of 2^-51 (of 2^(log C - 62) where C > 2048, log C rounded up), each
+ * off by less than 1e-13 and half a multiple; nothing else is rounded but
+ * top_p's product and log min_p, in double, so that an action does not depend
+ * on how a sum is formed, and equal logits are equally likely.
+ * u: n floats in [0, 1) (those below or NaN count as 0, those above as the
+ * last number below 1).  action: n int32, -1 for rows left out.  logp (n
+ * floats, may be NULL): the actions' log-probabilities under Z itself (T = 1,
+ * nothing cut off), as gnn_action_logp gives them, 0 for rows left out: the
+ * old_logp of gnn_policy_loss.  Workspace: gnn_sample_workspace_bytes.
+ *
+ * gnn_top_logits: the first k entries of each row's order (1 <= k <=
+ * GNN_TOP_MOST), with T > 0:
+ *   index[i, r]  their columns (n x k int32, contiguous)
+ *   logq[i, r] = Z[i, index] / T - log sum_j exp(Z[i, j] / T)     (n x k)
+ *   rest[i]    = the share of all other entries                   (n, may be NULL)
+ * Places past a row's entries, and rows left out, hold -1, -inf and a rest of
+ * 0.  Workspace: gnn_top_workspace_bytes.
+ *
+ * gnn_distill_loss: a student's loss against such a list, and its gradient.
+ *   q_r = exp(logq[i, r]) / N,  q_0 = rest[i] / N,  N = their sum
+ *         (rest NULL: 0, so that logq may be any logits of the teacher / T)
+ *   p   = softmax of Z[i] / T,  p_0 = the share of the entries not listed
+ *   kl_i = T^2 [ sum_r q_r log(q_r / p_index(r)) + q_0 log(q_0 / p_0) ]
+ *   out  = sum_i w_i kl_i                                    (one float)
+ *   dZ[i, j] = w_i T (p_j - q_r)           for entries j = index[i, r]
+ *              w_i T p_j (1 - q_0 / p_0)   for all others
+ * An index outside [0, C) marks a place that is not used, and one that a row
+ * repeats counts at its first place.  Rows are left out, with kl and gradient
+ * 0, whose list has no index in range, or nothing but q of 0, or whose logits
+ * are all -inf: of the first kind the logits may hold anything.  A row of
+ * weight 0 adds nothing and has a gradient of 0.  weight: n floats (NULL: 1/n).
+ * A q above 0 where the student has p = 0 makes kl infinite.  Columns of dZ's
+ * rows past C are not written; kl (n floats) and dZ (stride ld_dz) may be NULL.
+ * n = 0 gives out = 0.  Exponentials of the row are fp32's, everything of the
+ * list is in double, and so are all sums.  Workspace:
+ * gnn_distill_workspace_bytes.
+ *
+ * For all three: results are bit-reproducible, and no output may overlap an
+ * input, another output or the workspace. */
+#define GNN_TOP_MOST 256
+size_t gnn_sample_workspace_bytes(int32_t n, int32_t C);
+gnn_status gnn_sample_actions(int32_t n, int32_t C, const float* Z, int64_t ld_z,
+                              const float* u, double temperature, int32_t top_k,
+                              double top_p, double min_p, int32_t* action,
+                              float* logp, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream);
+size_t gnn_top_workspace_bytes(int32_t n, int32_t C, int32_t k);
+gnn_status gnn_top_logits(int32_t n, int32_t C, const float* Z, int64_t ld_z,
+                          int32_t k, double temperature, int32_t* index,
+                          float* logq, float* rest, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+size_t gnn_distill_workspace_bytes(int32_t n, int32_t C, int32_t k);
+gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
+                            int32_t k, const int32_t* index, const float* logq,
+                            const float* rest, const float* weight,
+                            double temperature, float* out, float* kl, float* dZ,
+                            int64_t ld_dz, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream);
+
 /* A set of tensors that are updated together (all weights of a model), each
  * of `count` contiguous elements (count 0: nothing).
  *   W, G     weights and gradients (device, 4-byte aligned; gradients may be
@@ -685,14 +761,15 @@ gnn_status gnn_mfma_rate_probe(int32_t kind, int32_t blocks, int32_t iters,
 #define GNN_K_COLSUM 8        /* bias-gradient column sums */
 #define GNN_K_PLAN 9          /* aggregation plan build */
 #define GNN_K_TRANSPOSE 10    /* transposed values (Algorithm 6) */
-#define GNN_K_LOSS 11         /* classifier or policy loss and its gradient */
+#define GNN_K_LOSS 11         /* classifier, policy or student's loss, its gradient */
 #define GNN_K_UPDATE 12       /* weight update (SGD, Adam or AdamW) */
 #define GNN_K_INDUCE 13       /* induced subgraph on the GPU */
 #define GNN_K_GATHER 14       /* feature / label row gather */
 #define GNN_K_SDDMM 15        /* GAT per-entry dot products */
 #define GNN_K_WSPLIT 16       /* weights split into bf16 pieces (split products) */
 #define GNN_K_NORM 17         /* norm of all gradients */
-#define GNN_K_COUNT 18
+#define GNN_K_SAMPLE 18       /* actions drawn, top logits */
+#define GNN_K_COUNT 19
 
 /* When enabled, every kernel launch is bracketed by a pair of HIP events on
  * its stream.  gnn_timer_read synchronises on the recorded events and

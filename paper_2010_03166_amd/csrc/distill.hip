@@ -1,0 +1,435 @@
+// The loss of a student that is taught by a teacher's top logits, and its
+// gradient (the formulas: include/gnnprop.h).
+//
+// The entries that the teacher names are taken from their list, all others
+// from the row: their sums are formed apart, so that the share left over is
+// never a difference of two sums that are nearly alike.  Of the others the
+// gradient is one factor times exp((z - their largest) / T), so a row is read
+// once and each exponential computed once.
+#include <cmath>
+
+#include "abi.hpp"
+#include "team.hpp"
+
+using namespace gnnprop;
+
+namespace {
+
+struct Part {   // of a row that several blocks share: its entries not named
+  double sum;   // of exp((z - top) / T)
+  float top;
+  float pad;
+};
+
+struct DistillArgs {
+  int32_t n, C;
+  const float* Z;
+  int64_t ld_z;
+  int32_t k;
+  const int32_t* index;
+  const float *logq, *rest, *weight;
+  double T, inv_t, mean;
+  float* out;
+  float* kl;
+  float* dZ;
+  int64_t ld_dz;
+  double* part;   // losses, one per block (split rows: one per row)
+  Part* parts;    // split rows: per_row for each row
+  int32_t per_row;
+  int64_t blocks, block0;  // of all launches, and in the launches before
+};
+
+// The teacher's list of one row.
+struct Named {
+  const int32_t* index;
+  const float* logq;
+  int32_t k, C;
+  bool repeats;  // whether an index may be there twice: its first place counts
+
+  __device__ int32_t at(int32_t j) const {
+    const int32_t c = index[j];
+    if (c < 0 || c >= C) return -1;
+    if (repeats)
+      for (int32_t i = 0; i < j; ++i)
+        if (index[i] == c) return -1;
+    return c;
+  }
+};
+
+// What a row's loss and gradient are made of.
+struct Scalars {
+  bool live;      // whether the row takes part
+  double kl;
+  double shift_q, scale_q;  // q = exp(logq - shift_q) scale_q
+  double top, scale_p;      // p = exp((z - top) / T) scale_p
+  float others;             // the factor of the other entries' exponentials
+};
+
+// From the sums over the entries not named: `high` their largest, `sum` of
+// exp((z - high) / T).
+template <class T>
+__device__ Scalars row_scalars(const DistillArgs& a, const T& team, const Named& named,
+                               const float* row, float rest, float high, double sum) {
+  Scalars s = {};
+  float most = -INFINITY, top = high;
+  bool any = false, bad = false;
+  for (int32_t j = team.t; j < a.k; j += T::LANES) {
+    const int32_t c = named.at(j);
+    if (c < 0) continue;
+    any = true;
+    bad |= named.logq[j] != named.logq[j];
+    most = fmaxf(most, named.logq[j]);
+    top = fmaxf(top, row[c]);
+  }
+  const double ln_rest = rest > 0.f ? log((double)rest) : rest == rest ? -INFINITY : rest;
+  most = fmaxf(team.max(most), (float)ln_rest);
+  top = team.max(top);
+  any = team.any(any);
+  s.live = (team.any(bad) || most > -INFINITY) && any && top > -INFINITY;
+  if (!s.live) return s;
+  double nq = 0.0, np = 0.0, cross = 0.0;
+  for (int32_t j = team.t; j < a.k; j += T::LANES) {
+    const int32_t c = named.at(j);
+    if (c < 0) continue;
+    const double lq = (double)named.logq[j] - most, lp = ((double)row[c] - top) * a.inv_t;
+    const double q = exp_exact(lq);
+    nq += q;
+    np += exp_exact(lp);
+    if (!(q == 0.0)) cross += q * (lq - lp);
+  }
+  const double high_p = sum > 0.0 ? ((double)high - top) * a.inv_t : 0.0;
+  const double down = sum == 0.0 ? 0.0 : exp_exact(high_p);
+  const double r = exp_exact(ln_rest - most);
+  nq = team.sum(nq) + r;
+  np = team.sum(np) + sum * down;
+  cross = team.sum(cross);
+  if (!(r == 0.0)) cross += r * (ln_rest - most - (high_p + log(sum)));
+  s.kl = a.T * a.T * (cross / nq - log(nq) + log(np));
+  s.shift_q = most;
+  s.scale_q = 1.0 / nq;
+  s.top = top;
+  s.scale_p = 1.0 / np;
+  s.others = sum == 0.0 ? 0.f : (float)(a.T * (down / np - r / (nq * sum)));
+  return s;
+}
+
+// The gradient's values at the entries that the teacher names in columns
+// [from, to).
+template <class T>
+__device__ void named_gradient(const DistillArgs& a, const T& team, const Named& named,
+                               const float* row, const Scalars& s, double w, float* to,
+                               int32_t from, int32_t end) {
+  for (int32_t j = team.t; j < a.k; j += T::LANES) {
+    const int32_t c = named.at(j);
+    if (c < from || c >= end) continue;
+    const double q = exp_exact((double)named.logq[j] - s.shift_q) * s.scale_q;
+    const double p = exp_exact(((double)row[c] - s.top) * a.inv_t) * s.scale_p;
+    to[c] = (float)(w * a.T * (p - q));
+  }
+}
+
+// A part of a row (or the row) in registers with the entries named taken out,
+// and the others' largest and sum.
+template <class T, class Row>
+struct Others {
+  Row row;
+  float high;
+  double sum;
+  bool repeats;
+
+  // bits: one for each column that the team holds.
+  __device__ void load(const DistillArgs& a, const T& team, const float* from, int32_t col0,
+                       const int32_t* index, uint32_t* bits) {
+    row.load(from + col0, a.C - col0, team.t);
+    for (int32_t k = team.t; k < (Row::MOST + 31) / 32; k += T::LANES) bits[k] = 0;
+    team.sync();
+    bool twice = false;
+    for (int32_t j = team.t; j < a.k; j += T::LANES) {
+      const int32_t c = index[j];
+      if (c < col0 || c >= a.C || c - col0 >= Row::MOST) continue;
+      const uint32_t bit = 1u << ((c - col0) & 31);
+      twice |= (atomicOr(&bits[(c - col0) >> 5], bit) & bit) != 0;
+    }
+    repeats = team.any(twice);
+    team.sync();
+    high = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < Row::CHUNKS; ++k) {
+      const int32_t c = row.column(k);
+      const uint32_t out = bits[c >> 5] >> (c & 31);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (out >> j & 1) row.z[k][j] = -INFINITY;
+      high = fmaxf(high, max4(row.z[k]));
+    }
+    high = team.max(high);
+    const float shift = shift_of(high), inv_t = (float)a.inv_t;
+    sum = 0.0;
+#pragma unroll
+    for (int k = 0; k < Row::CHUNKS; ++k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) row.z[k][j] = expf((row.z[k][j] - shift) * inv_t);
+      sum += sum4(row.z[k]);
+    }
+    sum = team.sum(sum);
+  }
+  __device__ void store(float* to, int32_t col0, int32_t C, float factor) const {
+#pragma unroll
+    for (int k = 0; k < Row::CHUNKS; ++k) {
+      f4 g = row.z[k] * factor;
+      if (factor == 0.f) g = {0.f, 0.f, 0.f, 0.f};
+      store_cols(to + col0, row.column(k), C - col0, g);
+    }
+  }
+};
+
+__device__ inline double weight_of(const DistillArgs& a, int32_t i) {
+  return a.weight ? (double)a.weight[i] : a.mean;
+}
+
+// What all lanes of a team have written to memory is there before what they
+// write next.
+template <class T>
+__device__ inline void stores_done(const T& team) {
+  if (T::W > 1) __syncthreads();
+  else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+}
+
+template <int G, int W, class Row>
+__global__ __launch_bounds__((threads_of<G, W>())) void distill_kernel(DistillArgs a) {
+  using T = Team<G, W>;
+  constexpr int THREADS = threads_of<G, W>(), R = THREADS / T::LANES;
+  __shared__ typename T::Shared s[R];
+  __shared__ uint32_t s_bits[R][(Row::MOST + 31) / 32];
+  __shared__ double s_loss[THREADS / 64];
+  const int own = threadIdx.x / T::LANES;
+  const T team(s[own], threadIdx.x % T::LANES);
+  const int64_t i = (a.block0 + blockIdx.x) * R + own;
+  double loss = 0.0;
+  if (i < a.n) {
+    const float* from = a.Z + i * a.ld_z;
+    Named named = {a.index + i * a.k, a.logq + i * a.k, a.k, a.C, false};
+    Others<T, Row> others;
+    others.load(a, team, from, 0, named.index, s_bits[own]);
+    named.repeats = others.repeats;
+    const Scalars x = row_scalars(a, team, named, from, a.rest ? a.rest[i] : 0.f, others.high,
+                                  others.sum);
+    const double w = weight_of(a, (int32_t)i);
+    const bool counts = x.live && w != 0.0;
+    if (counts) loss = w * x.kl;
+    if (a.kl && team.t == 0) a.kl[i] = (float)x.kl;
+    if (a.dZ) {
+      float* to = a.dZ + i * a.ld_dz;
+      others.store(to, 0, a.C, counts ? (float)(w * x.others) : 0.f);
+      stores_done(team);
+      if (counts) named_gradient(a, team, named, from, x, w, to, 0, a.C);
+    }
+  }
+  // the block's share of the loss, in a fixed order
+  if (team.t != 0) loss = 0.0;
+  loss = lanes_sum<64>(loss);
+  if ((threadIdx.x & 63) == 0) s_loss[threadIdx.x >> 6] = loss;
+  __syncthreads();
+  if (threadIdx.x) return;
+  loss = 0.0;
+  for (int k = 0; k < THREADS / 64; ++k) loss += s_loss[k];
+  if (a.blocks == 1) a.out[0] = (float)loss;
+  else a.part[a.block0 + blockIdx.x] = loss;
+}
+
+// Rows past 32,768 columns: a launch for the sums of their parts, one for the
+// scalars, which every block of the row forms alike, and the gradient.
+using SplitTeam = Team<64, 4>;
+using SplitRow = Held<64, 4, 4>;
+constexpr int32_t SPLIT_COLS = SplitRow::MOST;
+
+__global__ __launch_bounds__(256) void distill_sums_kernel(DistillArgs a) {
+  __shared__ SplitTeam::Shared s;
+  __shared__ uint32_t s_bits[SPLIT_COLS / 32];
+  const SplitTeam team(s, threadIdx.x);
+  const int64_t b = a.block0 + blockIdx.x, i = b / a.per_row;
+  Others<SplitTeam, SplitRow> others;
+  others.load(a, team, a.Z + i * a.ld_z, (int32_t)(b % a.per_row) * SPLIT_COLS, a.index + i * a.k,
+              s_bits);
+  if (team.t == 0) a.parts[b] = {others.sum, others.high, others.repeats ? 1.f : 0.f};
+}
+
+__global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a) {
+  __shared__ SplitTeam::Shared s;
+  __shared__ uint32_t s_bits[SPLIT_COLS / 32];
+  const SplitTeam team(s, threadIdx.x);
+  const int32_t todo = a.dZ ? a.per_row : 1;
+  const int64_t b = a.block0 + blockIdx.x, i = b / todo;
+  const int32_t part = (int32_t)(b % todo);
+  const float* from = a.Z + i * a.ld_z;
+  Named named = {a.index + i * a.k, a.logq + i * a.k, a.k, a.C, false};
+  const Part* at = a.parts + i * a.per_row;
+  float high = -INFINITY;
+  bool repeats = false;
+  for (int32_t k = team.t; k < a.per_row; k += 256) {
+    high = fmaxf(high, at[k].top);
+    repeats |= at[k].pad != 0.f;
+  }
+  high = team.max(high);
+  named.repeats = team.any(repeats);
+  double sum = 0.0;
+  for (int32_t k = team.t; k < a.per_row; k += 256)
+    if (at[k].sum != 0.0) sum += at[k].sum * exp_exact(((double)at[k].top - high) * a.inv_t);
+  sum = team.sum(sum);
+  const Scalars x = row_scalars(a, team, named, from, a.rest ? a.rest[i] : 0.f, high, sum);
+  const double w = weight_of(a, (int32_t)i);
+  const bool counts = x.live && w != 0.0;
+  if (part == 0 && team.t == 0) {
+    a.part[i] = counts ? w * x.kl : 0.0;
+    if (a.kl) a.kl[i] = (float)x.kl;
+  }
+  if (!a.dZ) return;
+  Others<SplitTeam, SplitRow> others;
+  const int32_t col0 = part * SPLIT_COLS;
+  others.load(a, team, from, col0, named.index, s_bits);
+  float* to = a.dZ + i * a.ld_dz;
+  const float down = others.sum == 0.0
+                         ? 0.f : (float)exp_exact(((double)others.high - high) * a.inv_t);
+  others.store(to, col0, a.C, counts ? (float)(w * x.others) * down : 0.f);
+  stores_done(team);
+  if (counts) named_gradient(a, team, named, from, x, w, to, col0, min(col0 + SPLIT_COLS, a.C));
+}
+
+// out = the sum of `count` terms, in a fixed order.
+__global__ __launch_bounds__(1024) void distill_final_kernel(int32_t count,
+                                                             const double* __restrict__ part,
+                                                             float* __restrict__ out) {
+  __shared__ double s[16];
+  double x = 0.0;
+  for (int32_t k = threadIdx.x; k < count; k += 1024) x += part[k];
+  x = lanes_sum<64>(x);
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+  __syncthreads();
+  if (threadIdx.x) return;
+  x = 0.0;
+  for (int k = 0; k < 16; ++k) x += s[k];
+  out[0] = (float)x;
+}
+
+struct Launch {
+  void (*kernel)(DistillArgs);  // NULL: split rows
+  int32_t rows, threads;
+};
+template <int G, int W, int V>
+Launch held() {
+  return {distill_kernel<G, W, Held<G, W, V>>, threads_of<G, W>() / (G * W), threads_of<G, W>()};
+}
+template <int G>
+Launch few(int32_t v) {
+  return v == 3 ? held<G, 1, 3>() : held<G, 1, 4>();
+}
+Launch choose(int32_t C) {
+  const int32_t q = (int32_t)ceil_div(C, 4);
+  if (q == 1) return held<1, 1, 1>();
+  if (q == 2) return held<1, 1, 2>();
+  if (q <= 4) return few<1>(q);
+  if (q <= 8) return few<2>((q + 1) / 2);
+  if (q <= 16) return few<4>((q + 3) / 4);
+  if (q <= 32) return few<8>((q + 7) / 8);
+  if (q <= 64) return few<16>((q + 15) / 16);
+  if (q <= 128) return few<32>((q + 31) / 32);
+  if (q <= 256) return few<64>((q + 63) / 64);
+  if (q <= 512) return held<64, 1, 8>();
+  if (q <= 1024) return held<64, 4, 4>();
+  if (q <= 2048) return held<64, 8, 4>();
+  if (q <= 4096) return held<64, 16, 4>();
+  if (q <= 6144) return held<64, 16, 6>();
+  if (q <= 8192) return held<64, 16, 8>();
+  return {nullptr, 1, 256};
+}
+
+// [losses | parts' sums]
+struct Layout {
+  size_t parts, total;
+};
+Layout layout_of(int32_t n, int32_t C) {
+  const Launch l = choose(C);
+  Layout o;
+  o.parts = round_up((size_t)ceil_div(n, l.rows) * sizeof(double), 256);
+  o.total = o.parts + (l.kernel ? 0 : (size_t)n * ceil_div(C, SPLIT_COLS) * sizeof(Part));
+  return o;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gnn_distill_workspace_bytes(int32_t n, int32_t C, int32_t k) {
+  if (n < 0 || C <= 0 || C > MOST_COLS || k <= 0 || k > GNN_TOP_MOST) return 0;
+  return layout_of(n, C).total;
+}
+
+gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, int32_t k,
+                            const int32_t* index, const float* logq, const float* rest,
+                            const float* weight, double temperature, float* out, float* kl,
+                            float* dZ, int64_t ld_dz, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream) {
+  if (n < 0 || C <= 0 || C > MOST_COLS || ld_z < C || k <= 0 || k > GNN_TOP_MOST ||
+      (dZ && ld_dz < C) || !temperature_ok(temperature))
+    return GNN_ERR_SHAPE;
+  if (!out || (n > 0 && (!Z || !index || !logq))) return GNN_ERR_NULL;
+  if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
+  const Layout o = layout_of(n, C);
+  if (workspace_bytes < o.total || (o.total > 0 && !workspace)) return GNN_ERR_WORKSPACE;
+  {
+    const size_t rows = (size_t)n * 4, list = rows * k;
+    const void* ins[] = {Z, index, logq, rest, weight};
+    const size_t inb[] = {mat_bytes(n, C, ld_z), list, list, rows, rows};
+    const void* outs[] = {out, kl, dZ, workspace};
+    const size_t outb[] = {4, rows, mat_bytes(n, C, ld_dz), o.total};
+    for (int i = 0; i < 4; ++i) {
+      for (int q = 0; q < 5; ++q)
+        if (ranges_overlap(outs[i], outb[i], ins[q], inb[q])) return GNN_ERR_ALIAS;
+      for (int q = 0; q < i; ++q)
+        if (ranges_overlap(outs[i], outb[i], outs[q], outb[q])) return GNN_ERR_ALIAS;
+    }
+  }
+  const Launch l = choose(C);
+  DistillArgs a = {};
+  a.n = n;
+  a.C = C;
+  a.Z = Z;
+  a.ld_z = ld_z;
+  a.k = k;
+  a.index = index;
+  a.logq = logq;
+  a.rest = rest;
+  a.weight = weight;
+  a.T = temperature;
+  a.inv_t = 1.0 / temperature;
+  a.mean = n > 0 ? 1.0 / n : 0.0;
+  a.out = out;
+  a.kl = kl;
+  a.dZ = dZ;
+  a.ld_dz = ld_dz;
+  char* ws = static_cast<char*>(workspace);
+  a.part = reinterpret_cast<double*>(ws);
+  a.parts = reinterpret_cast<Part*>(ws + o.parts);
+  a.per_row = (int32_t)ceil_div(C, SPLIT_COLS);
+  const auto run = [&](void (*kernel)(DistillArgs), int32_t threads, int64_t blocks) {
+    a.blocks = blocks;
+    for (a.block0 = 0; a.block0 < blocks; a.block0 += LAUNCH_BLOCKS)
+      kernel<<<(unsigned)std::min(blocks - a.block0, LAUNCH_BLOCKS), threads, 0, stream>>>(a);
+  };
+  timer_begin(GNN_K_LOSS, stream);
+  const int64_t parts = ceil_div(n, l.rows);
+  if (l.kernel) {
+    run(l.kernel, l.threads, parts);
+  } else {
+    const int64_t blocks = (int64_t)n * a.per_row;
+    run(distill_sums_kernel, 256, blocks);
+    run(distill_grad_kernel, 256, dZ ? blocks : n);
+  }
+  if (!l.kernel || parts != 1)
+    distill_final_kernel<<<1, 1024, 0, stream>>>((int32_t)parts, a.part, out);
+  timer_end(GNN_K_LOSS, (dZ ? 8.0 : 4.0) * n * C, stream);
+  GNN_HIP(hipGetLastError());
+  return GNN_OK;
+}
+
+}  // extern "C"

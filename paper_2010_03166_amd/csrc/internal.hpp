@@ -66,6 +66,16 @@ __device__ inline double butterfly(double v) {
   const uint32_t lo = (uint32_t)butterfly_word<D>((int)x);
   return __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
 }
+template <int D>
+__device__ inline uint64_t butterfly(uint64_t x) {
+  const uint32_t hi = (uint32_t)butterfly_word<D>((int)(x >> 32));
+  const uint32_t lo = (uint32_t)butterfly_word<D>((int)x);
+  return (uint64_t)hi << 32 | lo;
+}
+template <int D>
+__device__ inline int32_t butterfly(int32_t x) {
+  return butterfly_word<D>(x);
+}
 // Largest value and sum over groups of G consecutive lanes, in all of them.
 template <int G, int D = 1>
 __device__ inline float lanes_max(float v) {

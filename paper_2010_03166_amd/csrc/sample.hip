@@ -1,0 +1,496 @@
+// Actions drawn from rows of logits (temperature, top-k, top-p, min-p) by given
+// random numbers, and the top logits of rows (the formulas: include/gnnprop.h).
+//
+// A draw must not depend on the order in which a sum is formed, and what lies
+// next to a border (of the kept actions, of the random number) has to fall on
+// its own side of it.  So an action's weight exp((z - top) / T) is a whole
+// number: in units of 2^-51 of the largest, or more where a row's sum would
+// pass 2^62.  Sums of them are exact, and equal logits have equal weights.
+#include <cmath>
+
+#include "abi.hpp"
+#include "team.hpp"
+
+using namespace gnnprop;
+
+namespace {
+
+// 2^(i / 64), from the series of exp.
+constexpr double exp2_64th(int i) {
+  const double x = 0.6931471805599453094 * i / 64.0;
+  double sum = 1.0;
+  for (int k = 24; k > 0; --k) sum = 1.0 + sum * x / k;
+  return sum;
+}
+struct Table {
+  double at[64];
+};
+constexpr Table make_table() {
+  Table t = {};
+  for (int i = 0; i < 64; ++i) t.at[i] = exp2_64th(i);
+  return t;
+}
+__constant__ const Table TABLE = make_table();
+
+// Units of a weight: 2^bits of them are the largest one.  At most 2^62 a row,
+// and 51 bits leave the product below a double's first bit.
+inline int bits_of(int32_t C) {
+  int log = 0;
+  while ((int64_t)1 << log < C) ++log;
+  return std::min(51, 62 - log);
+}
+
+// exp(d / T) in units of 2^-bits, d <= 0: with d / T in 64ths of an octave,
+// 2^(q / 64) from the table and the remainder's series (below 4e-14 of it left
+// out), added to 2^52, whose last bits the whole number then is.
+__device__ inline uint64_t weight_of(double d, double scale, int bits, const double* table) {
+  constexpr double a = 0.6931471805599453 / 64.0;
+  const double t = fmax(d * scale, -64.0 * 56.0);
+  const double k = rint(t), f = t - k;
+  const int q = (int)k;
+  double p = fma(f, a * a * a * a / 24.0, a * a * a / 6.0);
+  p = fma(p, f, a * a / 2.0);
+  p = fma(p, f, a);
+  p = fma(p, f, 1.0);
+  const uint64_t unit = (uint64_t)__double_as_longlong(table[q & 63]);
+  const double e = __longlong_as_double((long long)(unit + ((uint64_t)(int64_t)((q >> 6) + bits) << 52)));
+  return (uint64_t)__double_as_longlong(fma(e, p, 4503599627370496.0)) & 0xfffffffffffffull;
+}
+
+// ------------------------------------------------------------------ draws
+
+struct SampleArgs {
+  int32_t n, C;
+  const float* Z;
+  int64_t ld_z;
+  const float* u;
+  double scale;  // 64 / (T ln 2); 0: the best action
+  float bins;    // bins of the logits to a unit, 8 / T
+  int32_t bits, top_k;
+  double top_p;
+  double cut;  // T ln(min_p), or -inf
+  int32_t* action;
+  float* logp;
+  int64_t block0;
+};
+
+// What is kept of a row, and its entries' weights.
+template <class Row>
+struct Kept {
+  const Row& row;
+  const SampleArgs& a;
+  const double* table;
+  double top;
+  Border k = NO_BORDER, p = NO_BORDER;
+  bool near = false;  // whether min-p counts
+
+  __device__ uint64_t weight(float z, int32_t col) const {
+    const double d = (double)z - top;
+    const uint64_t w = weight_of(d, a.scale, a.bits, table);
+    return within(k, z, col) && within(p, z, col) && !(near && d < a.cut) ? w : 0;
+  }
+  template <class F>
+  __device__ void each(F f) const {
+    each_chunk(row, [&](int i, f4 z) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(z[j], row.column(i) + j, weight(z[j], row.column(i) + j));
+    });
+  }
+  __device__ uint64_t sum4w(int i, f4 z) const {
+    uint64_t s = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s += weight(z[j], row.column(i) + j);
+    return s;
+  }
+  __device__ uint64_t sum() const {
+    uint64_t s = 0;
+    each_chunk(row, [&](int i, f4 z) { s += sum4w(i, z); });
+    return s;
+  }
+};
+
+// The logits that are there, one each.
+template <class Row>
+struct Present {
+  const Row& row;
+  template <class F>
+  __device__ void each(F f) const {
+    each_chunk(row, [&](int i, f4 z) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(z[j], row.column(i) + j, z[j] > -INFINITY);
+    });
+  }
+};
+
+__device__ inline uint64_t unit_fraction(float u) {
+  if (!(u > 0.f)) return 0;
+  if (u >= 1.f) return ~0ull;
+  return (uint64_t)((double)u * 18446744073709551616.0);
+}
+
+template <class T, class Row>
+__device__ void sample_row(const SampleArgs& a, const T& team, int32_t i, const double* table) {
+  Row row;
+  row.load(a.Z + (int64_t)i * a.ld_z, a.C, team.t);
+  float top = -INFINITY, low = INFINITY;
+  bool bad = false;
+  each_chunk(row, [&](int, f4 z) {
+    top = fmaxf(top, max4(z));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bad |= z[j] != z[j];
+      low = fminf(low, z[j] > -INFINITY ? z[j] : INFINITY);
+    }
+  });
+  top = team.max(top);
+  if (team.any(bad) || !(fabsf(top) < INFINITY)) {
+    if (team.t == 0) {
+      a.action[i] = -1;
+      if (a.logp) a.logp[i] = 0.f;
+    }
+    return;
+  }
+  double lse = 0.0;  // of the logits, from the largest
+  if (a.logp) {
+    each_chunk(row, [&](int, f4 z) { lse += (double)sum4(exp4(z, top)); });
+    lse = log_quick((float)team.sum(lse));
+  }
+  Kept<Row> kept = {row, a, table, top};
+  const Present<Row> present = {row};
+  if (a.scale == 0.0) {
+    kept.k = team.select(present, top, 0.f, 1);
+    if (team.t == 0) {
+      a.action[i] = kept.k.col;
+      if (a.logp) a.logp[i] = (float)-lse;
+    }
+    return;
+  }
+  if (a.top_k) {
+    const float range = top + team.max(-low);
+    const float scale = (T::BINS - 1) / range;
+    kept.k = team.select(present, top, scale < INFINITY ? scale : 0.f, (uint64_t)a.top_k);
+  }
+  if (a.top_p < 1.0) {
+    const uint64_t all = team.sum(kept.sum());
+    const uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
+    kept.p = team.select(kept, top, a.bins, P < 1 ? 1 : P < all ? P : all);
+  }
+  kept.near = true;
+  // the action that holds the random number's share of the sum
+  const uint64_t own = lanes_sum<T::G>(kept.sum());
+  uint64_t all = own, ahead = 0;
+  if (T::W > 1) {
+    if (team.lane == 0) team.s.sums[team.wave] = own;
+    team.sync();
+    all = 0;
+    for (int k = 0; k < T::W; ++k) {
+      all += team.s.sums[k];
+      if (k < team.wave) ahead += team.s.sums[k];
+    }
+    team.sync();
+  }
+  uint64_t target = __umul64hi(all, unit_fraction(a.u[i]));
+  if (target < ahead || target >= ahead + own) return;
+  target -= ahead;
+  for (int k = 0; k < row.chunks(); ++k) {
+    const f4 z = row.chunk(k);
+    const uint64_t mine = kept.sum4w(k, z), sum = lanes_sum<T::G>(mine);
+    if (target >= sum) {
+      target -= sum;
+      continue;
+    }
+    uint64_t x = team.before(mine);
+    if (target < x || target >= x + mine) break;
+    for (int j = 0; j < 4; ++j) {
+      x += kept.weight(z[j], row.column(k) + j);
+      if (target < x) {
+        a.action[i] = row.column(k) + j;
+        if (a.logp) a.logp[i] = (float)((double)z[j] - top - lse);
+        break;
+      }
+    }
+    break;
+  }
+}
+
+template <int G, int W, class Row>
+__global__ __launch_bounds__((threads_of<G, W>())) void sample_kernel(SampleArgs a) {
+  using T = Team<G, W>;
+  constexpr int R = threads_of<G, W>() / T::LANES;
+  __shared__ typename T::Shared s[R];
+  __shared__ double s_table[64];
+  if (threadIdx.x < 64) s_table[threadIdx.x] = TABLE.at[threadIdx.x];
+  __syncthreads();
+  const int own = threadIdx.x / T::LANES;
+  const int64_t i = (a.block0 + blockIdx.x) * R + own;
+  if (i >= a.n) return;
+  const T team(s[own], threadIdx.x % T::LANES);
+  sample_row<T, Row>(a, team, (int32_t)i, s_table);
+}
+
+// ------------------------------------------------------------- top logits
+
+constexpr int32_t MOST_TOP = GNN_TOP_MOST;
+
+struct TopArgs {
+  int32_t n, C;
+  const float* Z;
+  int64_t ld_z;
+  int32_t k;
+  double inv_t;
+  int32_t* index;
+  float *logq, *rest;
+  int64_t block0;
+};
+
+// Exponentials of entries, from the largest.
+__device__ inline float tempered(float z, float top, float inv_t) {
+  return z == -INFINITY ? 0.f : expf((z - top) * inv_t);
+}
+
+template <class T, class Row>
+__device__ void top_row(const TopArgs& a, const T& team, uint64_t* list, int32_t i) {
+  Row row;
+  row.load(a.Z + (int64_t)i * a.ld_z, a.C, team.t);
+  int32_t* index = a.index + (int64_t)i * a.k;
+  float* logq = a.logq + (int64_t)i * a.k;
+  float top = -INFINITY, low = INFINITY;
+  bool bad = false;
+  each_chunk(row, [&](int, f4 z) {
+    top = fmaxf(top, max4(z));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bad |= z[j] != z[j];
+      low = fminf(low, z[j] > -INFINITY ? z[j] : INFINITY);
+    }
+  });
+  top = team.max(top);
+  if (team.any(bad) || !(fabsf(top) < INFINITY)) {
+    for (int32_t j = team.t; j < a.k; j += T::LANES) {
+      index[j] = -1;
+      logq[j] = -INFINITY;
+    }
+    if (team.t == 0 && a.rest) a.rest[i] = 0.f;
+    return;
+  }
+  const float range = top + team.max(-low);
+  const float scale = (T::BINS - 1) / range;
+  const Border b = team.select(Present<Row>{row}, top, scale < INFINITY ? scale : 0.f,
+                               (uint64_t)a.k);
+  // the entries kept, and the sums of both parts
+  if (team.t == 0) team.s.count = 0;
+  team.sync();
+  const float inv_t = (float)a.inv_t;
+  double in = 0.0, out = 0.0;
+  each_chunk(row, [&](int c, f4 z) {
+    float more = 0.f, less = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int32_t col = row.column(c) + j;
+      const float e = tempered(z[j], top, inv_t);
+      if (z[j] > -INFINITY && within(b, z[j], col)) {
+        more += e;
+        list[atomicAdd(&team.s.count, 1)] = place(z[j], col);
+      } else {
+        less += e;
+      }
+    }
+    in += more;
+    out += less;
+  });
+  in = team.sum(in);
+  out = team.sum(out);
+  team.sync();
+  const int32_t m = team.s.count;
+  const double lse = log_quick((float)(in + out));
+  for (int32_t j = team.t; j < a.k; j += T::LANES) {
+    if (j >= m) {
+      index[j] = -1;
+      logq[j] = -INFINITY;
+      continue;
+    }
+    const uint64_t own = list[j];
+    int32_t rank = 0;
+    for (int32_t q = 0; q < m; ++q) rank += list[q] < own;
+    const uint32_t key = ~(uint32_t)(own >> 32);
+    const float z = __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
+    index[rank] = (int32_t)(uint32_t)own;
+    logq[rank] = (float)(((double)z - top) * a.inv_t - lse);
+  }
+  if (team.t == 0 && a.rest) a.rest[i] = (float)(out / (in + out));
+}
+
+template <int G, int W, class Row>
+__global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
+  using T = Team<G, W>;
+  constexpr int R = threads_of<G, W>() / T::LANES;
+  constexpr int MOST = Row::MOST < MOST_TOP
+                           ? Row::MOST : MOST_TOP;
+  __shared__ typename T::Shared s[R];
+  __shared__ uint64_t s_list[R][MOST];
+  const int own = threadIdx.x / T::LANES;
+  const int64_t i = (a.block0 + blockIdx.x) * R + own;
+  if (i >= a.n) return;
+  const T team(s[own], threadIdx.x % T::LANES);
+  top_row<T, Row>(a, team, s_list[own], (int32_t)i);
+}
+
+// ---------------------------------------------------------------- launches
+
+template <class Args>
+struct Launch {
+  void (*kernel)(Args);
+  int32_t rows, threads;
+};
+#define LAUNCH(G, W, ROW)                                                        \
+  Launch<Args>{Kernel::template of<G, W, ROW>(), threads_of<G, W>() / (G * W), \
+               threads_of<G, W>()}
+
+struct SampleKernel {
+  template <int G, int W, class Row>
+  static constexpr auto of() { return sample_kernel<G, W, Row>; }
+};
+struct TopKernel {
+  template <int G, int W, class Row>
+  static constexpr auto of() { return top_kernel<G, W, Row>; }
+};
+
+template <class Args, class Kernel, int G, int W, int V>
+Launch<Args> held() {
+  using Row = Held<G, W, V>;
+  return LAUNCH(G, W, Row);
+}
+
+template <class Args, class Kernel, int G>
+Launch<Args> few(int32_t v) {
+  return v == 3 ? held<Args, Kernel, G, 1, 3>() : held<Args, Kernel, G, 1, 4>();
+}
+
+template <class Args, class Kernel>
+Launch<Args> choose(int32_t C) {
+  const int32_t q = (int32_t)ceil_div(C, 4);
+  if (q == 1) return held<Args, Kernel, 1, 1, 1>();
+  if (q == 2) return held<Args, Kernel, 1, 1, 2>();
+  if (q <= 4) return few<Args, Kernel, 1>(q);
+  if (q <= 8) return few<Args, Kernel, 2>((q + 1) / 2);
+  if (q <= 16) return few<Args, Kernel, 4>((q + 3) / 4);
+  if (q <= 32) return few<Args, Kernel, 8>((q + 7) / 8);
+  if (q <= 64) return few<Args, Kernel, 16>((q + 15) / 16);
+  if (q <= 128) return few<Args, Kernel, 32>((q + 31) / 32);
+  if (q <= 256) return few<Args, Kernel, 64>((q + 63) / 64);
+  if (q <= 384) return held<Args, Kernel, 64, 1, 6>();
+  if (q <= 512) return held<Args, Kernel, 64, 1, 8>();
+  if (q <= 1024) return held<Args, Kernel, 64, 4, 4>();
+  if (q <= 2048) return held<Args, Kernel, 64, 8, 4>();
+  if (q <= 4096) return held<Args, Kernel, 64, 16, 4>();
+  if (q <= 6144) return held<Args, Kernel, 64, 16, 6>();
+  if (q <= 8192) return held<Args, Kernel, 64, 16, 8>();
+  using Row = Reread<64, 16>;
+  return LAUNCH(64, 16, Row);
+}
+
+template <class Args>
+gnn_status run(const Launch<Args>& l, Args a, int kclass, hipStream_t stream) {
+  const int64_t blocks = ceil_div(a.n, l.rows);
+  timer_begin(kclass, stream);
+  for (a.block0 = 0; a.block0 < blocks; a.block0 += LAUNCH_BLOCKS)
+    l.kernel<<<(unsigned)std::min(blocks - a.block0, LAUNCH_BLOCKS), l.threads, 0, stream>>>(a);
+  timer_end(kclass, 4.0 * a.n * a.C, stream);
+  GNN_HIP(hipGetLastError());
+  return GNN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t gnn_sample_workspace_bytes(int32_t n, int32_t C) {
+  (void)n;
+  (void)C;
+  return 0;
+}
+
+gnn_status gnn_sample_actions(int32_t n, int32_t C, const float* Z, int64_t ld_z, const float* u,
+                              double temperature, int32_t top_k, double top_p, double min_p,
+                              int32_t* action, float* logp, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream) {
+  if (n < 0 || C <= 0 || C > MOST_COLS || ld_z < C) return GNN_ERR_SHAPE;
+  if (!(temperature == 0.0 || temperature_ok(temperature)) || top_k < 0 ||
+      !(top_p > 0.0 && top_p <= 1.0) || !(min_p >= 0.0 && min_p <= 1.0))
+    return GNN_ERR_SHAPE;
+  if (n == 0) return GNN_OK;
+  if (!Z || !action || (!u && temperature > 0.0)) return GNN_ERR_NULL;
+  if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
+  const size_t need = gnn_sample_workspace_bytes(n, C);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return GNN_ERR_WORKSPACE;
+  {
+    const size_t rows = (size_t)n * 4;
+    const void* ins[] = {Z, u};
+    const size_t inb[] = {mat_bytes(n, C, ld_z), rows};
+    const void* outs[] = {action, logp, workspace};
+    const size_t outb[] = {rows, rows, need};
+    for (int i = 0; i < 3; ++i) {
+      for (int k = 0; k < 2; ++k)
+        if (ranges_overlap(outs[i], outb[i], ins[k], inb[k])) return GNN_ERR_ALIAS;
+      for (int k = 0; k < i; ++k)
+        if (ranges_overlap(outs[i], outb[i], outs[k], outb[k])) return GNN_ERR_ALIAS;
+    }
+  }
+  SampleArgs a = {};
+  a.n = n;
+  a.C = C;
+  a.Z = Z;
+  a.ld_z = ld_z;
+  a.u = u;
+  a.scale = temperature > 0.0 ? 64.0 / (temperature * 0.6931471805599453) : 0.0;
+  a.bins = temperature > 0.0 ? (float)(8.0 / temperature) : 0.f;
+  a.bits = bits_of(C);
+  a.top_k = top_k < C ? top_k : 0;
+  a.top_p = top_p;
+  a.cut = min_p > 0.0 ? temperature * std::log(min_p) : -INFINITY;
+  a.action = action;
+  a.logp = logp;
+  return run(choose<SampleArgs, SampleKernel>(C), a, GNN_K_SAMPLE, stream);
+}
+
+size_t gnn_top_workspace_bytes(int32_t n, int32_t C, int32_t k) {
+  (void)n;
+  (void)C;
+  (void)k;
+  return 0;
+}
+
+gnn_status gnn_top_logits(int32_t n, int32_t C, const float* Z, int64_t ld_z, int32_t k,
+                          double temperature, int32_t* index, float* logq, float* rest,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (n < 0 || C <= 0 || C > MOST_COLS || ld_z < C || k <= 0 || k > MOST_TOP ||
+      !temperature_ok(temperature))
+    return GNN_ERR_SHAPE;
+  if (n == 0) return GNN_OK;
+  if (!Z || !index || !logq) return GNN_ERR_NULL;
+  if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
+  const size_t need = gnn_top_workspace_bytes(n, C, k);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return GNN_ERR_WORKSPACE;
+  {
+    const void* outs[] = {index, logq, rest, workspace};
+    const size_t outb[] = {(size_t)n * k * 4, (size_t)n * k * 4, (size_t)n * 4, need};
+    for (int i = 0; i < 4; ++i) {
+      if (ranges_overlap(outs[i], outb[i], Z, mat_bytes(n, C, ld_z))) return GNN_ERR_ALIAS;
+      for (int q = 0; q < i; ++q)
+        if (ranges_overlap(outs[i], outb[i], outs[q], outb[q])) return GNN_ERR_ALIAS;
+    }
+  }
+  TopArgs a = {};
+  a.n = n;
+  a.C = C;
+  a.Z = Z;
+  a.ld_z = ld_z;
+  a.k = k;
+  a.inv_t = 1.0 / temperature;
+  a.index = index;
+  a.logq = logq;
+  a.rest = rest;
+  return run(choose<TopArgs, TopKernel>(C), a, GNN_K_SAMPLE, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,310 @@
+// The first entries of a row in its order: larger logits before smaller ones,
+// and equal ones by their columns.  A row is held by a team of lanes, and what
+// is kept of it is told by the last entry that is kept (the border).
+//
+// Amounts (1 an entry, or its weight) are whole numbers, so that their sums
+// are exact, the same in any order, and every sum over a part of the row fits
+// every other.  The border of an amount P is the entry with
+//   sum before it < P <= sum with it.
+// It is found without sorting the row: amounts are added up in bins of the
+// logits' distance from the largest, and only the entries of the bin that
+// holds the border are put in order.
+#pragma once
+
+#include "rows.hpp"
+
+namespace gnnprop {
+
+struct Border {
+  float z;
+  int32_t col;
+};
+constexpr Border NO_BORDER = {-INFINITY, 0x7fffffff};  // all are kept
+
+__device__ inline bool within(const Border& b, float z, int32_t col) {
+  return z > b.z || (z == b.z && col <= b.col);
+}
+
+// Bits whose unsigned order is the floats' (0 and -0 alike).
+__device__ inline uint32_t ordered(float z) {
+  const uint32_t x = __float_as_uint(z + 0.f);
+  return x >> 31 ? ~x : x | 0x80000000u;
+}
+// An entry's place in the order, as a number: smaller ones come first.
+__device__ inline uint64_t place(float z, int32_t col) {
+  return (uint64_t)~ordered(z) << 32 | (uint32_t)col;
+}
+
+// G lanes of a wavefront, or W whole wavefronts, that hold a row together.
+template <int G_, int W_>
+struct Team {
+  static constexpr int G = G_, W = W_, LANES = G * W;
+  static_assert(W == 1 || G == 64, "several wavefronts are whole ones");
+  // Bins, and entries that are put in order at once.
+  static constexpr int BINS = W > 1 ? 512 : G == 64 ? 256 : G == 32 ? 128 : G >= 8 ? 64 : 8 * G;
+  static constexpr int LIST = W > 1 ? 256 : G == 64 ? 128 : G == 32 ? 64 : G >= 8 ? 32 : 16;
+  static constexpr int LOG_BINS = __builtin_ctz(BINS);
+
+  struct Shared {
+    uint64_t bins[BINS];
+    uint64_t amount[LIST];
+    uint64_t place[LIST];
+    uint64_t lo, hi;
+    uint64_t sums[W];
+    float tops[W];
+    int32_t flags[W];
+    Border border;
+    int32_t count;
+  };
+
+  Shared& s;
+  const int t;     // own number in the team
+  const int lane;  // in its wavefront's part of it
+  const int wave;
+
+  __device__ Team(Shared& shared, int number)
+      : s(shared), t(number), lane(number % G), wave(number / G) {}
+
+  // What the team wrote to LDS before is there after.  (A wavefront's LDS
+  // accesses are done in their order.)
+  __device__ void sync() const {
+    if (W > 1) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  __device__ float max(float v) const {
+    v = lanes_max<G>(v);
+    if (W == 1) return v;
+    if (lane == 0) s.tops[wave] = v;
+    sync();
+    v = s.tops[0];
+    for (int k = 1; k < W; ++k) v = fmaxf(v, s.tops[k]);
+    sync();
+    return v;
+  }
+  __device__ uint64_t sum(uint64_t v) const {
+    v = lanes_sum<G>(v);
+    if (W == 1) return v;
+    if (lane == 0) s.sums[wave] = v;
+    sync();
+    v = 0;
+    for (int k = 0; k < W; ++k) v += s.sums[k];
+    sync();
+    return v;
+  }
+  __device__ double sum(double v) const {
+    v = lanes_sum<G>(v);
+    if (W == 1) return v;
+    if (lane == 0) s.sums[wave] = (uint64_t)__double_as_longlong(v);
+    sync();
+    v = 0.0;
+    for (int k = 0; k < W; ++k) v += __longlong_as_double((long long)s.sums[k]);
+    sync();
+    return v;
+  }
+  __device__ bool any(bool v) const {
+    uint64_t mine = __ballot(v);
+    if (G < 64) mine = mine >> ((threadIdx.x & 63) / G * G) & ((1ull << (G & 63)) - 1);
+    if (W == 1) return mine != 0;
+    if (lane == 0) s.flags[wave] = mine != 0;
+    sync();
+    bool r = false;
+    for (int k = 0; k < W; ++k) r |= s.flags[k] != 0;
+    sync();
+    return r;
+  }
+  // The sum over the lanes before this one, in the wavefront's part.
+  __device__ uint64_t before(uint64_t v) const {
+    uint64_t x = v;
+#pragma unroll
+    for (int d = 1; d < G; d *= 2) {
+      const uint64_t y = __shfl_up((unsigned long long)x, d, G);
+      if (lane >= d) x += y;
+    }
+    return x - v;
+  }
+
+  // The first bin with which the amounts reach P, and the amounts before it.
+  // Every wavefront finds it by itself.  False where all of them do not.
+  __device__ bool find(uint64_t P, int32_t* bin, uint64_t* base) const {
+    constexpr int EACH = BINS / G;
+    uint64_t own = 0;
+    for (int k = 0; k < EACH; ++k) own += s.bins[lane * EACH + k];
+    uint64_t sum = before(own);
+    const bool has = sum < P && sum + own >= P;
+    int32_t b = lane * EACH;
+    if (has)
+      for (uint64_t x = s.bins[b]; sum + x < P; x = s.bins[++b]) sum += x;
+    uint64_t who = __ballot(has);
+    if (G < 64) who = who >> ((threadIdx.x & 63) / G * G) & ((1ull << (G & 63)) - 1);
+    if (!who) return false;
+    const int from = __ffsll((unsigned long long)who) - 1;
+    *bin = __shfl(b, from, G);
+    *base = __shfl((unsigned long long)sum, from, G);
+    return true;
+  }
+
+  __device__ void clear() const {
+    for (int k = t; k < BINS; k += LANES) s.bins[k] = 0;
+    if (t == 0) {
+      s.count = 0;
+      s.lo = ~0ull;
+      s.hi = 0;
+    }
+    sync();
+  }
+  __device__ void add(int32_t bin, uint64_t x) const {
+    atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[bin]), (unsigned long long)x);
+  }
+  __device__ void list(float z, int32_t col, uint64_t x) const {
+    const int32_t at = atomicAdd(&s.count, 1);
+    if (at >= LIST) return;
+    s.place[at] = place(z, col);
+    s.amount[at] = x;
+  }
+  // The border among the entries listed, `base` being the amounts before them.
+  __device__ Border settle(uint64_t P, uint64_t base) const {
+    const int32_t m = s.count;
+    for (int32_t i = t; i < m; i += LANES) {
+      const uint64_t own = s.place[i], x = s.amount[i];
+      uint64_t sum = base;
+      for (int32_t j = 0; j < m; ++j) sum += s.place[j] < own ? s.amount[j] : 0;
+      if (sum < P && sum + x >= P) {
+        const uint32_t key = ~(uint32_t)(own >> 32);
+        s.border = {__uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key), (int32_t)(uint32_t)own};
+      }
+    }
+    sync();
+    return s.border;
+  }
+
+  // The border of P.  row.each(f) calls f(z, col, x) for the lane's entries,
+  // with their amounts x; bins are `scale` to a unit of z, from `top` down.
+  // NO_BORDER where the amounts do not reach P.
+  template <typename Row>
+  __device__ Border select(const Row& row, float top, float scale, uint64_t P) const {
+    const auto bin_of = [&](float z) { return (int32_t)fminf((top - z) * scale, (float)(BINS - 1)); };
+    clear();
+    row.each([&](float z, int32_t col, uint64_t x) {
+      if (x) add(bin_of(z), x);
+    });
+    sync();
+    int32_t bin = 0;
+    uint64_t base = 0;
+    if (!find(P, &bin, &base)) {
+      sync();
+      return NO_BORDER;
+    }
+    row.each([&](float z, int32_t col, uint64_t x) {
+      if (x && bin_of(z) == bin) list(z, col, x);
+    });
+    sync();
+    if (s.count <= LIST) return settle(P, base);
+    // Too many: bins of their places.  Each time the range shrinks BINS times,
+    // at last to one entry.
+    sync();
+    uint64_t lo = 0, hi = ~0ull;
+    for (bool first = true;; first = false) {
+      clear();
+      const auto member = [&](float z, int32_t col, uint64_t x) {
+        if (!x) return false;
+        if (first) return bin_of(z) == bin;
+        const uint64_t at = place(z, col);
+        return at >= lo && at <= hi;
+      };
+      row.each([&](float z, int32_t col, uint64_t x) {
+        if (!member(z, col, x)) return;
+        const unsigned long long at = place(z, col);
+        atomicMin(reinterpret_cast<unsigned long long*>(&s.lo), at);
+        atomicMax(reinterpret_cast<unsigned long long*>(&s.hi), at);
+      });
+      sync();
+      const uint64_t from = s.lo, range = s.hi - from;
+      const int shift = range < BINS ? 0 : 64 - LOG_BINS - __clzll((long long)range);
+      row.each([&](float z, int32_t col, uint64_t x) {
+        if (member(z, col, x)) add((int32_t)((place(z, col) - from) >> shift), x);
+      });
+      sync();
+      int32_t b;
+      uint64_t more = 0;
+      find(P - base, &b, &more);
+      base += more;
+      lo = from + ((uint64_t)b << shift);
+      hi = lo + ((1ull << shift) - 1);
+      row.each([&](float z, int32_t col, uint64_t x) {
+        const uint64_t at = place(z, col);
+        if (x && at >= lo && at <= hi) list(z, col, x);
+      });
+      sync();
+      if (s.count <= LIST) return settle(P, base);
+      sync();
+    }
+  }
+};
+
+// ----------------------------------------------------------------- rows
+
+// A row in the registers of its team: V chunks of four columns a lane, the
+// wavefronts' parts one after the other.
+template <int G, int W, int V>
+struct Held {
+  static constexpr int CHUNKS = V, MOST = G * W * V * 4;
+  f4 z[V];
+  int32_t first;  // column of the lane's first
+  int32_t C;
+
+  __device__ void load(const float* row, int32_t cols, int t) {
+    C = cols;
+    first = (t / G) * (G * V * 4) + t % G * 4;
+#pragma unroll
+    for (int k = 0; k < V; ++k) z[k] = load_cols(row, column(k), C);
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (column(k) - t % G * 4 + G * 4 > C) z[k] = cut_cols(z[k], column(k), C);
+  }
+  __device__ int32_t column(int k) const { return first + k * G * 4; }
+  __device__ int32_t chunks() const { return V; }
+  __device__ f4 chunk(int k) const { return z[k]; }
+};
+
+// A row that is read again for each pass over it.
+template <int G, int W>
+struct Reread {
+  static constexpr int CHUNKS = 0, MOST = MOST_COLS;
+  const float* row;
+  int32_t first, C, part;
+
+  __device__ void load(const float* from, int32_t cols, int t) {
+    row = from;
+    C = cols;
+    part = (int32_t)ceil_div(ceil_div(C, W), G * 4);
+    first = (t / G) * (part * G * 4) + t % G * 4;
+  }
+  __device__ int32_t column(int k) const { return first + k * G * 4; }
+  __device__ int32_t chunks() const { return part; }
+  __device__ f4 chunk(int k) const { return cut_cols(load_cols(row, column(k), C), column(k), C); }
+};
+
+template <class Row, class F>
+__device__ inline void each_chunk(const Row& row, F f) {
+  if constexpr (Row::CHUNKS > 0) {
+#pragma unroll
+    for (int k = 0; k < Row::CHUNKS; ++k) f(k, row.z[k]);
+  } else {
+    for (int k = 0; k < row.chunks(); ++k) f(k, row.chunk(k));
+  }
+}
+
+template <int G, int W>
+constexpr int threads_of() {
+  return W > 1 ? 64 * W : G == 1 ? 64 : 256;
+}
+
+// (written so that a NaN is refused)
+inline bool temperature_ok(double T) { return T >= 1e-6 && T <= 1e6; }
+
+}  // namespace gnnprop

@@ -29,8 +29,10 @@ GNN_LOSS_SIGMOID = 1
 KERNELS = {"spmm": 0, "spmm_reduce": 1, "gemm_nn": 2, "gemm_tn": 3,
            "gemm_nt": 4, "gemm_tt": 5, "gemm_reduce": 6, "mask": 7,
            "colsum": 8, "plan": 9, "transpose": 10, "loss": 11, "update": 12,
-           "induce": 13, "gather": 14, "sddmm": 15, "wsplit": 16, "norm": 17}
+           "induce": 13, "gather": 14, "sddmm": 15, "wsplit": 16, "norm": 17,
+           "sample": 18}
 GNN_STATE_BLOCK = 256
+GNN_TOP_MOST = 256
 GNN_NORM_ROW = 0
 GNN_NORM_SYM = 1
 GNN_PROBE_MFMA_BF16 = 0
@@ -150,6 +152,20 @@ EXPORTS = {
         ctypes.c_void_p, ctypes.c_int64] + [ctypes.c_void_p] * 5 + [ctypes.c_double] * 3
         + [ctypes.c_void_p] * 3 + [ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t,
                                    ctypes.c_void_p]),
+    "gnn_sample_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32] * 2),
+    "gnn_sample_actions": (ctypes.c_int32, [ctypes.c_int32] * 2 + [
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_double, ctypes.c_int32,
+        ctypes.c_double, ctypes.c_double] + [ctypes.c_void_p] * 3
+        + [ctypes.c_size_t, ctypes.c_void_p]),
+    "gnn_top_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32] * 3),
+    "gnn_top_logits": (ctypes.c_int32, [ctypes.c_int32] * 2 + [
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_double]
+        + [ctypes.c_void_p] * 4 + [ctypes.c_size_t, ctypes.c_void_p]),
+    "gnn_distill_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int32] * 3),
+    "gnn_distill_loss": (ctypes.c_int32, [ctypes.c_int32] * 2 + [
+        ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32] + [ctypes.c_void_p] * 4
+        + [ctypes.c_double] + [ctypes.c_void_p] * 3 + [
+            ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "gnn_params_plan_bytes": (ctypes.c_size_t, [ctypes.POINTER(gnn_params)]),
     "gnn_params_build_plan": (ctypes.c_int32, [ctypes.POINTER(gnn_params), ctypes.c_void_p,
                                                ctypes.c_size_t, ctypes.c_void_p]),
@@ -477,6 +493,41 @@ def gnn_policy_loss(n: int, C: int, Z, ld_z: int, action, advantage, old_logp, r
                                  float(clip_lo), float(clip_hi), float(beta), _ptr(out),
                                  _ptr(logp), _ptr(dZ), int(ld_dz), _ptr(workspace),
                                  _nbytes(workspace), _stream(stream)), "gnn_policy_loss")
+
+
+def gnn_sample_workspace_bytes(n: int, C: int) -> int:
+    return int(lib().gnn_sample_workspace_bytes(int(n), int(C)))
+
+
+def gnn_sample_actions(n: int, C: int, Z, ld_z: int, u, temperature: float, top_k: int,
+                       top_p: float, min_p: float, action, logp, workspace, stream=None):
+    _check(lib().gnn_sample_actions(int(n), int(C), _ptr(Z), int(ld_z), _ptr(u),
+                                    float(temperature), int(top_k), float(top_p), float(min_p),
+                                    _ptr(action), _ptr(logp), _ptr(workspace),
+                                    _nbytes(workspace), _stream(stream)), "gnn_sample_actions")
+
+
+def gnn_top_workspace_bytes(n: int, C: int, k: int) -> int:
+    return int(lib().gnn_top_workspace_bytes(int(n), int(C), int(k)))
+
+
+def gnn_top_logits(n: int, C: int, Z, ld_z: int, k: int, temperature: float, index, logq, rest,
+                   workspace, stream=None):
+    _check(lib().gnn_top_logits(int(n), int(C), _ptr(Z), int(ld_z), int(k), float(temperature),
+                                _ptr(index), _ptr(logq), _ptr(rest), _ptr(workspace),
+                                _nbytes(workspace), _stream(stream)), "gnn_top_logits")
+
+
+def gnn_distill_workspace_bytes(n: int, C: int, k: int) -> int:
+    return int(lib().gnn_distill_workspace_bytes(int(n), int(C), int(k)))
+
+
+def gnn_distill_loss(n: int, C: int, Z, ld_z: int, k: int, index, logq, rest, weight,
+                     temperature: float, out, kl, dZ, ld_dz: int, workspace, stream=None):
+    _check(lib().gnn_distill_loss(int(n), int(C), _ptr(Z), int(ld_z), int(k), _ptr(index),
+                                  _ptr(logq), _ptr(rest), _ptr(weight), float(temperature),
+                                  _ptr(out), _ptr(kl), _ptr(dZ), int(ld_dz), _ptr(workspace),
+                                  _nbytes(workspace), _stream(stream)), "gnn_distill_loss")
 
 
 def gnn_params_plan_bytes(params: gnn_params) -> int:
