@@ -46,7 +46,7 @@ struct Named {
   int32_t k, C;
   bool repeats;  // whether an index may be there twice: its first place counts
 
-  __device__ int32_t at(int32_t j) const {
+  __device__ __forceinline__ int32_t at(int32_t j) const {
     const int32_t c = index[j];
     if (c < 0 || c >= C) return -1;
     if (repeats)
@@ -68,7 +68,7 @@ struct Scalars {
 // From the sums over the entries not named: `high` their largest, `sum` of
 // exp((z - high) / T).
 template <class T>
-__device__ Scalars row_scalars(const DistillArgs& a, const T& team, const Named& named,
+__device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& team, const Named& named,
                                const float* row, float rest, float high, double sum) {
   Scalars s = {};
   float most = -INFINITY, top = high;
@@ -116,7 +116,7 @@ __device__ Scalars row_scalars(const DistillArgs& a, const T& team, const Named&
 // The gradient's values at the entries that the teacher names in columns
 // [from, to).
 template <class T>
-__device__ void named_gradient(const DistillArgs& a, const T& team, const Named& named,
+__device__ __forceinline__ void named_gradient(const DistillArgs& a, const T& team, const Named& named,
                                const float* row, const Scalars& s, double w, float* to,
                                int32_t from, int32_t end) {
   for (int32_t j = team.t; j < a.k; j += T::LANES) {
@@ -138,7 +138,7 @@ struct Others {
   bool repeats;
 
   // bits: one for each column that the team holds.
-  __device__ void load(const DistillArgs& a, const T& team, const float* from, int32_t col0,
+  __device__ __forceinline__ void load(const DistillArgs& a, const T& team, const float* from, int32_t col0,
                        const int32_t* index, uint32_t* bits) {
     row.load(from + col0, a.C - col0, team.t);
     for (int32_t k = team.t; k < (Row::MOST + 31) / 32; k += T::LANES) bits[k] = 0;
@@ -173,7 +173,7 @@ struct Others {
     }
     sum = team.sum(sum);
   }
-  __device__ void store(float* to, int32_t col0, int32_t C, float factor) const {
+  __device__ __forceinline__ void store(float* to, int32_t col0, int32_t C, float factor) const {
 #pragma unroll
     for (int k = 0; k < Row::CHUNKS; ++k) {
       f4 g = row.z[k] * factor;
@@ -183,14 +183,14 @@ struct Others {
   }
 };
 
-__device__ inline double weight_of(const DistillArgs& a, int32_t i) {
+__device__ __forceinline__ double weight_of(const DistillArgs& a, int32_t i) {
   return a.weight ? (double)a.weight[i] : a.mean;
 }
 
 // What all lanes of a team have written to memory is there before what they
 // write next.
 template <class T>
-__device__ inline void stores_done(const T& team) {
+__device__ __forceinline__ void stores_done(const T& team) {
   if (T::W > 1) __syncthreads();
   else __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
 }

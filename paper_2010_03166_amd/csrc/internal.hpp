@@ -76,16 +76,62 @@ template <int D>
 __device__ inline int32_t butterfly(int32_t x) {
   return butterfly_word<D>(x);
 }
+// The same for D of 16 and 32 as a pair, in the vector unit too: what the lower
+// lane of the two holds, and the upper.
+template <int D>
+__device__ inline uint2 both_words(int x) {
+  if (D == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return {r[0], r[1]};
+  }
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return {r[0], r[1]};
+}
+template <int D>
+__device__ inline void both(float v, float* a, float* b) {
+  const uint2 r = both_words<D>(__float_as_int(v));
+  *a = __uint_as_float(r.x);
+  *b = __uint_as_float(r.y);
+}
+template <int D>
+__device__ inline void both(int32_t v, int32_t* a, int32_t* b) {
+  const uint2 r = both_words<D>(v);
+  *a = (int32_t)r.x;
+  *b = (int32_t)r.y;
+}
+template <int D>
+__device__ inline void both(uint64_t v, uint64_t* a, uint64_t* b) {
+  const uint2 lo = both_words<D>((int)v), hi = both_words<D>((int)(v >> 32));
+  *a = (uint64_t)hi.x << 32 | lo.x;
+  *b = (uint64_t)hi.y << 32 | lo.y;
+}
+template <int D>
+__device__ inline void both(double v, double* a, double* b) {
+  uint64_t x, y;
+  both<D>((uint64_t)__double_as_longlong(v), &x, &y);
+  *a = __longlong_as_double((long long)x);
+  *b = __longlong_as_double((long long)y);
+}
 // Largest value and sum over groups of G consecutive lanes, in all of them.
 template <int G, int D = 1>
 __device__ inline float lanes_max(float v) {
-  if constexpr (D < G) return lanes_max<G, 2 * D>(fmaxf(v, butterfly<D>(v)));
-  else return v;
+  if constexpr (D >= G) return v;
+  else if constexpr (D < 16) return lanes_max<G, 2 * D>(fmaxf(v, butterfly<D>(v)));
+  else {
+    float a, b;
+    both<D>(v, &a, &b);
+    return lanes_max<G, 2 * D>(fmaxf(a, b));
+  }
 }
 template <int G, int D = 1, typename T>
 __device__ inline T lanes_sum(T v) {
-  if constexpr (D < G) return lanes_sum<G, 2 * D>(v + butterfly<D>(v));
-  else return v;
+  if constexpr (D >= G) return v;
+  else if constexpr (D < 16) return lanes_sum<G, 2 * D>(v + butterfly<D>(v));
+  else {
+    T a, b;
+    both<D>(v, &a, &b);
+    return lanes_sum<G, 2 * D>(a + b);
+  }
 }
 
 // ------------------------------------------------------------ work plan

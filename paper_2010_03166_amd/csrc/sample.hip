@@ -43,7 +43,7 @@ inline int bits_of(int32_t C) {
 // exp(d / T) in units of 2^-bits, d <= 0: with d / T in 64ths of an octave,
 // 2^(q / 64) from the table and the remainder's series (below 4e-14 of it left
 // out), added to 2^52, whose last bits the whole number then is.
-__device__ inline uint64_t weight_of(double d, double scale, int bits, const double* table) {
+__device__ __forceinline__ uint64_t weight_of(double d, double scale, int bits, const double* table) {
   constexpr double a = 0.6931471805599453 / 64.0;
   const double t = fmax(d * scale, -64.0 * 56.0);
   const double k = rint(t), f = t - k;
@@ -65,85 +65,124 @@ struct SampleArgs {
   int64_t ld_z;
   const float* u;
   double scale;  // 64 / (T ln 2); 0: the best action
-  float bins;    // bins of the logits to a unit, 8 / T
+  float inv_range;  // 1 / (T ln(C / (1 - top_p))): no border of top_p is as far from the top
   int32_t bits, top_k;
   double top_p;
-  double cut;  // T ln(min_p), or -inf
+  double cut;   // T ln(min_p), or -inf
+  double unit;  // 2^-bits where a sum of weights is that of the log-probabilities, or 0
   int32_t* action;
   float* logp;
   int64_t block0;
 };
 
-// What is kept of a row, and its entries' weights.
-template <class Row>
-struct Kept {
-  const Row& row;
-  const SampleArgs& a;
+// The weights of a row's entries, 0 for those not kept.  They are formed again
+// in each pass: a row's logits take half of the registers that weights would.
+struct Weights {
   const double* table;
-  double top;
-  Border k = NO_BORDER, p = NO_BORDER;
-  bool near = false;  // whether min-p counts
+  double scale, top;
+  int bits;
+  Border kept;
 
-  __device__ uint64_t weight(float z, int32_t col) const {
-    const double d = (double)z - top;
-    const uint64_t w = weight_of(d, a.scale, a.bits, table);
-    return within(k, z, col) && within(p, z, col) && !(near && d < a.cut) ? w : 0;
+  __device__ __forceinline__ uint64_t all(float z) const {
+    return weight_of((double)z - top, scale, bits, table);
   }
-  template <class F>
-  __device__ void each(F f) const {
-    each_chunk(row, [&](int i, f4 z) {
+  __device__ __forceinline__ uint64_t operator()(float z, int32_t col) const {
+    return within(kept, z, col) ? all(z) : 0;
+  }
+  // Of four entries; lanes without a kept one pass on.
+  __device__ __forceinline__ uint64_t sum4(f4 z, int32_t col) const {
+    bool in[4], any = false;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f(z[j], row.column(i) + j, weight(z[j], row.column(i) + j));
-    });
-  }
-  __device__ uint64_t sum4w(int i, f4 z) const {
-    uint64_t s = 0;
+    for (int j = 0; j < 4; ++j) any |= in[j] = within(kept, z[j], col + j);
+    uint64_t sum = 0;
+    if (any) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s += weight(z[j], row.column(i) + j);
-    return s;
-  }
-  __device__ uint64_t sum() const {
-    uint64_t s = 0;
-    each_chunk(row, [&](int i, f4 z) { s += sum4w(i, z); });
-    return s;
+      for (int j = 0; j < 4; ++j) sum += in[j] ? all(z[j]) : 0;
+    }
+    return sum;
   }
 };
 
-// The logits that are there, one each.
-template <class Row>
+// One for each logit that is there.
 struct Present {
-  const Row& row;
-  template <class F>
-  __device__ void each(F f) const {
-    each_chunk(row, [&](int i, f4 z) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f(z[j], row.column(i) + j, z[j] > -INFINITY);
-    });
-  }
+  __device__ __forceinline__ uint64_t operator()(float z, int32_t) const { return z > -INFINITY; }
 };
 
-__device__ inline uint64_t unit_fraction(float u) {
+// A row's largest logit, whether it is a finite number and none is a NaN; how
+// many lanes hold a logit, and the least of what they hold the largest of.
+template <class T, class Row>
+__device__ __forceinline__ bool row_range(const T& team, const Row& row, float* top, float* low,
+                                          int32_t* lanes) {
+  float most = -INFINITY;
+  bool bad = false;
+  row.each4([&](int32_t, f4 z) INLINE {
+    most = fmaxf(most, max4(z));
+    bad |= __builtin_isunordered(z.x, z.y) | __builtin_isunordered(z.z, z.w);
+  });
+  constexpr int32_t BAD = 1 << 16;
+  *top = most;
+  *low = most > -INFINITY ? most : INFINITY;
+  *lanes = (most > -INFINITY) + (bad ? BAD : 0);
+  team.range(top, low, lanes);
+  return *lanes < BAD && fabsf(*top) < INFINITY;
+}
+
+// The border of the first k entries; low and lanes from row_range().
+template <class T, class Row>
+__device__ __forceinline__ Border first_entries(const T& team, Row& row, const float* from,
+                                                int32_t C, int32_t k, float top, float low,
+                                                int32_t lanes) {
+  if (k > lanes) {  // (else as many entries as lanes are not below `low`)
+    low = INFINITY;
+    row.each([&](float z, int32_t) INLINE { low = fminf(low, z > -INFINITY ? z : INFINITY); });
+    low = -team.max(-low);
+  }
+  float scale = (T::BINS - 1) / (top - low);
+  if (!(scale < INFINITY)) scale = 0.f;
+  team.clear();
+  row.each([&](float z, int32_t) INLINE {
+    if (z >= low) team.add(T::bin_of(z, top, scale), 1);
+  });
+  team.sync();
+  Border b;
+  int32_t bin;
+  uint64_t base;
+  if (team.select(row, Present(), top, scale, k, &b, &bin, &base)) return b;
+  Reread<T::G, T::W> again;
+  again.load(from, C, team.t);
+  b = team.search(again, Present(), top, scale, bin, k, base);
+  row.load(from, C, team.t);
+  return b;
+}
+
+// The border of the entries with z - top >= cut, in doubles.
+__device__ __forceinline__ Border near_entries(float top, double cut) {
+  float z = (float)((double)top + cut);
+  while ((double)z - top < cut) z = nextafterf(z, INFINITY);
+  for (float y = nextafterf(z, -INFINITY); (double)y - top >= cut; y = nextafterf(z, -INFINITY))
+    z = y;
+  return {z, 0x7fffffff};
+}
+
+__device__ __forceinline__ Border earlier(Border a, Border b) {
+  const bool second = within(a, b.z, b.col);
+  return {second ? b.z : a.z, second ? b.col : a.col};
+}
+
+__device__ __forceinline__ uint64_t unit_fraction(float u) {
   if (!(u > 0.f)) return 0;
   if (u >= 1.f) return ~0ull;
   return (uint64_t)((double)u * 18446744073709551616.0);
 }
 
 template <class T, class Row>
-__device__ void sample_row(const SampleArgs& a, const T& team, int32_t i, const double* table) {
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, int32_t i, const double* table) {
+  const float* from = a.Z + (int64_t)i * a.ld_z;
   Row row;
-  row.load(a.Z + (int64_t)i * a.ld_z, a.C, team.t);
-  float top = -INFINITY, low = INFINITY;
-  bool bad = false;
-  each_chunk(row, [&](int, f4 z) {
-    top = fmaxf(top, max4(z));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bad |= z[j] != z[j];
-      low = fminf(low, z[j] > -INFINITY ? z[j] : INFINITY);
-    }
-  });
-  top = team.max(top);
-  if (team.any(bad) || !(fabsf(top) < INFINITY)) {
+  row.load(from, a.C, team.t);
+  float top, low;
+  int32_t lanes;
+  if (!row_range(team, row, &top, &low, &lanes)) {
     if (team.t == 0) {
       a.action[i] = -1;
       if (a.logp) a.logp[i] = 0.f;
@@ -151,34 +190,62 @@ __device__ void sample_row(const SampleArgs& a, const T& team, int32_t i, const 
     return;
   }
   double lse = 0.0;  // of the logits, from the largest
-  if (a.logp) {
-    each_chunk(row, [&](int, f4 z) { lse += (double)sum4(exp4(z, top)); });
+  if (a.logp && a.unit == 0.0) {
+    row.each4([&](int32_t, f4 z) INLINE { lse += (double)sum4(exp4(z, top)); });
     lse = log_quick((float)team.sum(lse));
   }
-  Kept<Row> kept = {row, a, table, top};
-  const Present<Row> present = {row};
-  if (a.scale == 0.0) {
-    kept.k = team.select(present, top, 0.f, 1);
+  if (a.scale == 0.0) {  // the first of the largest: a column's negative fits a float
+    float first = -INFINITY;
+    row.each([&](float z, int32_t col) INLINE {
+      first = fmaxf(first, z == top ? -(float)col : -INFINITY);
+    });
+    first = team.max(first);
     if (team.t == 0) {
-      a.action[i] = kept.k.col;
+      a.action[i] = (int32_t)-first;
       if (a.logp) a.logp[i] = (float)-lse;
     }
     return;
   }
-  if (a.top_k) {
-    const float range = top + team.max(-low);
-    const float scale = (T::BINS - 1) / range;
-    kept.k = team.select(present, top, scale < INFINITY ? scale : 0.f, (uint64_t)a.top_k);
-  }
+  Weights weight = {table, a.scale, top, a.bits, NO_BORDER};
+  if (a.top_k) weight.kept = first_entries(team, row, from, a.C, a.top_k, top, low, lanes);
   if (a.top_p < 1.0) {
-    const uint64_t all = team.sum(kept.sum());
-    const uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
-    kept.p = team.select(kept, top, a.bins, P < 1 ? 1 : P < all ? P : all);
+    const float scale = (T::BINS - 1) * a.inv_range;
+    uint64_t all = 0;
+    team.clear();
+    const auto fill = [&](float z, uint64_t w) INLINE {
+      all += w;
+      if (w) team.add(T::bin_of(z, top, scale), w);
+    };
+    if (a.top_k) row.each([&](float z, int32_t col) INLINE { fill(z, weight(z, col)); });
+    else row.each([&](float z, int32_t) INLINE { fill(z, weight.all(z)); });
+    all = team.sum(all);
+    team.sync();
+    if (a.unit > 0.0) lse = log_quick((float)((double)all * a.unit));
+    uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
+    P = P < 1 ? 1 : P < all ? P : all;
+    Border b;
+    int32_t bin;
+    uint64_t base;
+    if (!team.select(row, weight, top, scale, P, &b, &bin, &base)) {
+      Reread<T::G, T::W> again;
+      again.load(from, a.C, team.t);
+      b = team.search(again, weight, top, scale, bin, P, base);
+      row.load(from, a.C, team.t);
+    }
+    weight.kept = b;
   }
-  kept.near = true;
+  if (a.cut > -INFINITY) weight.kept = earlier(weight.kept, near_entries(top, a.cut));
   // the action that holds the random number's share of the sum
-  const uint64_t own = lanes_sum<T::G>(kept.sum());
-  uint64_t all = own, ahead = 0;
+  constexpr int KEPT = Row::CHUNKS > 0 ? Row::CHUNKS : 1;
+  uint64_t own = 0, sums[KEPT];
+  int at_chunk = 0;
+  row.each4([&](int32_t col, f4 z) INLINE {
+    const uint64_t sum = weight.sum4(z, col);
+    own += sum;
+    if (Row::CHUNKS > 0) sums[at_chunk++] = sum;
+  });
+  own = lanes_sum<T::G>(own);
+  uint64_t ahead = 0, all = own;
   if (T::W > 1) {
     if (team.lane == 0) team.s.sums[team.wave] = own;
     team.sync();
@@ -187,34 +254,51 @@ __device__ void sample_row(const SampleArgs& a, const T& team, int32_t i, const 
       all += team.s.sums[k];
       if (k < team.wave) ahead += team.s.sums[k];
     }
-    team.sync();
   }
+  if (a.unit > 0.0 && a.top_p == 1.0) lse = log_quick((float)((double)all * a.unit));
   uint64_t target = __umul64hi(all, unit_fraction(a.u[i]));
   if (target < ahead || target >= ahead + own) return;
   target -= ahead;
-  for (int k = 0; k < row.chunks(); ++k) {
-    const f4 z = row.chunk(k);
-    const uint64_t mine = kept.sum4w(k, z), sum = lanes_sum<T::G>(mine);
-    if (target >= sum) {
+  // its chunks of the wavefront, one after the other
+  bool found = false;
+  at_chunk = 0;
+  int32_t col = 0;
+  f4 z = {};
+  row.each4([&](int32_t at, f4 v) INLINE {
+    uint64_t sum = 0;
+    if (Row::CHUNKS > 0) sum = sums[at_chunk++];
+    if (found) return;
+    if (Row::CHUNKS == 0) sum = weight.sum4(v, at);
+    sum = lanes_sum<T::G>(sum);
+    found = target < sum;
+    if (!found) {
       target -= sum;
-      continue;
+      return;
     }
-    uint64_t x = team.before(mine);
-    if (target < x || target >= x + mine) break;
-    for (int j = 0; j < 4; ++j) {
-      x += kept.weight(z[j], row.column(k) + j);
-      if (target < x) {
-        a.action[i] = row.column(k) + j;
-        if (a.logp) a.logp[i] = (float)((double)z[j] - top - lse);
-        break;
-      }
-    }
-    break;
+    col = at;
+    z = v;
+  });
+  const uint64_t w0 = weight(z.x, col), w1 = weight(z.y, col + 1), w2 = weight(z.z, col + 2),
+                 mine = w0 + w1 + w2 + weight(z.w, col + 3), x = team.before(mine);
+  if (target < x || target >= x + mine) return;
+  target -= x;
+  const int j = target < w0 ? 0 : target < w0 + w1 ? 1 : target < w0 + w1 + w2 ? 2 : 3;
+  a.action[i] = col + j;
+  if (a.logp) {
+    const float za = j == 0 ? z.x : j == 1 ? z.y : j == 2 ? z.z : z.w;
+    a.logp[i] = (float)((double)za - top - lse);
   }
 }
 
+// Blocks that share a CU, by the registers that a row takes.
 template <int G, int W, class Row>
-__global__ __launch_bounds__((threads_of<G, W>())) void sample_kernel(SampleArgs a) {
+constexpr int blocks_of() {
+  const int waves = W < 16 && Row::CHUNKS > 4 ? 12 : 16;  // of a CU
+  return waves * 64 / threads_of<G, W>();
+}
+
+template <int G, int W, class Row>
+__global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>())) void sample_kernel(SampleArgs a) {
   using T = Team<G, W>;
   constexpr int R = threads_of<G, W>() / T::LANES;
   __shared__ typename T::Shared s[R];
@@ -244,28 +328,19 @@ struct TopArgs {
 };
 
 // Exponentials of entries, from the largest.
-__device__ inline float tempered(float z, float top, float inv_t) {
+__device__ __forceinline__ float tempered(float z, float top, float inv_t) {
   return z == -INFINITY ? 0.f : expf((z - top) * inv_t);
 }
 
 template <class T, class Row>
-__device__ void top_row(const TopArgs& a, const T& team, uint64_t* list, int32_t i) {
+__device__ __forceinline__ void top_row(const TopArgs& a, const T& team, uint64_t* list, int32_t i) {
   Row row;
   row.load(a.Z + (int64_t)i * a.ld_z, a.C, team.t);
   int32_t* index = a.index + (int64_t)i * a.k;
   float* logq = a.logq + (int64_t)i * a.k;
-  float top = -INFINITY, low = INFINITY;
-  bool bad = false;
-  each_chunk(row, [&](int, f4 z) {
-    top = fmaxf(top, max4(z));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      bad |= z[j] != z[j];
-      low = fminf(low, z[j] > -INFINITY ? z[j] : INFINITY);
-    }
-  });
-  top = team.max(top);
-  if (team.any(bad) || !(fabsf(top) < INFINITY)) {
+  float top, low;
+  int32_t lanes;
+  if (!row_range(team, row, &top, &low, &lanes)) {
     for (int32_t j = team.t; j < a.k; j += T::LANES) {
       index[j] = -1;
       logq[j] = -INFINITY;
@@ -273,20 +348,18 @@ __device__ void top_row(const TopArgs& a, const T& team, uint64_t* list, int32_t
     if (team.t == 0 && a.rest) a.rest[i] = 0.f;
     return;
   }
-  const float range = top + team.max(-low);
-  const float scale = (T::BINS - 1) / range;
-  const Border b = team.select(Present<Row>{row}, top, scale < INFINITY ? scale : 0.f,
-                               (uint64_t)a.k);
+  const Border b = first_entries(team, row, a.Z + (int64_t)i * a.ld_z, a.C, a.k, top, low,
+                                 lanes);
   // the entries kept, and the sums of both parts
   if (team.t == 0) team.s.count = 0;
   team.sync();
   const float inv_t = (float)a.inv_t;
   double in = 0.0, out = 0.0;
-  each_chunk(row, [&](int c, f4 z) {
+  row.each4([&](int32_t at, f4 z) INLINE {
     float more = 0.f, less = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int32_t col = row.column(c) + j;
+      const int32_t col = at + j;
       const float e = tempered(z[j], top, inv_t);
       if (z[j] > -INFINITY && within(b, z[j], col)) {
         more += e;
@@ -443,11 +516,14 @@ gnn_status gnn_sample_actions(int32_t n, int32_t C, const float* Z, int64_t ld_z
   a.ld_z = ld_z;
   a.u = u;
   a.scale = temperature > 0.0 ? 64.0 / (temperature * 0.6931471805599453) : 0.0;
-  a.bins = temperature > 0.0 ? (float)(8.0 / temperature) : 0.f;
+  a.inv_range = top_p < 1.0 && temperature > 0.0
+                    ? (float)(1.0 / (temperature * std::log(C / (1.0 - top_p)))) : 0.f;
   a.bits = bits_of(C);
   a.top_k = top_k < C ? top_k : 0;
   a.top_p = top_p;
   a.cut = min_p > 0.0 ? temperature * std::log(min_p) : -INFINITY;
+  a.unit = temperature == 1.0 && logp && !a.top_k && (top_p < 1.0 || min_p == 0.0)
+               ? std::ldexp(1.0, -a.bits) : 0.0;
   a.action = action;
   a.logp = logp;
   return run(choose<SampleArgs, SampleKernel>(C), a, GNN_K_SAMPLE, stream);

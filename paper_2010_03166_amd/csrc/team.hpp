@@ -13,6 +13,9 @@
 
 #include "rows.hpp"
 
+// (a lambda; left to itself the compiler calls some, and a row goes to the stack)
+#define INLINE __attribute__((always_inline))
+
 namespace gnnprop {
 
 struct Border {
@@ -21,18 +24,27 @@ struct Border {
 };
 constexpr Border NO_BORDER = {-INFINITY, 0x7fffffff};  // all are kept
 
-__device__ inline bool within(const Border& b, float z, int32_t col) {
+__device__ __forceinline__ bool within(const Border& b, float z, int32_t col) {
   return z > b.z || (z == b.z && col <= b.col);
 }
 
 // Bits whose unsigned order is the floats' (0 and -0 alike).
-__device__ inline uint32_t ordered(float z) {
+__device__ __forceinline__ uint32_t ordered(float z) {
   const uint32_t x = __float_as_uint(z + 0.f);
   return x >> 31 ? ~x : x | 0x80000000u;
 }
 // An entry's place in the order, as a number: smaller ones come first.
-__device__ inline uint64_t place(float z, int32_t col) {
+__device__ __forceinline__ uint64_t place(float z, int32_t col) {
   return (uint64_t)~ordered(z) << 32 | (uint32_t)col;
+}
+
+// v, as values that nothing computed from them before is kept for: what a later
+// pass over a row in registers needs of them is formed again, since the row
+// leaves few registers.
+template <typename T>
+__device__ __forceinline__ T fresh(T v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // G lanes of a wavefront, or W whole wavefronts, that hold a row together.
@@ -51,7 +63,7 @@ struct Team {
     uint64_t place[LIST];
     uint64_t lo, hi;
     uint64_t sums[W];
-    float tops[W];
+    float tops[W], lows[W];
     int32_t flags[W];
     Border border;
     int32_t count;
@@ -62,12 +74,12 @@ struct Team {
   const int lane;  // in its wavefront's part of it
   const int wave;
 
-  __device__ Team(Shared& shared, int number)
+  __device__ __forceinline__ Team(Shared& shared, int number)
       : s(shared), t(number), lane(number % G), wave(number / G) {}
 
   // What the team wrote to LDS before is there after.  (A wavefront's LDS
   // accesses are done in their order.)
-  __device__ void sync() const {
+  __device__ __forceinline__ void sync() const {
     if (W > 1) {
       __syncthreads();
     } else {
@@ -76,7 +88,7 @@ struct Team {
     }
   }
 
-  __device__ float max(float v) const {
+  __device__ __forceinline__ float max(float v) const {
     v = lanes_max<G>(v);
     if (W == 1) return v;
     if (lane == 0) s.tops[wave] = v;
@@ -86,7 +98,32 @@ struct Team {
     sync();
     return v;
   }
-  __device__ uint64_t sum(uint64_t v) const {
+  // The largest and the least value, and the sum of small numbers.
+  __device__ __forceinline__ void range(float* high, float* low, int32_t* number) const {
+    float h = lanes_max<G>(*high), l = -lanes_max<G>(-*low);
+    int32_t m = lanes_sum<G>(*number);
+    if (W > 1) {
+      if (lane == 0) {
+        s.tops[wave] = h;
+        s.lows[wave] = l;
+        s.flags[wave] = m;
+      }
+      sync();
+      h = s.tops[0];
+      l = s.lows[0];
+      m = s.flags[0];
+      for (int k = 1; k < W; ++k) {
+        h = fmaxf(h, s.tops[k]);
+        l = fminf(l, s.lows[k]);
+        m += s.flags[k];
+      }
+      sync();
+    }
+    *high = h;
+    *low = l;
+    *number = m;
+  }
+  __device__ __forceinline__ uint64_t sum(uint64_t v) const {
     v = lanes_sum<G>(v);
     if (W == 1) return v;
     if (lane == 0) s.sums[wave] = v;
@@ -96,7 +133,7 @@ struct Team {
     sync();
     return v;
   }
-  __device__ double sum(double v) const {
+  __device__ __forceinline__ double sum(double v) const {
     v = lanes_sum<G>(v);
     if (W == 1) return v;
     if (lane == 0) s.sums[wave] = (uint64_t)__double_as_longlong(v);
@@ -106,7 +143,7 @@ struct Team {
     sync();
     return v;
   }
-  __device__ bool any(bool v) const {
+  __device__ __forceinline__ bool any(bool v) const {
     uint64_t mine = __ballot(v);
     if (G < 64) mine = mine >> ((threadIdx.x & 63) / G * G) & ((1ull << (G & 63)) - 1);
     if (W == 1) return mine != 0;
@@ -118,7 +155,7 @@ struct Team {
     return r;
   }
   // The sum over the lanes before this one, in the wavefront's part.
-  __device__ uint64_t before(uint64_t v) const {
+  __device__ __forceinline__ uint64_t before(uint64_t v) const {
     uint64_t x = v;
 #pragma unroll
     for (int d = 1; d < G; d *= 2) {
@@ -130,7 +167,7 @@ struct Team {
 
   // The first bin with which the amounts reach P, and the amounts before it.
   // Every wavefront finds it by itself.  False where all of them do not.
-  __device__ bool find(uint64_t P, int32_t* bin, uint64_t* base) const {
+  __device__ __forceinline__ bool find(uint64_t P, int32_t* bin, uint64_t* base) const {
     constexpr int EACH = BINS / G;
     uint64_t own = 0;
     for (int k = 0; k < EACH; ++k) own += s.bins[lane * EACH + k];
@@ -148,7 +185,7 @@ struct Team {
     return true;
   }
 
-  __device__ void clear() const {
+  __device__ __forceinline__ void clear() const {
     for (int k = t; k < BINS; k += LANES) s.bins[k] = 0;
     if (t == 0) {
       s.count = 0;
@@ -157,17 +194,17 @@ struct Team {
     }
     sync();
   }
-  __device__ void add(int32_t bin, uint64_t x) const {
+  __device__ __forceinline__ void add(int32_t bin, uint64_t x) const {
     atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[bin]), (unsigned long long)x);
   }
-  __device__ void list(float z, int32_t col, uint64_t x) const {
+  __device__ __forceinline__ void list(float z, int32_t col, uint64_t x) const {
     const int32_t at = atomicAdd(&s.count, 1);
     if (at >= LIST) return;
     s.place[at] = place(z, col);
     s.amount[at] = x;
   }
   // The border among the entries listed, `base` being the amounts before them.
-  __device__ Border settle(uint64_t P, uint64_t base) const {
+  __device__ __forceinline__ Border settle(uint64_t P, uint64_t base) const {
     const int32_t m = s.count;
     for (int32_t i = t; i < m; i += LANES) {
       const uint64_t own = s.place[i], x = s.amount[i];
@@ -182,42 +219,53 @@ struct Team {
     return s.border;
   }
 
-  // The border of P.  row.each(f) calls f(z, col, x) for the lane's entries,
-  // with their amounts x; bins are `scale` to a unit of z, from `top` down.
-  // NO_BORDER where the amounts do not reach P.
-  template <typename Row>
-  __device__ Border select(const Row& row, float top, float scale, uint64_t P) const {
-    const auto bin_of = [&](float z) { return (int32_t)fminf((top - z) * scale, (float)(BINS - 1)); };
-    clear();
-    row.each([&](float z, int32_t col, uint64_t x) {
-      if (x) add(bin_of(z), x);
-    });
-    sync();
-    int32_t bin = 0;
-    uint64_t base = 0;
-    if (!find(P, &bin, &base)) {
+  // The border of P, once the amounts are in their bins and the team has met:
+  // row.each(f) calls f(z, col) for the lane's entries, amount(z, col) is what
+  // one adds, bins are `scale` to a unit of z, from `top` down.  NO_BORDER where
+  // the amounts do not reach P.  False where a bin holds more entries than are
+  // put in order at once: *bin and *base are for search() then.
+  template <typename Row, typename Amount>
+  __device__ __forceinline__ bool select(const Row& row, Amount amount, float top, float scale, uint64_t P,
+                         Border* border, int32_t* bin, uint64_t* base) const {
+    if (!find(P, bin, base)) {
+      *border = NO_BORDER;
       sync();
-      return NO_BORDER;
+      return true;
     }
-    row.each([&](float z, int32_t col, uint64_t x) {
-      if (x && bin_of(z) == bin) list(z, col, x);
+    row.each([&](float z, int32_t col) INLINE {
+      if (bin_of(z, top, scale) != *bin) return;
+      const uint64_t x = amount(z, col);
+      if (x) list(z, col, x);
     });
     sync();
-    if (s.count <= LIST) return settle(P, base);
-    // Too many: bins of their places.  Each time the range shrinks BINS times,
-    // at last to one entry.
-    sync();
+    if (s.count > LIST) {
+      sync();
+      return false;
+    }
+    *border = settle(P, *base);
+    return true;
+  }
+
+  __device__ __forceinline__ static int32_t bin_of(float z, float top, float scale) {
+    return (int32_t)fminf((top - z) * scale, (float)(BINS - 1));
+  }
+
+  // The border in a bin of many entries: by bins of their places, whose range
+  // shrinks BINS times in each turn, at last to one entry.  (The row is one that
+  // is read again, so that a row in registers need not be kept for it.)
+  template <typename Row, typename Amount>
+  __device__ __forceinline__ Border search(const Row& row, Amount amount, float top, float scale, int32_t bin,
+                           uint64_t P, uint64_t base) const {
     uint64_t lo = 0, hi = ~0ull;
     for (bool first = true;; first = false) {
       clear();
-      const auto member = [&](float z, int32_t col, uint64_t x) {
-        if (!x) return false;
-        if (first) return bin_of(z) == bin;
+      const auto member = [&](float z, int32_t col) INLINE {
+        if (first) return bin_of(z, top, scale) == bin;
         const uint64_t at = place(z, col);
         return at >= lo && at <= hi;
       };
-      row.each([&](float z, int32_t col, uint64_t x) {
-        if (!member(z, col, x)) return;
+      row.each([&](float z, int32_t col) INLINE {
+        if (!member(z, col) || !amount(z, col)) return;
         const unsigned long long at = place(z, col);
         atomicMin(reinterpret_cast<unsigned long long*>(&s.lo), at);
         atomicMax(reinterpret_cast<unsigned long long*>(&s.hi), at);
@@ -225,8 +273,10 @@ struct Team {
       sync();
       const uint64_t from = s.lo, range = s.hi - from;
       const int shift = range < BINS ? 0 : 64 - LOG_BINS - __clzll((long long)range);
-      row.each([&](float z, int32_t col, uint64_t x) {
-        if (member(z, col, x)) add((int32_t)((place(z, col) - from) >> shift), x);
+      row.each([&](float z, int32_t col) INLINE {
+        if (!member(z, col)) return;
+        const uint64_t x = amount(z, col);
+        if (x) add((int32_t)((place(z, col) - from) >> shift), x);
       });
       sync();
       int32_t b;
@@ -235,9 +285,11 @@ struct Team {
       base += more;
       lo = from + ((uint64_t)b << shift);
       hi = lo + ((1ull << shift) - 1);
-      row.each([&](float z, int32_t col, uint64_t x) {
+      row.each([&](float z, int32_t col) INLINE {
         const uint64_t at = place(z, col);
-        if (x && at >= lo && at <= hi) list(z, col, x);
+        if (at < lo || at > hi) return;
+        const uint64_t x = amount(z, col);
+        if (x) list(z, col, x);
       });
       sync();
       if (s.count <= LIST) return settle(P, base);
@@ -257,18 +309,35 @@ struct Held {
   int32_t first;  // column of the lane's first
   int32_t C;
 
-  __device__ void load(const float* row, int32_t cols, int t) {
+  __device__ __forceinline__ void load(const float* row, int32_t cols, int t) {
     C = cols;
     first = (t / G) * (G * V * 4) + t % G * 4;
 #pragma unroll
-    for (int k = 0; k < V; ++k) z[k] = load_cols(row, column(k), C);
+    for (int k = 0; k < V; ++k)  // (rows of more than one chunk have at least four columns)
+      z[k] = MOST > 4 ? *reinterpret_cast<const f4u*>(row + min(column(k), C - 4))
+                      : load_cols(row, column(k), C);
 #pragma unroll
     for (int k = 0; k < V; ++k)
       if (column(k) - t % G * 4 + G * 4 > C) z[k] = cut_cols(z[k], column(k), C);
   }
-  __device__ int32_t column(int k) const { return first + k * G * 4; }
-  __device__ int32_t chunks() const { return V; }
-  __device__ f4 chunk(int k) const { return z[k]; }
+  __device__ __forceinline__ int32_t column(int k) const { return first + k * G * 4; }
+  // f(column, its and the next three logits) for the lane's chunks
+  template <class F>
+  __device__ __forceinline__ void each4(F f) const {
+    const int32_t at = fresh(first);
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      f(at + k * G * 4, fresh(z[k]));
+      __builtin_amdgcn_sched_barrier(0);  // (what is formed of one chunk only has registers)
+    }
+  }
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    each4([&](int32_t col, f4 v) INLINE {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(v[j], col + j);
+    });
+  }
 };
 
 // A row that is read again for each pass over it.
@@ -278,26 +347,26 @@ struct Reread {
   const float* row;
   int32_t first, C, part;
 
-  __device__ void load(const float* from, int32_t cols, int t) {
+  __device__ __forceinline__ void load(const float* from, int32_t cols, int t) {
     row = from;
     C = cols;
     part = (int32_t)ceil_div(ceil_div(C, W), G * 4);
     first = (t / G) * (part * G * 4) + t % G * 4;
   }
-  __device__ int32_t column(int k) const { return first + k * G * 4; }
-  __device__ int32_t chunks() const { return part; }
-  __device__ f4 chunk(int k) const { return cut_cols(load_cols(row, column(k), C), column(k), C); }
-};
-
-template <class Row, class F>
-__device__ inline void each_chunk(const Row& row, F f) {
-  if constexpr (Row::CHUNKS > 0) {
-#pragma unroll
-    for (int k = 0; k < Row::CHUNKS; ++k) f(k, row.z[k]);
-  } else {
-    for (int k = 0; k < row.chunks(); ++k) f(k, row.chunk(k));
+  __device__ __forceinline__ int32_t column(int k) const { return first + k * G * 4; }
+  template <class F>
+  __device__ __forceinline__ void each4(F f) const {
+#pragma unroll 1
+    for (int k = 0; k < part; ++k) f(column(k), cut_cols(load_cols(row, column(k), C), column(k), C));
   }
-}
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    each4([&](int32_t col, f4 v) INLINE {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(v[j], col + j);
+    });
+  }
+};
 
 template <int G, int W>
 constexpr int threads_of() {
