@@ -42,20 +42,42 @@ inline int bits_of(int32_t C) {
 
 // exp(d / T) in units of 2^-bits, d <= 0: with d / T in 64ths of an octave,
 // 2^(q / 64) from the table and the remainder's series (below 4e-14 of it left
-// out), added to 2^52, whose last bits the whole number then is.
-__device__ __forceinline__ uint64_t weight_of(double d, double scale, int bits, const double* table) {
-  constexpr double a = 0.6931471805599453 / 64.0;
-  const double t = fmax(d * scale, -64.0 * 56.0);
-  const double k = rint(t), f = t - k;
-  const int q = (int)k;
-  double p = fma(f, a * a * a * a / 24.0, a * a * a / 6.0);
-  p = fma(p, f, a * a / 2.0);
-  p = fma(p, f, a);
-  p = fma(p, f, 1.0);
-  const uint64_t unit = (uint64_t)__double_as_longlong(table[q & 63]);
-  const double e = __longlong_as_double((long long)(unit + ((uint64_t)(int64_t)((q >> 6) + bits) << 52)));
-  return (uint64_t)__double_as_longlong(fma(e, p, 4503599627370496.0)) & 0xfffffffffffffull;
-}
+// out), added to 2^52, whose last bits the whole number then is.  The numbers
+// are kept in scalar registers: as literals they took two moves a step.
+struct Exponential {
+  const double* table;
+  double scale;
+  int bits;
+  double c1, c2, c3, c4, one52;
+
+  __device__ __forceinline__ Exponential(const double* t, double s, int b)
+      : table(t), scale(s), bits(b) {
+    constexpr double a = 0.6931471805599453 / 64.0;
+    c1 = scalar(a);
+    c2 = scalar(a * a / 2.0);
+    c3 = scalar(a * a * a / 6.0);
+    c4 = a * a * a * a / 24.0;
+    asm("" : "+v"(c4));  // (an instruction reads one of the others)
+    one52 = scalar(4503599627370496.0);
+  }
+  static __device__ __forceinline__ double scalar(double x) {
+    asm("" : "+s"(x));
+    return x;
+  }
+  __device__ __forceinline__ uint64_t operator()(double d) const {
+    const double t = fmax(d * scale, -64.0 * 56.0);
+    const double k = rint(t), f = t - k;
+    const int q = (int)k;
+    double p = fma(f, c4, c3);
+    p = fma(p, f, c2);
+    p = fma(p, f, c1);
+    p = fma(p, f, 1.0);
+    const uint64_t unit = (uint64_t)__double_as_longlong(table[q & 63]);
+    const uint32_t hi = (uint32_t)(unit >> 32) + ((uint32_t)((q >> 6) + bits) << 20);
+    const double e = __longlong_as_double((long long)((uint64_t)hi << 32 | (uint32_t)unit));
+    return (uint64_t)__double_as_longlong(fma(e, p, one52)) & 0xfffffffffffffull;
+  }
+};
 
 // ------------------------------------------------------------------ draws
 
@@ -78,27 +100,28 @@ struct SampleArgs {
 // The weights of a row's entries, 0 for those not kept.  They are formed again
 // in each pass: a row's logits take half of the registers that weights would.
 struct Weights {
-  const double* table;
-  double scale, top;
-  int bits;
+  Exponential of;
+  double top;
   Border kept;
 
   __device__ __forceinline__ uint64_t all(float z) const {
-    return weight_of((double)z - top, scale, bits, table);
+    return of((double)z - top);
   }
   __device__ __forceinline__ uint64_t operator()(float z, int32_t col) const {
-    return within(kept, z, col) ? all(z) : 0;
+    const uint64_t w = all(z);
+    return within(kept, z, col) ? w : 0;
   }
-  // Of four entries; lanes without a kept one pass on.
+  // Of four entries, formed side by side; lanes without a kept one pass on.
   __device__ __forceinline__ uint64_t sum4(f4 z, int32_t col) const {
     bool in[4], any = false;
 #pragma unroll
     for (int j = 0; j < 4; ++j) any |= in[j] = within(kept, z[j], col + j);
-    uint64_t sum = 0;
-    if (any) {
+    if (!any) return 0;
+    uint64_t w[4], sum = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sum += in[j] ? all(z[j]) : 0;
-    }
+    for (int j = 0; j < 4; ++j) w[j] = all(z[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += in[j] ? w[j] : 0;
     return sum;
   }
 };
@@ -141,7 +164,7 @@ __device__ __forceinline__ Border first_entries(const T& team, Row& row, const f
   if (!(scale < INFINITY)) scale = 0.f;
   team.clear();
   row.each([&](float z, int32_t) INLINE {
-    if (z >= low) team.add(T::bin_of(z, top, scale), 1);
+    team.add(T::bin_of(z, top, scale), 1, z >= low);
   });
   team.sync();
   Border b;
@@ -206,18 +229,34 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
     }
     return;
   }
-  Weights weight = {table, a.scale, top, a.bits, NO_BORDER};
+  Weights weight = {Exponential(table, a.scale, a.bits), top, NO_BORDER};
   if (a.top_k) weight.kept = first_entries(team, row, from, a.C, a.top_k, top, low, lanes);
   if (a.top_p < 1.0) {
     const float scale = (T::BINS - 1) * a.inv_range;
     uint64_t all = 0;
     team.clear();
-    const auto fill = [&](float z, uint64_t w) INLINE {
-      all += w;
-      if (w) team.add(T::bin_of(z, top, scale), w);
+    const auto fill = [&](f4 z, const uint64_t (&w)[4]) INLINE {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        all += w[j];
+        team.add(T::bin_of(z[j], top, scale), w[j], w[j] != 0);
+      }
     };
-    if (a.top_k) row.each([&](float z, int32_t col) INLINE { fill(z, weight(z, col)); });
-    else row.each([&](float z, int32_t) INLINE { fill(z, weight.all(z)); });
+    if (a.top_k) {
+      row.each4([&](int32_t col, f4 z) INLINE {
+        uint64_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = weight(z[j], col + j);
+        fill(z, w);
+      });
+    } else {
+      row.each4([&](int32_t, f4 z) INLINE {
+        uint64_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = weight.all(z[j]);
+        fill(z, w);
+      });
+    }
     all = team.sum(all);
     team.sync();
     if (a.unit > 0.0) lse = log_quick((float)((double)all * a.unit));

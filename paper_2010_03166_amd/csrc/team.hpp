@@ -25,7 +25,7 @@ struct Border {
 constexpr Border NO_BORDER = {-INFINITY, 0x7fffffff};  // all are kept
 
 __device__ __forceinline__ bool within(const Border& b, float z, int32_t col) {
-  return z > b.z || (z == b.z && col <= b.col);
+  return (z > b.z) | ((z == b.z) & (col <= b.col));
 }
 
 // Bits whose unsigned order is the floats' (0 and -0 alike).
@@ -38,13 +38,12 @@ __device__ __forceinline__ uint64_t place(float z, int32_t col) {
   return (uint64_t)~ordered(z) << 32 | (uint32_t)col;
 }
 
-// v, as values that nothing computed from them before is kept for: what a later
-// pass over a row in registers needs of them is formed again, since the row
-// leaves few registers.
+// Makes v a value that nothing computed from it before is kept for: what a later
+// pass over a row in registers needs of it is formed again, since the row leaves
+// few registers.
 template <typename T>
-__device__ __forceinline__ T fresh(T v) {
+__device__ __forceinline__ void refresh(T& v) {
   asm volatile("" : "+v"(v));
-  return v;
 }
 
 // G lanes of a wavefront, or W whole wavefronts, that hold a row together.
@@ -58,7 +57,7 @@ struct Team {
   static constexpr int LOG_BINS = __builtin_ctz(BINS);
 
   struct Shared {
-    uint64_t bins[BINS];
+    uint64_t bins[BINS + G];  // (the last G, one a lane, for entries that are in none)
     uint64_t amount[LIST];
     uint64_t place[LIST];
     uint64_t lo, hi;
@@ -154,15 +153,25 @@ struct Team {
     sync();
     return r;
   }
-  // The sum over the lanes before this one, in the wavefront's part.
+  // The sum over the lanes before this one, in the wavefront's part: within
+  // rows of 16 lanes, then the last lanes of rows added to the rows after them.
   __device__ __forceinline__ uint64_t before(uint64_t v) const {
     uint64_t x = v;
-#pragma unroll
-    for (int d = 1; d < G; d *= 2) {
-      const uint64_t y = __shfl_up((unsigned long long)x, d, G);
-      if (lane >= d) x += y;
-    }
+    if (G > 1) x = shifted<0x111, 0xF, 1>(x);
+    if (G > 2) x = shifted<0x112, 0xF, 2>(x);
+    if (G > 4) x = shifted<0x114, 0xF, 4>(x);
+    if (G > 8) x = shifted<0x118, 0xF, 8>(x);
+    if (G > 16) x = shifted<0x142, 0xA, 0>(x);
+    if (G > 32) x = shifted<0x143, 0xC, 0>(x);
     return x - v;
+  }
+  template <int CTRL, int ROWS, int D>
+  __device__ __forceinline__ uint64_t shifted(uint64_t x) const {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xF, false);
+    const uint64_t y = (uint64_t)hi << 32 | lo;
+    // (a row of 16 lanes holds several teams)
+    return G >= 16 || lane >= D ? x + y : x;
   }
 
   // The first bin with which the amounts reach P, and the amounts before it.
@@ -193,6 +202,10 @@ struct Team {
       s.hi = 0;
     }
     sync();
+  }
+  // (without a branch: what is to be in no bin goes to the lane's own place)
+  __device__ __forceinline__ void add(int32_t bin, uint64_t x, bool in) const {
+    add(in ? bin : BINS + lane, x);
   }
   __device__ __forceinline__ void add(int32_t bin, uint64_t x) const {
     atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[bin]), (unsigned long long)x);
@@ -232,10 +245,16 @@ struct Team {
       sync();
       return true;
     }
-    row.each([&](float z, int32_t col) INLINE {
-      if (bin_of(z, top, scale) != *bin) return;
-      const uint64_t x = amount(z, col);
-      if (x) list(z, col, x);
+    row.each4([&](int32_t col, f4 z) INLINE {
+      bool in[4], any = false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) any |= in[j] = bin_of(z[j], top, scale) == *bin;
+      if (!any) return;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t x = in[j] ? amount(z[j], col + j) : 0;
+        if (x) list(z[j], col + j, x);
+      }
     });
     sync();
     if (s.count > LIST) {
@@ -305,8 +324,8 @@ struct Team {
 template <int G, int W, int V>
 struct Held {
   static constexpr int CHUNKS = V, MOST = G * W * V * 4;
-  f4 z[V];
-  int32_t first;  // column of the lane's first
+  mutable f4 z[V];
+  mutable int32_t first;  // column of the lane's first
   int32_t C;
 
   __device__ __forceinline__ void load(const float* row, int32_t cols, int t) {
@@ -324,10 +343,11 @@ struct Held {
   // f(column, its and the next three logits) for the lane's chunks
   template <class F>
   __device__ __forceinline__ void each4(F f) const {
-    const int32_t at = fresh(first);
+    refresh(first);
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      f(at + k * G * 4, fresh(z[k]));
+      refresh(z[k]);
+      f(column(k), z[k]);
       __builtin_amdgcn_sched_barrier(0);  // (what is formed of one chunk only has registers)
     }
   }
