@@ -39,6 +39,23 @@ struct DistillArgs {
   int64_t blocks, block0;  // of all launches, and in the launches before
 };
 
+// ln(x), x > 0, to a few 2^-53: k ln 2 + 2 atanh((m - 1) / (m + 1)) for
+// 0.7 < m < 1.42 (the first term left out is below 1e-16).
+__device__ __forceinline__ double log_of(double x) {
+  if (!(x < INFINITY)) return x;
+  int k;
+  double m = frexp(x, &k);
+  if (m < 0.7071067811865476) {
+    m *= 2.0;
+    --k;
+  }
+  const double s = (m - 1.0) / (m + 1.0), s2 = s * s;
+  double sum = 1.0 / 21.0;
+#pragma unroll
+  for (int i = 19; i >= 1; i -= 2) sum = fma(sum, s2, 1.0 / i);
+  return fma((double)k, 0.6931471805599453, 2.0 * s * sum);
+}
+
 // The teacher's list of one row.
 struct Named {
   const int32_t* index;
@@ -48,7 +65,7 @@ struct Named {
 
   __device__ __forceinline__ int32_t at(int32_t j) const {
     const int32_t c = index[j];
-    if (c < 0 || c >= C) return -1;
+    if ((c < 0) | (c >= C)) return -1;
     if (repeats)
       for (int32_t i = 0; i < j; ++i)
         if (index[i] == c) return -1;
@@ -58,74 +75,127 @@ struct Named {
 
 // What a row's loss and gradient are made of.
 struct Scalars {
-  bool live;      // whether the row takes part
+  bool live;       // whether the row takes part
   double kl;
-  double shift_q, scale_q;  // q = exp(logq - shift_q) scale_q
-  double top, scale_p;      // p = exp((z - top) / T) scale_p
-  float others;             // the factor of the other entries' exponentials
+  double scale_q, scale_p;  // q and p from exponentials relative to the largest
+  float others;    // the factor of the other entries' exponentials
+};
+
+// A lane's places of the list: E of them in registers, or (E = 0) any number,
+// read and computed again in each pass.
+template <class T, int E>
+struct Places {
+  static constexpr int MOST = E > 0 ? E : 1;
+  const Named& named;
+  const float* row;
+  int32_t t, k;
+  int32_t col[MOST];
+  float lq[MOST], z[MOST];
+  double q[MOST], p[MOST];
+
+  __device__ __forceinline__ Places(const Named& n, const float* r, int32_t lane)
+      : named(n), row(r), t(lane), k(n.k) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int32_t j = t + e * T::LANES;
+      col[e] = j < k ? named.at(j) : -1;
+      lq[e] = j < k ? named.logq[j] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) z[e] = col[e] >= 0 ? row[col[e]] : 0.f;
+  }
+  // f(column, logq, z, q, p) for the places that are used
+  template <class F>
+  __device__ __forceinline__ void each(F f) {
+    if constexpr (E > 0) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (col[e] >= 0) f(col[e], lq[e], z[e], q[e], p[e]);
+    } else {
+#pragma unroll 1
+      for (int32_t j = t; j < k; j += T::LANES) {
+        const int32_t c = named.at(j);
+        if (c < 0) continue;
+        double q0 = 0.0, p0 = 0.0;
+        f(c, named.logq[j], row[c], q0, p0);
+      }
+    }
+  }
 };
 
 // From the sums over the entries not named: `high` their largest, `sum` of
-// exp((z - high) / T).
-template <class T>
-__device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& team, const Named& named,
-                               const float* row, float rest, float high, double sum) {
-  Scalars s = {};
+// exp((z - high) / T); and the gradient's values at the named ones in columns
+// [from, end) (to NULL: none; `ready` is called before the first).
+template <class T, int E, class F>
+__device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& team,
+                                               const Named& named, const float* row, float rest,
+                                               float high, double sum, double w, float* to,
+                                               int32_t from, int32_t end, F ready) {
+  Places<T, E> places(named, row, team.t);
   float most = -INFINITY, top = high;
-  bool any = false, bad = false;
-  for (int32_t j = team.t; j < a.k; j += T::LANES) {
-    const int32_t c = named.at(j);
-    if (c < 0) continue;
-    any = true;
-    bad |= named.logq[j] != named.logq[j];
-    most = fmaxf(most, named.logq[j]);
-    top = fmaxf(top, row[c]);
+  constexpr int32_t BAD = 1 << 16;
+  int32_t used = 0;
+  places.each([&](int32_t, float lq, float z, double&, double&) INLINE {
+    used = (used & BAD) | (lq != lq ? BAD + 1 : 1);
+    most = fmaxf(most, lq);
+    top = fmaxf(top, z);
+  });
+  float low = -most;  // (the largest of both in one exchange)
+  team.range(&top, &low, &used);
+  most = -low;
+  rest = rest > 0.f ? rest : rest == rest ? 0.f : rest;
+  if (rest > 0.f) most = fmaxf(most, (float)log_quick(rest));
+  Scalars s = {};
+  s.live = (used > 0) & ((used >= BAD) | (most > -INFINITY)) & (top > -INFINITY);
+  if (!s.live) {
+    ready(s);
+    return s;
   }
-  const double ln_rest = rest > 0.f ? log((double)rest) : rest == rest ? -INFINITY : rest;
-  most = fmaxf(team.max(most), (float)ln_rest);
-  top = team.max(top);
-  any = team.any(any);
-  s.live = (team.any(bad) || most > -INFINITY) && any && top > -INFINITY;
-  if (!s.live) return s;
   double nq = 0.0, np = 0.0, cross = 0.0;
-  for (int32_t j = team.t; j < a.k; j += T::LANES) {
-    const int32_t c = named.at(j);
-    if (c < 0) continue;
-    const double lq = (double)named.logq[j] - most, lp = ((double)row[c] - top) * a.inv_t;
-    const double q = exp_exact(lq);
+  places.each([&](int32_t, float logq, float z, double& q, double& p) INLINE {
+    const double lq = (double)logq - most, lp = ((double)z - top) * a.inv_t;
+    q = exp_exact(lq);
+    p = exp_exact(lp);
     nq += q;
-    np += exp_exact(lp);
+    np += p;
     if (!(q == 0.0)) cross += q * (lq - lp);
-  }
+  });
+  team.sum3(&nq, &np, &cross);
   const double high_p = sum > 0.0 ? ((double)high - top) * a.inv_t : 0.0;
   const double down = sum == 0.0 ? 0.0 : exp_exact(high_p);
-  const double r = exp_exact(ln_rest - most);
-  nq = team.sum(nq) + r;
-  np = team.sum(np) + sum * down;
-  cross = team.sum(cross);
-  if (!(r == 0.0)) cross += r * (ln_rest - most - (high_p + log(sum)));
-  s.kl = a.T * a.T * (cross / nq - log(nq) + log(np));
-  s.shift_q = most;
+  const double r = rest == 0.f ? 0.0 : (double)rest * exp_exact(-(double)most);
+  nq += r;
+  np += sum * down;
+  if (!(r == 0.0))
+    cross += r * (sum == 0.0 ? INFINITY : log_of((double)rest / sum) - most - high_p);
+  s.kl = a.T * a.T * (cross / nq + log_of(np / nq));
   s.scale_q = 1.0 / nq;
-  s.top = top;
   s.scale_p = 1.0 / np;
-  s.others = sum == 0.0 ? 0.f : (float)(a.T * (down / np - r / (nq * sum)));
+  s.others = sum == 0.0 ? 0.f : (float)(a.T * (down * s.scale_p - r * s.scale_q / sum));
+  ready(s);
+  if (!to) return s;
+  places.each([&](int32_t c, float logq, float z, double q, double p) INLINE {
+    if ((c < from) | (c >= end)) return;
+    if (E == 0) {
+      q = exp_exact((double)logq - most);
+      p = exp_exact(((double)z - top) * a.inv_t);
+    }
+    to[c] = (float)(w * a.T * (p * s.scale_p - q * s.scale_q));
+  });
   return s;
 }
 
-// The gradient's values at the entries that the teacher names in columns
-// [from, to).
-template <class T>
-__device__ __forceinline__ void named_gradient(const DistillArgs& a, const T& team, const Named& named,
-                               const float* row, const Scalars& s, double w, float* to,
-                               int32_t from, int32_t end) {
-  for (int32_t j = team.t; j < a.k; j += T::LANES) {
-    const int32_t c = named.at(j);
-    if (c < from || c >= end) continue;
-    const double q = exp_exact((double)named.logq[j] - s.shift_q) * s.scale_q;
-    const double p = exp_exact(((double)row[c] - s.top) * a.inv_t) * s.scale_p;
-    to[c] = (float)(w * a.T * (p - q));
-  }
+// The same with as many places in registers as the list asks for.
+template <class T, class F>
+__device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& team,
+                                               const Named& named, const float* row, float rest,
+                                               float high, double sum, double w, float* to,
+                                               int32_t from, int32_t end, F ready) {
+  if (T::LANES >= GNN_TOP_MOST || a.k <= T::LANES)
+    return row_scalars<T, 1>(a, team, named, row, rest, high, sum, w, to, from, end, ready);
+  if (a.k <= 4 * T::LANES)
+    return row_scalars<T, 4>(a, team, named, row, rest, high, sum, w, to, from, end, ready);
+  return row_scalars<T, 0>(a, team, named, row, rest, high, sum, w, to, from, end, ready);
 }
 
 // A part of a row (or the row) in registers with the entries named taken out,
@@ -140,7 +210,7 @@ struct Others {
   // bits: one for each column that the team holds.
   __device__ __forceinline__ void load(const DistillArgs& a, const T& team, const float* from, int32_t col0,
                        const int32_t* index, uint32_t* bits) {
-    row.load(from + col0, a.C - col0, team.t);
+    row.load(from, a.C, team.t, col0);
     for (int32_t k = team.t; k < (Row::MOST + 31) / 32; k += T::LANES) bits[k] = 0;
     team.sync();
     bool twice = false;
@@ -155,7 +225,7 @@ struct Others {
     high = -INFINITY;
 #pragma unroll
     for (int k = 0; k < Row::CHUNKS; ++k) {
-      const int32_t c = row.column(k);
+      const int32_t c = row.column(k) - col0;
       const uint32_t out = bits[c >> 5] >> (c & 31);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -163,22 +233,24 @@ struct Others {
       high = fmaxf(high, max4(row.z[k]));
     }
     high = team.max(high);
-    const float shift = shift_of(high), inv_t = (float)a.inv_t;
+    // (exp as a power of two: what falls below the smallest normal number is 0)
+    const float shift = shift_of(high), octaves = (float)(a.inv_t * 1.4426950408889634);
     sum = 0.0;
 #pragma unroll
     for (int k = 0; k < Row::CHUNKS; ++k) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) row.z[k][j] = expf((row.z[k][j] - shift) * inv_t);
+      for (int j = 0; j < 4; ++j)
+        row.z[k][j] = __builtin_amdgcn_exp2f((row.z[k][j] - shift) * octaves);
       sum += sum4(row.z[k]);
     }
     sum = team.sum(sum);
   }
-  __device__ __forceinline__ void store(float* to, int32_t col0, int32_t C, float factor) const {
+  __device__ __forceinline__ void store(float* to, float factor) const {
 #pragma unroll
     for (int k = 0; k < Row::CHUNKS; ++k) {
       f4 g = row.z[k] * factor;
       if (factor == 0.f) g = {0.f, 0.f, 0.f, 0.f};
-      store_cols(to + col0, row.column(k), C - col0, g);
+      store_cols(to, row.column(k), row.C, g);
     }
   }
 };
@@ -196,9 +268,9 @@ __device__ __forceinline__ void stores_done(const T& team) {
 }
 
 template <int G, int W, class Row>
-__global__ __launch_bounds__((threads_of<G, W>())) void distill_kernel(DistillArgs a) {
-  using T = Team<G, W>;
-  constexpr int THREADS = threads_of<G, W>(), R = THREADS / T::LANES;
+__global__ __launch_bounds__(W > 1 ? 64 * W : 256) void distill_kernel(DistillArgs a) {
+  using T = Team<G, W, Exchange>;
+  constexpr int THREADS = W > 1 ? 64 * W : 256, R = THREADS / T::LANES;
   __shared__ typename T::Shared s[R];
   __shared__ uint32_t s_bits[R][(Row::MOST + 31) / 32];
   __shared__ double s_loss[THREADS / 64];
@@ -212,18 +284,17 @@ __global__ __launch_bounds__((threads_of<G, W>())) void distill_kernel(DistillAr
     Others<T, Row> others;
     others.load(a, team, from, 0, named.index, s_bits[own]);
     named.repeats = others.repeats;
-    const Scalars x = row_scalars(a, team, named, from, a.rest ? a.rest[i] : 0.f, others.high,
-                                  others.sum);
     const double w = weight_of(a, (int32_t)i);
-    const bool counts = x.live && w != 0.0;
-    if (counts) loss = w * x.kl;
+    float* to = a.dZ ? a.dZ + i * a.ld_dz : nullptr;
+    const Scalars x = row_scalars(
+        a, team, named, from, a.rest ? a.rest[i] : 0.f, others.high, others.sum, w,
+        w != 0.0 ? to : nullptr, 0, a.C, [&](const Scalars& x) INLINE {
+          if (!to) return;
+          others.store(to, x.live && w != 0.0 ? (float)(w * x.others) : 0.f);
+          stores_done(team);
+        });
+    if (x.live && w != 0.0) loss = w * x.kl;
     if (a.kl && team.t == 0) a.kl[i] = (float)x.kl;
-    if (a.dZ) {
-      float* to = a.dZ + i * a.ld_dz;
-      others.store(to, 0, a.C, counts ? (float)(w * x.others) : 0.f);
-      stores_done(team);
-      if (counts) named_gradient(a, team, named, from, x, w, to, 0, a.C);
-    }
   }
   // the block's share of the loss, in a fixed order
   if (team.t != 0) loss = 0.0;
@@ -239,7 +310,7 @@ __global__ __launch_bounds__((threads_of<G, W>())) void distill_kernel(DistillAr
 
 // Rows past 32,768 columns: a launch for the sums of their parts, one for the
 // scalars, which every block of the row forms alike, and the gradient.
-using SplitTeam = Team<64, 4>;
+using SplitTeam = Team<64, 4, Exchange>;
 using SplitRow = Held<64, 4, 4>;
 constexpr int32_t SPLIT_COLS = SplitRow::MOST;
 
@@ -276,23 +347,24 @@ __global__ __launch_bounds__(256) void distill_grad_kernel(DistillArgs a) {
   for (int32_t k = team.t; k < a.per_row; k += 256)
     if (at[k].sum != 0.0) sum += at[k].sum * exp_exact(((double)at[k].top - high) * a.inv_t);
   sum = team.sum(sum);
-  const Scalars x = row_scalars(a, team, named, from, a.rest ? a.rest[i] : 0.f, high, sum);
   const double w = weight_of(a, (int32_t)i);
-  const bool counts = x.live && w != 0.0;
+  const int32_t col0 = part * SPLIT_COLS;
+  float* to = a.dZ ? a.dZ + i * a.ld_dz : nullptr;
+  const Scalars x = row_scalars(
+      a, team, named, from, a.rest ? a.rest[i] : 0.f, high, sum, w, w != 0.0 ? to : nullptr, col0,
+      min(col0 + SPLIT_COLS, a.C), [&](const Scalars& x) INLINE {
+        if (!to) return;
+        Others<SplitTeam, SplitRow> others;
+        others.load(a, team, from, col0, named.index, s_bits);
+        const float down = others.sum == 0.0
+                               ? 0.f : (float)exp_exact(((double)others.high - high) * a.inv_t);
+        others.store(to, x.live && w != 0.0 ? (float)(w * x.others) * down : 0.f);
+        stores_done(team);
+      });
   if (part == 0 && team.t == 0) {
-    a.part[i] = counts ? w * x.kl : 0.0;
+    a.part[i] = x.live && w != 0.0 ? w * x.kl : 0.0;
     if (a.kl) a.kl[i] = (float)x.kl;
   }
-  if (!a.dZ) return;
-  Others<SplitTeam, SplitRow> others;
-  const int32_t col0 = part * SPLIT_COLS;
-  others.load(a, team, from, col0, named.index, s_bits);
-  float* to = a.dZ + i * a.ld_dz;
-  const float down = others.sum == 0.0
-                         ? 0.f : (float)exp_exact(((double)others.high - high) * a.inv_t);
-  others.store(to, col0, a.C, counts ? (float)(w * x.others) * down : 0.f);
-  stores_done(team);
-  if (counts) named_gradient(a, team, named, from, x, w, to, col0, min(col0 + SPLIT_COLS, a.C));
 }
 
 // out = the sum of `count` terms, in a fixed order.
@@ -317,7 +389,8 @@ struct Launch {
 };
 template <int G, int W, int V>
 Launch held() {
-  return {distill_kernel<G, W, Held<G, W, V>>, threads_of<G, W>() / (G * W), threads_of<G, W>()};
+  constexpr int THREADS = W > 1 ? 64 * W : 256;
+  return {distill_kernel<G, W, Held<G, W, V>>, THREADS / (G * W), THREADS};
 }
 template <int G>
 Launch few(int32_t v) {

@@ -160,7 +160,7 @@ __device__ __forceinline__ Border first_entries(const T& team, Row& row, const f
     row.each([&](float z, int32_t) INLINE { low = fminf(low, z > -INFINITY ? z : INFINITY); });
     low = -team.max(-low);
   }
-  float scale = (T::BINS - 1) / (top - low);
+  float scale = (T::Shared::BINS - 1) / (top - low);
   if (!(scale < INFINITY)) scale = 0.f;
   team.clear();
   row.each([&](float z, int32_t) INLINE {
@@ -232,7 +232,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
   Weights weight = {Exponential(table, a.scale, a.bits), top, NO_BORDER};
   if (a.top_k) weight.kept = first_entries(team, row, from, a.C, a.top_k, top, low, lanes);
   if (a.top_p < 1.0) {
-    const float scale = (T::BINS - 1) * a.inv_range;
+    const float scale = (T::Shared::BINS - 1) * a.inv_range;
     uint64_t all = 0;
     team.clear();
     const auto fill = [&](f4 z, const uint64_t (&w)[4]) INLINE {

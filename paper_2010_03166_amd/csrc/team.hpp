@@ -46,27 +46,33 @@ __device__ __forceinline__ void refresh(T& v) {
   asm volatile("" : "+v"(v));
 }
 
+// What the wavefronts of a team give each other.
+template <int G, int W>
+struct Exchange {
+  uint64_t sums[W];
+  float tops[W], lows[W];
+  int32_t flags[W];
+};
+// And what a border is found with: bins, and entries that are put in order at
+// once.
+template <int G, int W>
+struct Bins : Exchange<G, W> {
+  static constexpr int BINS = W > 1 ? 512 : G == 64 ? 256 : G == 32 ? 128 : G >= 8 ? 64 : 8 * G;
+  static constexpr int LIST = W > 1 ? 256 : G == 64 ? 128 : G == 32 ? 64 : G >= 8 ? 32 : 16;
+  uint64_t bins[BINS + G];  // (the last G, one a lane, for entries that are in none)
+  uint64_t amount[LIST];
+  uint64_t place[LIST];
+  uint64_t lo, hi;
+  Border border;
+  int32_t count;
+};
+
 // G lanes of a wavefront, or W whole wavefronts, that hold a row together.
-template <int G_, int W_>
+template <int G_, int W_, template <int, int> class S = Bins>
 struct Team {
   static constexpr int G = G_, W = W_, LANES = G * W;
   static_assert(W == 1 || G == 64, "several wavefronts are whole ones");
-  // Bins, and entries that are put in order at once.
-  static constexpr int BINS = W > 1 ? 512 : G == 64 ? 256 : G == 32 ? 128 : G >= 8 ? 64 : 8 * G;
-  static constexpr int LIST = W > 1 ? 256 : G == 64 ? 128 : G == 32 ? 64 : G >= 8 ? 32 : 16;
-  static constexpr int LOG_BINS = __builtin_ctz(BINS);
-
-  struct Shared {
-    uint64_t bins[BINS + G];  // (the last G, one a lane, for entries that are in none)
-    uint64_t amount[LIST];
-    uint64_t place[LIST];
-    uint64_t lo, hi;
-    uint64_t sums[W];
-    float tops[W], lows[W];
-    int32_t flags[W];
-    Border border;
-    int32_t count;
-  };
+  using Shared = S<G, W>;
 
   Shared& s;
   const int t;     // own number in the team
@@ -142,6 +148,12 @@ struct Team {
     sync();
     return v;
   }
+  // Three sums.
+  __device__ __forceinline__ void sum3(double* x, double* y, double* z) const {
+    *x = sum(*x);
+    *y = sum(*y);
+    *z = sum(*z);
+  }
   __device__ __forceinline__ bool any(bool v) const {
     uint64_t mine = __ballot(v);
     if (G < 64) mine = mine >> ((threadIdx.x & 63) / G * G) & ((1ull << (G & 63)) - 1);
@@ -177,7 +189,7 @@ struct Team {
   // The first bin with which the amounts reach P, and the amounts before it.
   // Every wavefront finds it by itself.  False where all of them do not.
   __device__ __forceinline__ bool find(uint64_t P, int32_t* bin, uint64_t* base) const {
-    constexpr int EACH = BINS / G;
+    constexpr int EACH = Shared::BINS / G;
     uint64_t own = 0;
     for (int k = 0; k < EACH; ++k) own += s.bins[lane * EACH + k];
     uint64_t sum = before(own);
@@ -195,7 +207,7 @@ struct Team {
   }
 
   __device__ __forceinline__ void clear() const {
-    for (int k = t; k < BINS; k += LANES) s.bins[k] = 0;
+    for (int k = t; k < Shared::BINS; k += LANES) s.bins[k] = 0;
     if (t == 0) {
       s.count = 0;
       s.lo = ~0ull;
@@ -205,14 +217,14 @@ struct Team {
   }
   // (without a branch: what is to be in no bin goes to the lane's own place)
   __device__ __forceinline__ void add(int32_t bin, uint64_t x, bool in) const {
-    add(in ? bin : BINS + lane, x);
+    add(in ? bin : Shared::BINS + lane, x);
   }
   __device__ __forceinline__ void add(int32_t bin, uint64_t x) const {
     atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[bin]), (unsigned long long)x);
   }
   __device__ __forceinline__ void list(float z, int32_t col, uint64_t x) const {
     const int32_t at = atomicAdd(&s.count, 1);
-    if (at >= LIST) return;
+    if (at >= Shared::LIST) return;
     s.place[at] = place(z, col);
     s.amount[at] = x;
   }
@@ -257,7 +269,7 @@ struct Team {
       }
     });
     sync();
-    if (s.count > LIST) {
+    if (s.count > Shared::LIST) {
       sync();
       return false;
     }
@@ -266,7 +278,7 @@ struct Team {
   }
 
   __device__ __forceinline__ static int32_t bin_of(float z, float top, float scale) {
-    return (int32_t)fminf((top - z) * scale, (float)(BINS - 1));
+    return (int32_t)fminf((top - z) * scale, (float)(Shared::BINS - 1));
   }
 
   // The border in a bin of many entries: by bins of their places, whose range
@@ -291,7 +303,7 @@ struct Team {
       });
       sync();
       const uint64_t from = s.lo, range = s.hi - from;
-      const int shift = range < BINS ? 0 : 64 - LOG_BINS - __clzll((long long)range);
+      const int shift = range < Shared::BINS ? 0 : 64 - __builtin_ctz(Shared::BINS) - __clzll((long long)range);
       row.each([&](float z, int32_t col) INLINE {
         if (!member(z, col)) return;
         const uint64_t x = amount(z, col);
@@ -311,7 +323,7 @@ struct Team {
         if (x) list(z, col, x);
       });
       sync();
-      if (s.count <= LIST) return settle(P, base);
+      if (s.count <= Shared::LIST) return settle(P, base);
       sync();
     }
   }
@@ -328,9 +340,10 @@ struct Held {
   mutable int32_t first;  // column of the lane's first
   int32_t C;
 
-  __device__ __forceinline__ void load(const float* row, int32_t cols, int t) {
+  // The row of `cols` columns, or MOST of them from column `from` on.
+  __device__ __forceinline__ void load(const float* row, int32_t cols, int t, int32_t from = 0) {
     C = cols;
-    first = (t / G) * (G * V * 4) + t % G * 4;
+    first = from + (t / G) * (G * V * 4) + t % G * 4;
 #pragma unroll
     for (int k = 0; k < V; ++k)  // (rows of more than one chunk have at least four columns)
       z[k] = MOST > 4 ? *reinterpret_cast<const f4u*>(row + min(column(k), C - 4))
