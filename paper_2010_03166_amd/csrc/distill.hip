@@ -308,7 +308,7 @@ __global__ __launch_bounds__(W > 1 ? 64 * W : 256) void distill_kernel(DistillAr
   else a.part[a.block0 + blockIdx.x] = loss;
 }
 
-// Rows past 32,768 columns: a launch for the sums of their parts, one for the
+// Rows past 16,384 columns: a launch for the sums of their parts, one for the
 // scalars, which every block of the row forms alike, and the gradient.
 using SplitTeam = Team<64, 4, Exchange>;
 using SplitRow = Held<64, 4, 4>;
@@ -396,23 +396,25 @@ template <int G>
 Launch few(int32_t v) {
   return v == 3 ? held<G, 1, 3>() : held<G, 1, 4>();
 }
-Launch choose(int32_t C) {
-  const int32_t q = (int32_t)ceil_div(C, 4);
-  if (q == 1) return held<1, 1, 1>();
-  if (q == 2) return held<1, 1, 2>();
-  if (q <= 4) return few<1>(q);
-  if (q <= 8) return few<2>((q + 1) / 2);
-  if (q <= 16) return few<4>((q + 3) / 4);
-  if (q <= 32) return few<8>((q + 7) / 8);
-  if (q <= 64) return few<16>((q + 15) / 16);
-  if (q <= 128) return few<32>((q + 31) / 32);
-  if (q <= 256) return few<64>((q + 63) / 64);
+// As many lanes as a row takes at three or four chunks each, and a quarter of
+// the list's places at least: a lane's places stay in registers.
+Launch choose(int32_t C, int32_t places) {
+  if (C < 4) return held<1, 1, 1>();
+  const int32_t q = (int32_t)ceil_div(C, 4), lanes = std::max(q, places);
+  const auto three = [&](int32_t lanes) { return (int32_t)ceil_div(q, lanes) <= 3 ? 3 : 4; };
+  if (lanes == 1) return held<1, 1, 1>();
+  if (lanes == 2) return held<1, 1, 2>();
+  if (lanes <= 4) return few<1>(three(1));
+  if (lanes <= 8) return few<2>(three(2));
+  if (lanes <= 16) return few<4>(three(4));
+  if (lanes <= 32) return few<8>(three(8));
+  if (lanes <= 64) return few<16>(three(16));
+  if (lanes <= 128) return few<32>(three(32));
+  if (q <= 256) return few<64>(three(64));
   if (q <= 512) return held<64, 1, 8>();
   if (q <= 1024) return held<64, 4, 4>();
-  if (q <= 2048) return held<64, 8, 4>();
-  if (q <= 4096) return held<64, 16, 4>();
-  if (q <= 6144) return held<64, 16, 6>();
-  if (q <= 8192) return held<64, 16, 8>();
+  if (q <= 2048) return held<64, 4, 8>();
+  if (q <= 4096) return held<64, 8, 8>();
   return {nullptr, 1, 256};
 }
 
@@ -420,8 +422,8 @@ Launch choose(int32_t C) {
 struct Layout {
   size_t parts, total;
 };
-Layout layout_of(int32_t n, int32_t C) {
-  const Launch l = choose(C);
+Layout layout_of(int32_t n, int32_t C, int32_t k) {
+  const Launch l = choose(C, k);
   Layout o;
   o.parts = round_up((size_t)ceil_div(n, l.rows) * sizeof(double), 256);
   o.total = o.parts + (l.kernel ? 0 : (size_t)n * ceil_div(C, SPLIT_COLS) * sizeof(Part));
@@ -434,7 +436,7 @@ extern "C" {
 
 size_t gnn_distill_workspace_bytes(int32_t n, int32_t C, int32_t k) {
   if (n < 0 || C <= 0 || C > MOST_COLS || k <= 0 || k > GNN_TOP_MOST) return 0;
-  return layout_of(n, C).total;
+  return layout_of(n, C, k).total;
 }
 
 gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, int32_t k,
@@ -447,7 +449,7 @@ gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, 
     return GNN_ERR_SHAPE;
   if (!out || (n > 0 && (!Z || !index || !logq))) return GNN_ERR_NULL;
   if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
-  const Layout o = layout_of(n, C);
+  const Layout o = layout_of(n, C, k);
   if (workspace_bytes < o.total || (o.total > 0 && !workspace)) return GNN_ERR_WORKSPACE;
   {
     const size_t rows = (size_t)n * 4, list = rows * k;
@@ -462,7 +464,7 @@ gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, 
         if (ranges_overlap(outs[i], outb[i], outs[q], outb[q])) return GNN_ERR_ALIAS;
     }
   }
-  const Launch l = choose(C);
+  const Launch l = choose(C, k);
   DistillArgs a = {};
   a.n = n;
   a.C = C;

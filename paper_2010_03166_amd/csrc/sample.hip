@@ -366,11 +366,6 @@ struct TopArgs {
   int64_t block0;
 };
 
-// Exponentials of entries, from the largest.
-__device__ __forceinline__ float tempered(float z, float top, float inv_t) {
-  return z == -INFINITY ? 0.f : expf((z - top) * inv_t);
-}
-
 template <class T, class Row>
 __device__ __forceinline__ void top_row(const TopArgs& a, const T& team, uint64_t* list, int32_t i) {
   Row row;
@@ -392,29 +387,40 @@ __device__ __forceinline__ void top_row(const TopArgs& a, const T& team, uint64_
   // the entries kept, and the sums of both parts
   if (team.t == 0) team.s.count = 0;
   team.sync();
-  const float inv_t = (float)a.inv_t;
+  const float octaves = (float)(a.inv_t * 1.4426950408889634);
   double in = 0.0, out = 0.0;
-  row.each4([&](int32_t at, f4 z) INLINE {
-    float more = 0.f, less = 0.f;
+  row.each4([&](int32_t col, f4 z) INLINE {
+    bool kept[4], any = false;
+    f4 e;
+    float less = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int32_t col = at + j;
-      const float e = tempered(z[j], top, inv_t);
-      if (z[j] > -INFINITY && within(b, z[j], col)) {
-        more += e;
-        list[atomicAdd(&team.s.count, 1)] = place(z[j], col);
-      } else {
-        less += e;
-      }
+      kept[j] = within(b, z[j], col + j) & (z[j] > -INFINITY);
+      any |= kept[j];
+      // (exp as a power of two: what falls below the smallest normal number is 0)
+      e[j] = __builtin_amdgcn_exp2f((z[j] - top) * octaves);
+      less += kept[j] ? 0.f : e[j];
+    }
+    out += less;
+    if (!any) return;
+    float more = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (!kept[j]) continue;
+      more += e[j];
+      list[atomicAdd(&team.s.count, 1)] = place(z[j], col + j);
     }
     in += more;
-    out += less;
   });
   in = team.sum(in);
   out = team.sum(out);
   team.sync();
   const int32_t m = team.s.count;
   const double lse = log_quick((float)(in + out));
+  // each in its place: those before it are counted, eight at a time
+  if (team.t < 8 || T::LANES < 8)
+    for (int32_t j = m + team.t; j < (m + 7) / 8 * 8; j += T::LANES) list[j] = ~0ull;
+  team.sync();
   for (int32_t j = team.t; j < a.k; j += T::LANES) {
     if (j >= m) {
       index[j] = -1;
@@ -423,7 +429,10 @@ __device__ __forceinline__ void top_row(const TopArgs& a, const T& team, uint64_
     }
     const uint64_t own = list[j];
     int32_t rank = 0;
-    for (int32_t q = 0; q < m; ++q) rank += list[q] < own;
+    for (int32_t q = 0; q < m; q += 8) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) rank += list[q + k] < own;
+    }
     const uint32_t key = ~(uint32_t)(own >> 32);
     const float z = __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
     index[rank] = (int32_t)(uint32_t)own;
@@ -437,7 +446,7 @@ __global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
   using T = Team<G, W>;
   constexpr int R = threads_of<G, W>() / T::LANES;
   constexpr int MOST = Row::MOST < MOST_TOP
-                           ? Row::MOST : MOST_TOP;
+                           ? (Row::MOST + 7) / 8 * 8 : MOST_TOP;
   __shared__ typename T::Shared s[R];
   __shared__ uint64_t s_list[R][MOST];
   const int own = threadIdx.x / T::LANES;
@@ -493,7 +502,7 @@ Launch<Args> choose(int32_t C) {
   if (q <= 384) return held<Args, Kernel, 64, 1, 6>();
   if (q <= 512) return held<Args, Kernel, 64, 1, 8>();
   if (q <= 1024) return held<Args, Kernel, 64, 4, 4>();
-  if (q <= 2048) return held<Args, Kernel, 64, 8, 4>();
+  if (q <= 2048) return held<Args, Kernel, 64, 4, 8>();
   if (q <= 4096) return held<Args, Kernel, 64, 16, 4>();
   if (q <= 6144) return held<Args, Kernel, 64, 16, 6>();
   if (q <= 8192) return held<Args, Kernel, 64, 16, 8>();

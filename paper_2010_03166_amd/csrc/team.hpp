@@ -234,6 +234,7 @@ struct Team {
     for (int32_t i = t; i < m; i += LANES) {
       const uint64_t own = s.place[i], x = s.amount[i];
       uint64_t sum = base;
+#pragma unroll 4
       for (int32_t j = 0; j < m; ++j) sum += s.place[j] < own ? s.amount[j] : 0;
       if (sum < P && sum + x >= P) {
         const uint32_t key = ~(uint32_t)(own >> 32);
