@@ -449,7 +449,9 @@ class Trainer:
     stack's forward pass, the classifier and loss (Section 3.1), the backward
     pass from the classifier's input gradient down (Section 5.1), then SGD,
     Adam or AdamW on every weight.  policy_step is the same iteration with the
-    clipped policy loss in the place of the classifier's.  All arithmetic runs
+    clipped policy loss in the place of the classifier's, distill_step with the
+    loss against another network's top logits; act draws actions for the first,
+    top_logits gives the second.  All arithmetic runs
     in libgnnprop; the loss stays on the device (read it with `loss.item()`
     when needed)."""
 
@@ -543,6 +545,7 @@ class Trainer:
         # made when first used
         self._Z, self._dZ = _Rows(self.C, ld_p, device), _Rows(self.C, ld_p, device)
         self.policy_out = torch.zeros(3, device=device)
+        self.distill_out = torch.zeros(1, device=device)
         self.logp = self._logp = torch.empty(0, device=device)
         self.policy_ws = None
         self._policy_streams = set()  # handles of the streams they were used on
@@ -600,7 +603,8 @@ class Trainer:
         other use, once they are replaced, until every stream that used them
         is done."""
         n, C, f = self.n, self.C, self.f_top
-        need = max(G.gnn_policy_workspace_bytes(n, C), G.gnn_gemm_workspace_bytes(n, C, f),
+        need = max(G.gnn_policy_workspace_bytes(n, C), G.gnn_sample_workspace_bytes(n, C),
+                   G.gnn_distill_workspace_bytes(n, C, G.GNN_TOP_MOST), G.gnn_gemm_workspace_bytes(n, C, f),
                    G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C), 256)
         if self.policy_ws is None or self.policy_ws.numel() < need or self._Z.buf.shape[0] < n:
             with torch.cuda.stream(_stream_object(stream)):
@@ -634,14 +638,48 @@ class Trainer:
         what the call reads has to be ready there, and what it gives is."""
         self._per_row("actions", actions, torch.int32)
         _, _, Z, ld = self._logits(X, stream)
-        if stream is None:
-            logp = torch.empty(self.n, device=self.device)
-        else:
-            with torch.cuda.stream(_stream_object(stream)):
-                logp = torch.empty(self.n, device=self.device)
-            logp.record_stream(torch.cuda.current_stream())
+        logp = self._new((self.n,), torch.float32, stream)
         G.gnn_action_logp(self.n, self.C, Z, ld, actions, logp, self.policy_ws, stream)
         return logp
+
+    def _new(self, shape, dtype, stream):
+        """A tensor that the call fills on `stream` and the caller reads on the
+        current one."""
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(_stream_object(stream)):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        t.record_stream(torch.cuda.current_stream())
+        return t
+
+    def act(self, X: torch.Tensor, u: torch.Tensor, temperature: float = 1.0, top_k: int = 0,
+            top_p: float = 1.0, min_p: float = 0.0, stream=None):
+        """Draws each row's action under the present weights by its random
+        number (u: n floats in [0, 1)), as gnn_sample_actions does: (actions,
+        int32, their log-probabilities under the whole policy), new tensors, for
+        policy_step's actions and old_logp.  stream: as in action_logp."""
+        self._per_row("u", u)
+        _, _, Z, ld = self._logits(X, stream)
+        actions = self._new((self.n,), torch.int32, stream)
+        logp = self._new((self.n,), torch.float32, stream)
+        G.gnn_sample_actions(self.n, self.C, Z, ld, u, temperature, top_k, top_p, min_p, actions,
+                             logp, self.policy_ws, stream)
+        return actions, logp
+
+    def top_logits(self, X: torch.Tensor, k: int, temperature: float = 1.0, stream=None):
+        """What this network teaches another about X's rows: (columns of the k
+        largest logits, n x k int32, -1 where there are fewer; their
+        log-probabilities at the temperature; the share of all others, n), new
+        tensors, for another Trainer's distill_step.  stream: as in
+        action_logp."""
+        _, _, Z, ld = self._logits(X, stream)
+        ws = self._new((max(G.gnn_top_workspace_bytes(self.n, self.C, k), 256),), torch.uint8,
+                       stream)
+        index = self._new((self.n, k), torch.int32, stream)
+        logq = self._new((self.n, k), torch.float32, stream)
+        rest = self._new((self.n,), torch.float32, stream)
+        G.gnn_top_logits(self.n, self.C, Z, ld, k, temperature, index, logq, rest, ws, stream)
+        return index, logq, rest
 
     def policy_step(self, X: torch.Tensor, actions: torch.Tensor, advantage: torch.Tensor,
                     old_logp: Optional[torch.Tensor] = None,
@@ -659,16 +697,45 @@ class Trainer:
                         ("ref_logp", ref_logp), ("weight", weight)):
             self._per_row(name, t)
         self._per_row("actions", actions, torch.int32)
-        n, C, f = self.n, self.C, self.f_top
+        n, C = self.n, self.C
         top, ld_top, Z, ld = self._logits(X, stream)
         dZ, self.logp = self._dZ.view(n), self._logp[:n]
         G.gnn_policy_loss(n, C, Z, ld, actions, advantage, old_logp, ref_logp, weight, clip[0],
                           clip[1], beta, self.policy_out, self.logp, dZ, ld, self.policy_ws,
                           stream)
+        self._learn(top, ld_top, dZ, ld, stream)
+        return self.policy_out
+
+    def _learn(self, top, ld_top: int, dZ, ld: int, stream):
+        """The rest of an iteration from the gradient of the logits on."""
+        n, C, f = self.n, self.C, self.f_top
         G.gnn_gemm(True, False, f, C, n, top, ld_top, dZ, ld, self.dW_mlp, C, self.flags,
                    self.policy_ws, stream)
         G.gnn_gemm(False, True, n, f, C, dZ, ld, self.W_mlp, C, self.dX_top,
                    self.dX_top.stride(0) if n else f, self.flags, self.policy_ws, stream)
         self.stack.backward(self.dX_top, want_dx_first=False, stream=stream)
         self._update(stream)
-        return self.policy_out
+
+    def distill_step(self, X: torch.Tensor, index: torch.Tensor, logq: torch.Tensor,
+                     rest: Optional[torch.Tensor] = None,
+                     weight: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                     stream=None) -> torch.Tensor:
+        """One iteration with the loss against a teacher's top logits
+        (gnn_distill_loss) on the logits X^(L) W_MLP: forward, loss, backward,
+        update.  index, logq: n x k, as top_logits gives them; rest (None: all
+        that the teacher says is in its list), weight (None: 1/n): n floats.
+        Returns the loss, one float on the device.  stream: as in action_logp."""
+        for name, t, dtype in (("index", index, torch.int32), ("logq", logq, torch.float32)):
+            if t.dtype != dtype or t.dim() != 2 or t.shape != (self.n, index.shape[-1]) or \
+                    not t.is_contiguous() or not _on_current(t):
+                raise ValueError("%s must be %d x k contiguous values of %s on the current device" %
+                                 (name, self.n, dtype))
+        self._per_row("rest", rest)
+        self._per_row("weight", weight)
+        n, C, k = self.n, self.C, int(index.shape[1])
+        top, ld_top, Z, ld = self._logits(X, stream)
+        dZ = self._dZ.view(n)
+        G.gnn_distill_loss(n, C, Z, ld, k, index, logq, rest, weight, temperature,
+                           self.distill_out, None, dZ, ld, self.policy_ws, stream)
+        self._learn(top, ld_top, dZ, ld, stream)
+        return self.distill_out

@@ -21,6 +21,9 @@ import torch
 
 from oracle import choose as O
 from paper_2010_03166_amd import gnnprop as G
+from paper_2010_03166_amd import runtime, synth
+
+from gpu_helpers import prepared, to_dev
 
 pytestmark = pytest.mark.gpu
 
@@ -454,3 +457,184 @@ def test_many_blocks():
     want = (cum <= u.double()[:, None]).sum(1)
     near = ((cum - u.double()[:, None]).abs() < 1e-12).any(1)
     assert int(near.sum()) < 10 and torch.equal(a[0].long()[~near], want[~near])
+
+
+# ----------------------------------------- the Trainer, streams and graphs
+
+def _trainer(optimizer="sgd", seed=0, **kw):
+    wl = synth.WORKLOADS[synth.TINY_WORKLOAD]
+    d = synth.workload_inputs(wl, bias=True)
+    c = synth.classifier_inputs(wl)
+    w_mlp = c["w_mlp"] + 0.3 * np.random.default_rng(seed).standard_normal(c["w_mlp"].shape)
+    tr = runtime.Trainer(prepared(d["graph"]), d["params"], wl.f_in, w_mlp.astype(np.float32),
+                         wl.multilabel, optimizer, **kw)
+    return tr, to_dev(d["x"], wl.f_in + 14)
+
+
+def test_acting_and_a_policy_step():
+    """Actions drawn by the Trainer are the oracle's on the Trainer's logits, and
+    with their log-probabilities as old_logp nothing is clipped."""
+    tr, X = _trainer(lr=1e-3)
+    n, C = tr.n, tr.C
+    u = torch.rand(n, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    for T, top_k, top_p, min_p in ((1.0, 0, 1.0, 0.0), (0.8, 3, 0.9, 0.01)):
+        a, lp = tr.act(X, u, T, top_k, top_p, min_p)
+        Z = tr._Z.view(n).cpu().numpy()
+        check_sample(Z, u.cpu().numpy(), T, top_k, top_p, min_p, a.cpu().numpy(), lp.cpu().numpy())
+        assert torch.allclose(lp, tr.action_logp(X, a), rtol=0, atol=(40 + 2 * np.log(C)) * U)
+    out = tr.policy_step(X, a, torch.ones(n, device="cuda"), lp)
+    assert float(out[2]) == 0.0 and torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("T,rest", [(1.0, True), (2.0, True), (2.0, False)])
+def test_teaching(T, rest):
+    """A teacher's top logits, a student's iteration with them: loss and the
+    head's gradient against the oracle, the stack's against the stack's own
+    backward pass."""
+    teacher, X = _trainer(seed=1)
+    tr, _ = _trainer(seed=2, lr=0.0)
+    n, C, k = tr.n, tr.C, min(4, tr.C)
+    index, logq, left = teacher.top_logits(X, k, T)
+    check_top(teacher._Z.view(n).cpu().numpy(), k, T,
+              (index.cpu().numpy(), logq.cpu().numpy(), left.cpu().numpy()))
+    loss = tr.distill_step(X, index, logq, left if rest else None, temperature=T)
+    torch.cuda.synchronize()
+    Z = tr._Z.view(n).cpu().numpy()
+    args = (Z, index.cpu().numpy(), logq.cpu().numpy(), left.cpu().numpy() if rest else None, None, T)
+    r = dict(out=float(loss), dZ=tr._dZ.view(n).cpu().numpy())
+    check_distill(r, *args, kl=False)
+    top = tr.stack.forward(X).cpu().numpy().astype(np.float64)
+    want = top.T @ r["dZ"].astype(np.float64)
+    assert np.abs(tr.dW_mlp.cpu().numpy() - want).max() <= 1e-5 * np.abs(want).max()
+    grads = [g.clone() for _, g in tr.pairs]
+    tr.stack.forward(X)
+    tr.stack.backward(tr.dX_top, want_dx_first=False)
+    for g, (_, again) in zip(grads, tr.pairs):
+        assert torch.equal(g, again)
+
+
+def test_teaching_lowers_the_loss_along_its_gradient():
+    """The loss after a small step is the loss less lr |gradient|^2, to second
+    order: what the whole iteration's gradient says."""
+    teacher, X = _trainer(seed=1)
+    index, logq, left = teacher.top_logits(X, 3)
+    losses = []
+    tr, _ = _trainer(seed=2, lr=1e-3)
+    for _ in range(2):
+        losses.append(float(tr.distill_step(X, index, logq, left)))
+        if len(losses) == 1:
+            g2 = sum(float((g.double() ** 2).sum()) for _, g in tr.pairs)
+    assert abs((losses[0] - losses[1]) / (1e-3 * g2) - 1) < 0.05
+
+
+def test_trainer_refuses_lists_that_do_not_fit():
+    tr, X = _trainer()
+    n = tr.n
+    i, q = torch.zeros((n, 3), dtype=torch.int32, device="cuda"), torch.zeros((n, 3), device="cuda")
+    for bad in ((i.long(), q), (i, q.double()), (i[1:], q), (i, q[:, :2]), (i[0], q[0]),
+                (i.t().contiguous().t(), q), (i.cpu(), q)):
+        with pytest.raises(ValueError):
+            tr.distill_step(X, *bad)
+    with pytest.raises(ValueError):
+        tr.distill_step(X, i, q, torch.zeros(n + 1, device="cuda"))
+    with pytest.raises(ValueError):
+        tr.act(X, torch.zeros(n - 1, device="cuda"))
+    with pytest.raises(G.GnnError):
+        tr.act(X, torch.zeros(n, device="cuda"), top_p=0.0)
+    with pytest.raises(G.GnnError):
+        tr.top_logits(X, 300)
+
+
+def test_trainer_captured_and_replayed():
+    """Acting, a policy step, teaching: captured on another stream, replayed
+    between eager iterations of a second trainer, everything equal."""
+    teacher, X = _trainer(seed=1)
+    cap, _ = _trainer(seed=2, lr=1e-3)
+    eager, _ = _trainer(seed=2, lr=1e-3)
+    n = cap.n
+    gen = torch.Generator("cuda").manual_seed(3)
+    u, adv = torch.rand(n, device="cuda", generator=gen), torch.randn(n, device="cuda", generator=gen)
+    cap.act(X, u)
+    teacher.top_logits(X, 3)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def once(tr, stream):
+        a, lp = tr.act(X, u, 0.9, 4, 0.95, 0.01, stream=stream)
+        out = tr.policy_step(X, a, adv, lp, stream=stream).clone()
+        i, q, r = teacher.top_logits(X, 3, 2.0, stream=stream)
+        return a, lp, out, i, q, r, tr.distill_step(X, i, q, r, temperature=2.0, stream=stream)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = once(cap, s.cuda_stream)
+    for it in range(4):
+        u.copy_(torch.rand(n, device="cuda", generator=gen))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = once(eager, None)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y), it
+        for (w, _), (v, _) in zip(cap.pairs, eager.pairs):
+            assert torch.equal(w, v), it
+
+
+@pytest.mark.parametrize("n,C", [(300, 7), (100, 121), (20, 2048), (6, 5000), (4, 20011), (3, 70001)])
+def test_calls_at_once_and_replayed(n, C):
+    """The same calls on the default stream, on two others at once and from a
+    graph: the same bits."""
+    z, rng = _logits(n, C, 4, mask=0.2, skip=0.1)
+    k = min(9, C)
+    Z, u = _rows(z, C, 0), _f(rng.random(n))
+    i0, q0, r0 = (_f(x) for x in O.top_logits(z + rng.standard_normal(z.shape).astype(np.float32),
+                                              k, 1.0))
+    i0 = i0.int()
+
+    def calls(stream=None):
+        a = torch.empty(n, dtype=torch.int32, device="cuda")
+        i, q = torch.empty((n, k), dtype=torch.int32, device="cuda"), torch.empty((n, k), device="cuda")
+        lp, r, kl, out = (torch.empty(m, device="cuda") for m in (n, n, n, 1))
+        dZ = torch.empty((n, C), device="cuda")
+        w = [_ws(G.gnn_sample_workspace_bytes(n, C)), _ws(G.gnn_top_workspace_bytes(n, C, k)),
+             _ws(G.gnn_distill_workspace_bytes(n, C, k))]
+        def run(stream=None):
+            G.gnn_sample_actions(n, C, Z, C, u, 0.9, 50, 0.9, 0.01, a, lp, w[0], stream)
+            G.gnn_top_logits(n, C, Z, C, k, 2.0, i, q, r, w[1], stream)
+            G.gnn_distill_loss(n, C, Z, C, k, i0, q0, r0, None, 2.0, out, kl, dZ, C, w[2], stream)
+        return run, (a, lp, i, q, r, kl, out, dZ)
+
+    run, want = calls()
+    run()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = [calls() for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (go, _), s in zip(both, streams):
+            go(s.cuda_stream)
+    torch.cuda.synchronize()
+    graph_run, graph_out = calls()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        graph_run(streams[0].cuda_stream)
+    for _ in range(3):
+        for x in graph_out:
+            x.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        for outs in (both[0][1], both[1][1], graph_out):
+            for x, y in zip(outs, want):
+                assert torch.equal(torch.nan_to_num(x.float(), 3.0), torch.nan_to_num(y.float(), 3.0))
+
+
+def test_timer_counts_the_calls():
+    z, _ = _logits(10, 20, 1)
+    G.gnn_timer_enable()
+    G.gnn_timer_reset()
+    try:
+        run_sample(z, np.zeros(10))
+        run_top(z, 3)
+        ms, launches, work = G.gnn_timer_read("sample")
+    finally:
+        G.gnn_timer_enable(False)
+    assert launches == 2 and ms > 0
