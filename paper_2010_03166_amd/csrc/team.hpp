@@ -67,6 +67,12 @@ struct Bins : Exchange<G, W> {
   int32_t count;
 };
 
+// The logit of an entry's place.
+__device__ __forceinline__ float logit_of(uint64_t place) {
+  const uint32_t key = ~(uint32_t)(place >> 32);
+  return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
+}
+
 // G lanes of a wavefront, or W whole wavefronts, that hold a row together.
 template <int G_, int W_, template <int, int> class S = Bins>
 struct Team {
@@ -237,8 +243,7 @@ struct Team {
 #pragma unroll 4
       for (int32_t j = 0; j < m; ++j) sum += s.place[j] < own ? s.amount[j] : 0;
       if (sum < P && sum + x >= P) {
-        const uint32_t key = ~(uint32_t)(own >> 32);
-        s.border = {__uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key), (int32_t)(uint32_t)own};
+        s.border = {logit_of(own), (int32_t)(uint32_t)own};
       }
     }
     sync();
@@ -258,17 +263,25 @@ struct Team {
       sync();
       return true;
     }
-    row.each4([&](int32_t col, f4 z) INLINE {
-      bool in[4], any = false;
+    if constexpr (Row::CHUNKS > 0) {
+      row.each4([&](int32_t col, f4 z) INLINE {
+        bool in[4], any = false;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) any |= in[j] = bin_of(z[j], top, scale) == *bin;
-      if (!any) return;
+        for (int j = 0; j < 4; ++j) any |= in[j] = bin_of(z[j], top, scale) == *bin;
+        if (!any) return;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t x = in[j] ? amount(z[j], col + j) : 0;
-        if (x) list(z[j], col + j, x);
-      }
-    });
+        for (int j = 0; j < 4; ++j) {
+          const uint64_t x = in[j] ? amount(z[j], col + j) : 0;
+          if (x) list(z[j], col + j, x);
+        }
+      });
+    } else {
+      row.each([&](float z, int32_t col) INLINE {
+        if (bin_of(z, top, scale) != *bin) return;
+        const uint64_t x = amount(z, col);
+        if (x) list(z, col, x);
+      });
+    }
     sync();
     if (s.count > Shared::LIST) {
       sync();
@@ -381,11 +394,12 @@ struct Reread {
   const float* row;
   int32_t first, C, part;
 
-  __device__ __forceinline__ void load(const float* from, int32_t cols, int t) {
-    row = from;
+  // Columns [from, cols) of the row.
+  __device__ __forceinline__ void load(const float* at, int32_t cols, int t, int32_t from = 0) {
+    row = at;
     C = cols;
-    part = (int32_t)ceil_div(ceil_div(C, W), G * 4);
-    first = (t / G) * (part * G * 4) + t % G * 4;
+    part = (int32_t)ceil_div(ceil_div(C - from, W), G * 4);
+    first = from + (t / G) * (part * G * 4) + t % G * 4;
   }
   __device__ __forceinline__ int32_t column(int k) const { return first + k * G * 4; }
   template <class F>
@@ -399,6 +413,22 @@ struct Reread {
 #pragma unroll
       for (int j = 0; j < 4; ++j) f(v[j], col + j);
     });
+  }
+};
+
+// Entries by their places, in any order, from memory (the columns are the
+// entries' own).
+template <int G, int W>
+struct Listed {
+  static constexpr int CHUNKS = 0, MOST = MOST_COLS;
+  const uint64_t* places;
+  int64_t count;
+  int32_t t;
+
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll 1
+    for (int64_t k = t; k < count; k += G * W) f(logit_of(places[k]), (int32_t)(uint32_t)places[k]);
   }
 };
 

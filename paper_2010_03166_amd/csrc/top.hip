@@ -1,0 +1,93 @@
+// The top logits of rows, in their order, with their log-probabilities.
+#include "choose.hpp"
+
+using namespace gnnprop;
+
+namespace {
+
+template <int G, int W, class Row>
+__global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
+  using T = Team<G, W>;
+  constexpr int R = threads_of<G, W>() / T::LANES;
+  constexpr int MOST = Row::MOST < MOST_TOP
+                           ? (Row::MOST + 7) / 8 * 8 : MOST_TOP;
+  __shared__ typename T::Shared s[R];
+  __shared__ uint64_t s_list[R][MOST];
+  const int own = threadIdx.x / T::LANES;
+  const int64_t i = (a.block0 + blockIdx.x) * R + own;
+  if (i >= a.n) return;
+  const T team(s[own], threadIdx.x % T::LANES);
+  uint64_t* list = s_list[own];
+  const float* from = a.Z + i * a.ld_z;
+  Row row;
+  row.load(from, a.C, team.t);
+  float top, low;
+  int32_t lanes;
+  if (!row_range(team, row, &top, &low, &lanes)) {
+    write_none(a, team, (int32_t)i);
+    return;
+  }
+  const Border b = first_entries(team, row, from, a.C, a.k, top, low, lanes);
+  if (team.t == 0) team.s.count = 0;
+  team.sync();
+  double in, out;
+  collect(team, row, b, top, a.inv_t, list, &in, &out);
+  in = team.sum(in);
+  out = team.sum(out);
+  team.sync();
+  write_top(a, team, list, (int32_t)i, top, in, out);
+}
+
+struct TopKernel {
+  template <int G, int W, class Row>
+  static constexpr auto of() { return top_kernel<G, W, Row>; }
+};
+
+}  // namespace
+
+extern "C" {
+
+size_t gnn_top_workspace_bytes(int32_t n, int32_t C, int32_t k) {
+  if (n < 0 || C <= 0 || C > MOST_COLS || k <= 0 || k > MOST_TOP || C <= LONG_COLS) return 0;
+  return top_long_bytes(n, C, k);
+}
+
+gnn_status gnn_top_logits(int32_t n, int32_t C, const float* Z, int64_t ld_z, int32_t k,
+                          double temperature, int32_t* index, float* logq, float* rest,
+                          void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (n < 0 || C <= 0 || C > MOST_COLS || ld_z < C || k <= 0 || k > MOST_TOP ||
+      !temperature_ok(temperature))
+    return GNN_ERR_SHAPE;
+  if (n == 0) return GNN_OK;
+  if (!Z || !index || !logq) return GNN_ERR_NULL;
+  if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
+  const size_t need = gnn_top_workspace_bytes(n, C, k);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return GNN_ERR_WORKSPACE;
+  {
+    const void* outs[] = {index, logq, rest, workspace};
+    const size_t outb[] = {(size_t)n * k * 4, (size_t)n * k * 4, (size_t)n * 4, need};
+    for (int i = 0; i < 4; ++i) {
+      if (ranges_overlap(outs[i], outb[i], Z, mat_bytes(n, C, ld_z))) return GNN_ERR_ALIAS;
+      for (int q = 0; q < i; ++q)
+        if (ranges_overlap(outs[i], outb[i], outs[q], outb[q])) return GNN_ERR_ALIAS;
+    }
+  }
+  TopArgs a = {};
+  a.n = n;
+  a.C = C;
+  a.Z = Z;
+  a.ld_z = ld_z;
+  a.k = k;
+  a.inv_t = 1.0 / temperature;
+  a.index = index;
+  a.logq = logq;
+  a.rest = rest;
+  timer_begin(GNN_K_SAMPLE, stream);
+  const hipError_t e = C > LONG_COLS ? top_long(a, workspace, stream)
+                                     : run(choose<TopArgs, TopKernel>(C), a, stream);
+  timer_end(GNN_K_SAMPLE, 4.0 * n * C, stream);
+  GNN_HIP(e);
+  return GNN_OK;
+}
+
+}  // extern "C"
