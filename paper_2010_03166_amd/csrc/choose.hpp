@@ -16,7 +16,7 @@
 namespace gnnprop {
 
 // Rows past so many columns are shared by several blocks.
-constexpr int32_t LONG_COLS = 16384;
+constexpr int32_t LONG_SAMPLE = 32768, LONG_TOP = 16384;
 
 // 2^(i / 64), from the series of exp.
 constexpr double exp2_64th(int i) {
@@ -97,6 +97,7 @@ struct SampleArgs {
   double unit;  // 2^-bits where a sum of weights is that of the log-probabilities, or 0
   int32_t* action;
   float* logp;
+  int32_t group;  // see row_range
   int64_t block0;
   // rows that several blocks share (long_rows.hip)
   struct LongRow* rows;
@@ -138,11 +139,12 @@ struct Present {
   __device__ __forceinline__ uint64_t operator()(float z, int32_t) const { return z > -INFINITY; }
 };
 
-// A row's largest logit, whether it is a finite number and none is a NaN; how
-// many lanes hold a logit, and the least of what they hold the largest of.
+// A row's largest logit, whether it is a finite number and none is a NaN; and of
+// groups of `group` lanes (a power of two, at most G) how many hold a logit, and
+// the least of what they hold the largest of.
 template <class T, class Row>
-__device__ __forceinline__ bool row_range(const T& team, const Row& row, float* top, float* low,
-                                          int32_t* lanes) {
+__device__ __forceinline__ bool row_range(const T& team, const Row& row, int32_t group, float* top,
+                                          float* low, int32_t* groups) {
   float most = -INFINITY;
   bool bad = false;
   row.each4([&](int32_t, f4 z) INLINE {
@@ -150,19 +152,31 @@ __device__ __forceinline__ bool row_range(const T& team, const Row& row, float* 
     bad |= __builtin_isunordered(z.x, z.y) | __builtin_isunordered(z.z, z.w);
   });
   constexpr int32_t BAD = 1 << 16;
+  if (T::G > 1 && group > 1) most = fmaxf(most, butterfly<1>(most));
+  if (T::G > 2 && group > 2) most = fmaxf(most, butterfly<2>(most));
+  if (T::G > 4 && group > 4) most = fmaxf(most, butterfly<4>(most));
+  if (T::G > 8 && group > 8) most = fmaxf(most, butterfly<8>(most));
   *top = most;
   *low = most > -INFINITY ? most : INFINITY;
-  *lanes = (most > -INFINITY) + (bad ? BAD : 0);
-  team.range(top, low, lanes);
-  return *lanes < BAD && fabsf(*top) < INFINITY;
+  *groups = (most > -INFINITY && team.lane % group == 0) + (bad ? BAD : 0);
+  team.range(top, low, groups);
+  return *groups < BAD && fabsf(*top) < INFINITY;
+}
+// Groups of so many lanes that there are k of them where the row is not masked:
+// the first k entries are then found above the least group's largest.
+inline int32_t group_of(int64_t lanes, int32_t C, int32_t k) {
+  const int64_t held = std::min<int64_t>(lanes, ceil_div(C, 4));
+  int32_t g = 1;
+  while (g < 16 && held / (2 * g) > k) g *= 2;
+  return g;
 }
 
-// The border of the first k entries; low and lanes from row_range().
+// The border of the first k entries; low and groups from row_range().
 template <class T, class Row>
 __device__ __forceinline__ Border first_entries(const T& team, Row& row, const float* from,
                                                 int32_t C, int32_t k, float top, float low,
-                                                int32_t lanes, int32_t base_col = 0) {
-  if (k > lanes) {  // (else as many entries as lanes are not below `low`)
+                                                int32_t groups, int32_t base_col = 0) {
+  if (k > groups) {  // (else as many entries as groups are not below `low`)
     low = INFINITY;
     row.each([&](float z, int32_t) INLINE { low = fminf(low, z > -INFINITY ? z : INFINITY); });
     low = -team.max(-low);
@@ -257,6 +271,7 @@ struct TopArgs {
   double inv_t;
   int32_t* index;
   float *logq, *rest;
+  int32_t group;  // see row_range
   int64_t block0;
   // rows that several blocks share (long_rows.hip)
   struct TopPart* parts;
@@ -344,7 +359,8 @@ __device__ __forceinline__ void write_none(const TopArgs& a, const T& team, int3
 template <class Args>
 struct Launch {
   void (*kernel)(Args);
-  int32_t rows, threads;
+  int32_t rows, threads;  // of a block
+  int32_t lanes() const { return threads / rows; }
 };
 #define LAUNCH(G, W, ROW)                                                        \
   Launch<Args>{Kernel::template of<G, W, ROW>(), threads_of<G, W>() / (G * W), \
@@ -361,7 +377,7 @@ Launch<Args> few(int32_t v) {
   return v == 3 ? held<Args, Kernel, G, 1, 3>() : held<Args, Kernel, G, 1, 4>();
 }
 
-// Rows of at most LONG_COLS columns.
+// Rows of at most LONG_SAMPLE columns.
 template <class Args, class Kernel>
 Launch<Args> choose(int32_t C) {
   const int32_t q = (int32_t)ceil_div(C, 4);
@@ -378,7 +394,8 @@ Launch<Args> choose(int32_t C) {
   if (q <= 512) return held<Args, Kernel, 64, 1, 8>();
   if (q <= 1024) return held<Args, Kernel, 64, 4, 4>();
   if (q <= 2048) return held<Args, Kernel, 64, 4, 8>();
-  return held<Args, Kernel, 64, 8, 8>();
+  if (q <= 4096) return held<Args, Kernel, 64, 8, 8>();
+  return held<Args, Kernel, 64, 16, 8>();
 }
 
 template <class Args>
@@ -390,7 +407,7 @@ hipError_t run(const Launch<Args>& l, Args a, hipStream_t stream) {
 }
 
 
-// Rows past LONG_COLS (long_rows.hip).
+// Rows past LONG_SAMPLE and LONG_TOP columns (long_rows.hip).
 size_t sample_long_bytes(int32_t n, int32_t C);
 hipError_t sample_long(SampleArgs a, void* workspace, hipStream_t stream);
 size_t top_long_bytes(int32_t n, int32_t C, int32_t k);

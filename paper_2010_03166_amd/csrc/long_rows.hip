@@ -1,5 +1,5 @@
-// Drawing actions from and finding the top logits of rows past LONG_COLS
-// columns: parts of 4,096, a block each, and what is one of a row joined from
+// Drawing actions from and finding the top logits of rows past 32,768
+// and 16,384 columns: parts of 4,096, a block each, and what is one of a row joined from
 // them by every block alike or by a launch of a block a row.  A draw reads its
 // row once for its range, twice for each border that is asked for, once for the
 // kept sums and a part of it for the action, out of the caches for the few rows
@@ -9,7 +9,22 @@
 
 namespace gnnprop {
 
-using PartTeam = Team<64, 4>;
+// More bins and longer lists than for rows of a block: of 131,071 logits spread
+// like a normal distribution some 200 lie in one.
+template <int G, int W>
+struct LongBins : Exchange<G, W> {
+  static constexpr int BINS = 1024, LIST = 1024;
+  uint64_t bins[BINS + G];
+  uint64_t amount[LIST];
+  uint64_t place[LIST];
+  uint64_t lo, hi;
+  Border border;
+  int32_t count;
+};
+using PartTeam = Team<64, 4, LongBins>;   // a part's
+using RowTeam = Team<64, 16, LongBins>;   // a row's, where one block has all of it
+using SumTeam = Team<64, 4, Exchange>;    // a part's, of which only sums are formed
+using TopTeam = Team<64, 4>;
 using PartRow = Held<64, 4, 4>;
 constexpr int32_t PART_COLS = PartRow::MOST;
 constexpr int BINS = PartTeam::Shared::BINS, LIST = PartTeam::Shared::LIST;
@@ -20,15 +35,17 @@ constexpr int32_t BAD_LANES = 1 << 16;  // (row_range's mark, in a part's count 
 struct Search {
   uint64_t bins[BINS];
   uint64_t place[LIST], amount[LIST];
-  int32_t count, pad;
+  uint64_t wanted, base;  // the amount looked for, and what lies in bins before
+  int32_t bin;            // the border's (-1: all are kept)
+  int32_t count;          // entries in it
 };
 struct LongRow {
   Search of[2];    // of the first top_k, of top_p's share
   Border kept[2];  // what is kept up to there
 };
 struct LongPart {
-  float top, low, least;  // largest, least of the lanes' largest, least logit
-  int32_t lanes;          // with a logit
+  float top, low, least;  // largest, least of the groups' largest, least logit
+  int32_t lanes;          // groups with a logit
   double sum;             // of exp(z - top)
   uint64_t kept;          // weights
 };
@@ -50,11 +67,11 @@ struct Joined {
   int32_t lanes;
   bool ok;
 };
-template <class P>
-__device__ __forceinline__ Joined joined(const PartTeam& team, const P* parts, int32_t count) {
+template <class T, class P>
+__device__ __forceinline__ Joined joined(const T& team, const P* parts, int32_t count) {
   Joined x = {-INFINITY, INFINITY, INFINITY, 0, true};
   bool bad = false;
-  for (int32_t k = team.t; k < count; k += THREADS) {
+  for (int32_t k = team.t; k < count; k += T::LANES) {
     x.top = fmaxf(x.top, parts[k].top);
     const int32_t lanes = parts[k].lanes;
     bad |= lanes >= BAD_LANES;
@@ -85,8 +102,8 @@ __device__ __forceinline__ Where where(const Args& a) {
 // ------------------------------------------------------------------ draws
 
 __global__ __launch_bounds__(THREADS) void long_range_kernel(SampleArgs a) {
-  __shared__ PartTeam::Shared s;
-  const PartTeam team(s, threadIdx.x);
+  __shared__ SumTeam::Shared s;
+  const SumTeam team(s, threadIdx.x);
   const Where at = where(a);
   const float* from = a.Z + at.i * a.ld_z;
   PartRow row;
@@ -99,7 +116,7 @@ __global__ __launch_bounds__(THREADS) void long_range_kernel(SampleArgs a) {
     if (at.part == 0 && team.t == 0) mine.of[w].count = 0;
   }
   LongPart p = {};
-  row_range(team, row, &p.top, &p.low, &p.lanes);
+  row_range(team, row, a.group, &p.top, &p.low, &p.lanes);
   p.least = INFINITY;
   if (a.top_k) {
     row.each([&](float z, int32_t) INLINE { p.least = fminf(p.least, z > -INFINITY ? z : INFINITY); });
@@ -123,10 +140,11 @@ __device__ __forceinline__ Look look_for(const SampleArgs& a, int which, const J
   const float scale = (BINS - 1) / (x.top - from);
   return {scale < INFINITY ? scale : 0.f, from};
 }
-__device__ __forceinline__ uint64_t wanted(const SampleArgs& a, int which, const PartTeam& team) {
+template <class T>
+__device__ __forceinline__ uint64_t wanted(const SampleArgs& a, int which, const T& team) {
   if (which == 0) return (uint64_t)a.top_k;
   uint64_t all = 0;
-  for (int k = team.t; k < BINS; k += THREADS) all += team.s.bins[k];
+  for (int k = team.t; k < BINS; k += T::LANES) all += team.s.bins[k];
   all = team.sum(all);
   const uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
   return P < 1 ? 1 : P < all ? P : all;
@@ -174,24 +192,31 @@ __global__ __launch_bounds__(THREADS) void long_bins_kernel(SampleArgs a) {
                 (unsigned long long)s.bins[k]);
 }
 
-// The row's bins in the block's, and the border's.
+// A block a row: the border's bin.
 template <int WHICH>
-__device__ __forceinline__ bool long_find(const SampleArgs& a, const PartTeam& team,
-                                          const LongRow& mine, uint64_t* P, int32_t* bin,
-                                          uint64_t* base) {
-  for (int k = team.t; k < BINS; k += THREADS) team.s.bins[k] = mine.of[WHICH].bins[k];
-  if (team.t == 0) team.s.count = 0;
+__global__ __launch_bounds__(THREADS) void long_find_kernel(SampleArgs a) {
+  __shared__ PartTeam::Shared s;
+  const PartTeam team(s, threadIdx.x);
+  Search& mine = a.rows[a.block0 + blockIdx.x].of[WHICH];
+  for (int k = team.t; k < BINS; k += THREADS) s.bins[k] = mine.bins[k];
   team.sync();
-  *P = wanted(a, WHICH, team);
-  return team.find(*P, bin, base);
+  const uint64_t P = wanted(a, WHICH, team);
+  int32_t bin = -1;
+  uint64_t base = 0;
+  if (!team.find(P, &bin, &base)) bin = -1;
+  if (team.t) return;
+  mine.wanted = P;
+  mine.base = base;
+  mine.bin = bin;
 }
 
-template <int WHICH>
+// The entries of the border's bin go to the row's list; LAST: it is the last
+// border, and the weights of the bins before it are added up.
+template <int WHICH, bool LAST>
 __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
-  __shared__ PartTeam::Shared s;
+  __shared__ SumTeam::Shared s;
   __shared__ double s_table[64];
-  __shared__ int32_t s_at;
-  const PartTeam team(s, threadIdx.x);
+  const SumTeam team(s, threadIdx.x);
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
@@ -199,89 +224,118 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
   LongRow& mine = a.rows[at.i];
-  uint64_t P, base;
-  int32_t bin;
-  if (!long_find<WHICH>(a, team, mine, &P, &bin, &base)) return;
+  Search& to = mine.of[WHICH];
+  const int32_t bin = to.bin;
   const Look look = look_for(a, WHICH, x);
-  const Weights weight = weights_of(a, s_table, WHICH, x, mine);
+  Weights weight = weights_of(a, s_table, WHICH, x, mine);
+  if (bin >= 0)
+    row.each4([&](int32_t col, f4 z) INLINE {
+      bool in[4], any = false;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) any |= in[j] = RowTeam::bin_of(z[j], x.top, look.scale) == bin;
+      if (!any) return;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint64_t amount = !in[j] ? 0 : WHICH == 0 ? z[j] > -INFINITY : weight(z[j], col + j);
+        if (!amount) continue;
+        const int32_t k = atomicAdd(&to.count, 1);
+        if (k >= LIST) continue;
+        to.place[k] = place(z[j], col + j);
+        to.amount[k] = amount;
+      }
+    });
+  if (!LAST) return;
+  if (a.cut > -INFINITY) weight.kept = earlier(weight.kept, near_entries(x.top, a.cut));
+  uint64_t sum = 0;
   row.each4([&](int32_t col, f4 z) INLINE {
     bool in[4], any = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      any |= in[j] = PartTeam::bin_of(z[j], x.top, look.scale) == bin;
-    if (!any) return;
-#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint64_t amount = !in[j] ? 0 : WHICH == 0 ? z[j] > -INFINITY : weight(z[j], col + j);
-      if (amount) team.list(z[j], col + j, amount);
+      in[j] = within(weight.kept, z[j], col + j) &
+              (bin < 0 || RowTeam::bin_of(z[j], x.top, look.scale) < bin);
+      any |= in[j];
     }
+    if (!any) return;
+    uint64_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = weight.all(z[j]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum += in[j] ? w[j] : 0;
   });
-  team.sync();
-  const int32_t own = s.count;
-  if (own == 0) return;
-  Search& to = mine.of[WHICH];
-  if (team.t == 0) s_at = atomicAdd(&to.count, min(own, LIST + 1));
-  team.sync();
-  const int32_t first = s_at;
-  for (int32_t k = team.t; k < min(own, LIST); k += THREADS)
-    if (first + k < LIST) {
-      to.place[first + k] = s.place[k];
-      to.amount[first + k] = s.amount[k];
-    }
+  sum = team.sum(sum);
+  if (team.t == 0) a.parts[at.i * a.per_row + at.part].kept = sum;
 }
 
-// A block a row: the border.
-template <int WHICH>
-__global__ __launch_bounds__(THREADS) void long_border_kernel(SampleArgs a) {
-  __shared__ PartTeam::Shared s;
+// A block a row: the border.  LAST: the weights of what is kept of its bin are
+// added to their parts'.
+template <int WHICH, bool LAST>
+__global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
+  __shared__ RowTeam::Shared s;
   __shared__ double s_table[64];
-  const PartTeam team(s, threadIdx.x);
+  const RowTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
   if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
-  const Joined x = joined(team, a.parts + i * a.per_row, a.per_row);
+  LongPart* parts = a.parts + i * a.per_row;
+  const Joined x = joined(team, parts, a.per_row);
   if (!x.ok) return;
   LongRow& mine = a.rows[i];
-  uint64_t P, base;
-  int32_t bin;
+  const Search& found = mine.of[WHICH];
+  const int32_t bin = found.bin, m = found.count;
+  const uint64_t P = found.wanted, base = found.base;
+  const Look look = look_for(a, WHICH, x);
+  Weights weight = weights_of(a, s_table, WHICH, x, mine);
+  Reread<64, 16> row;
+  row.load(a.Z + i * a.ld_z, a.C, team.t);
   Border b = NO_BORDER;
-  if (long_find<WHICH>(a, team, mine, &P, &bin, &base)) {
-    const Search& found = mine.of[WHICH];
-    const int32_t m = found.count;
-    team.sync();  // (all have read the bins)
+  if (bin >= 0) {
     if (m <= LIST) {
-      for (int32_t k = team.t; k < m; k += THREADS) {
+      for (int32_t k = team.t; k < m; k += 1024) {
         s.place[k] = found.place[k];
         s.amount[k] = found.amount[k];
       }
       if (team.t == 0) s.count = m;
       team.sync();
       b = team.settle(P, base);
+    } else if (WHICH == 0) {
+      b = team.search(row, Present(), x.top, look.scale, bin, P, base);
     } else {
-      const Look look = look_for(a, WHICH, x);
-      Reread<64, 4> row;
-      row.load(a.Z + i * a.ld_z, a.C, team.t);
-      if (WHICH == 0)
-        b = team.search(row, Present(), x.top, look.scale, bin, P, base);
-      else
-        b = team.search(row, weights_of(a, s_table, WHICH, x, mine), x.top, look.scale, bin, P,
-                        base);
+      b = team.search(row, weight, x.top, look.scale, bin, P, base);
     }
   }
-  if (team.t == 0) mine.kept[WHICH] = b;
+  weight.kept = b;
+  if (LAST && a.cut > -INFINITY) weight.kept = earlier(b, near_entries(x.top, a.cut));
+  if (team.t == 0) mine.kept[WHICH] = weight.kept;
+  if (!LAST || bin < 0) return;
+  const auto add = [&](float z, int32_t col) INLINE {
+    const uint64_t w = weight(z, col);
+    if (w)
+      atomicAdd(reinterpret_cast<unsigned long long*>(&parts[col / PART_COLS].kept),
+                (unsigned long long)w);
+  };
+  if (m <= LIST) {
+    for (int32_t k = team.t; k < m; k += 1024)
+      add(logit_of(found.place[k]), (int32_t)(uint32_t)found.place[k]);
+  } else {
+    row.each([&](float z, int32_t col) INLINE {
+      if (RowTeam::bin_of(z, x.top, look.scale) == bin) add(z, col);
+    });
+  }
 }
 
 __device__ __forceinline__ Weights final_weights(const SampleArgs& a, const double* table,
                                                  const Joined& x, const LongRow& mine) {
-  Weights w = {Exponential(table, a.scale, a.bits), x.top,
-               a.top_p < 1.0 ? mine.kept[1] : a.top_k ? mine.kept[0] : NO_BORDER};
-  if (a.cut > -INFINITY) w.kept = earlier(w.kept, near_entries(x.top, a.cut));
+  Weights w = {Exponential(table, a.scale, a.bits), x.top, NO_BORDER};
+  if (a.top_p < 1.0) w.kept = mine.kept[1];
+  else if (a.top_k) w.kept = mine.kept[0];
+  else if (a.cut > -INFINITY) w.kept = near_entries(x.top, a.cut);
   return w;
 }
 
+// The parts' weights, where no border was searched.
 __global__ __launch_bounds__(THREADS) void long_kept_kernel(SampleArgs a) {
-  __shared__ PartTeam::Shared s;
+  __shared__ SumTeam::Shared s;
   __shared__ double s_table[64];
-  const PartTeam team(s, threadIdx.x);
+  const SumTeam team(s, threadIdx.x);
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
@@ -298,11 +352,11 @@ __global__ __launch_bounds__(THREADS) void long_kept_kernel(SampleArgs a) {
 // A block a row: its log-sum, the part that holds the random number's share of
 // the kept sum (temperature 0: the first with the largest), and the action.
 __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
-  __shared__ PartTeam::Shared s;
+  __shared__ SumTeam::Shared s;
   __shared__ double s_table[64];
   __shared__ int32_t s_part;
   __shared__ uint64_t s_target;
-  const PartTeam team(s, threadIdx.x);
+  const SumTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
   if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
   const LongPart* parts = a.parts + i * a.per_row;
@@ -382,16 +436,16 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
 // ------------------------------------------------------------- top logits
 
 __global__ __launch_bounds__(THREADS) void top_part_kernel(TopArgs a) {
-  __shared__ PartTeam::Shared s;
+  __shared__ TopTeam::Shared s;
   __shared__ uint64_t s_list[MOST_TOP];
-  const PartTeam team(s, threadIdx.x);
+  const TopTeam team(s, threadIdx.x);
   const Where at = where(a);
   const float* from = a.Z + at.i * a.ld_z;
   PartRow row;
   row.load(from, a.C, team.t, at.col0);
   TopPart p = {};
   float low;
-  const bool ok = row_range(team, row, &p.top, &low, &p.lanes);
+  const bool ok = row_range(team, row, a.group, &p.top, &low, &p.lanes);
   const int64_t part = at.i * a.per_row + at.part;
   uint64_t* to = a.candidates + part * a.k;
   int32_t m = 0;
@@ -412,10 +466,12 @@ __global__ __launch_bounds__(THREADS) void top_part_kernel(TopArgs a) {
   if (team.t == 0) a.parts[part] = p;
 }
 
-__global__ __launch_bounds__(THREADS) void top_join_kernel(TopArgs a) {
-  __shared__ PartTeam::Shared s;
+template <int W>
+__global__ __launch_bounds__(64 * W) void top_join_kernel(TopArgs a) {
+  using JoinTeam = Team<64, W>;
+  __shared__ typename JoinTeam::Shared s;
   __shared__ uint64_t s_list[MOST_TOP];
-  const PartTeam team(s, threadIdx.x);
+  const JoinTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
   const TopPart* parts = a.parts + i * a.per_row;
   const Joined x = joined(team, parts, a.per_row);
@@ -423,7 +479,7 @@ __global__ __launch_bounds__(THREADS) void top_join_kernel(TopArgs a) {
     write_none(a, team, (int32_t)i);
     return;
   }
-  const Listed<64, 4> row = {a.candidates + i * a.per_row * a.k, (int64_t)a.per_row * a.k, team.t};
+  const Listed<64, W> row = {a.candidates + i * a.per_row * a.k, (int64_t)a.per_row * a.k, team.t};
   float top = -INFINITY, low;
   row.each([&](float z, int32_t) INLINE { top = fmaxf(top, z); });
   low = top > -INFINITY ? top : INFINITY;
@@ -443,7 +499,7 @@ __global__ __launch_bounds__(THREADS) void top_join_kernel(TopArgs a) {
       out += e;
     }
   });
-  for (int32_t k = team.t; k < a.per_row; k += THREADS)
+  for (int32_t k = team.t; k < a.per_row; k += JoinTeam::LANES)
     if (parts[k].others != 0.0)
       out += parts[k].others * exp_exact(((double)parts[k].top - top) * a.inv_t);
   in = team.sum(in);
@@ -453,9 +509,10 @@ __global__ __launch_bounds__(THREADS) void top_join_kernel(TopArgs a) {
 }
 
 template <class Args>
-void launch(void (*kernel)(Args), Args a, int64_t blocks, hipStream_t stream) {
+void launch(void (*kernel)(Args), Args a, int64_t blocks, hipStream_t stream,
+            int32_t threads = THREADS) {
   for (a.block0 = 0; a.block0 < blocks; a.block0 += LAUNCH_BLOCKS)
-    kernel<<<(unsigned)std::min(blocks - a.block0, LAUNCH_BLOCKS), THREADS, 0, stream>>>(a);
+    kernel<<<(unsigned)std::min(blocks - a.block0, LAUNCH_BLOCKS), threads, 0, stream>>>(a);
 }
 
 size_t rows_bytes(int32_t n) { return round_up((size_t)n * sizeof(LongRow), 256); }
@@ -470,20 +527,27 @@ hipError_t sample_long(SampleArgs a, void* workspace, hipStream_t stream) {
   a.rows = static_cast<LongRow*>(workspace);
   a.parts = reinterpret_cast<LongPart*>(static_cast<char*>(workspace) + rows_bytes(a.n));
   a.per_row = parts_of(a.C);
+  a.group = a.top_k ? group_of((int64_t)a.per_row * THREADS, a.C, a.top_k) : 1;
   const int64_t blocks = (int64_t)a.n * a.per_row;
   launch(long_range_kernel, a, blocks, stream);
   if (a.scale > 0.0) {
-    if (a.top_k) {
-      launch(long_bins_kernel<0>, a, blocks, stream);
-      launch(long_list_kernel<0>, a, blocks, stream);
-      launch(long_border_kernel<0>, a, a.n, stream);
-    }
-    if (a.top_p < 1.0) {
-      launch(long_bins_kernel<1>, a, blocks, stream);
-      launch(long_list_kernel<1>, a, blocks, stream);
-      launch(long_border_kernel<1>, a, a.n, stream);
-    }
-    launch(long_kept_kernel, a, blocks, stream);
+    const auto search = [&](auto bins, auto find, auto list, auto border) {
+      launch(bins, a, blocks, stream);
+      launch(find, a, a.n, stream);
+      launch(list, a, blocks, stream);
+      launch(border, a, a.n, stream, RowTeam::LANES);
+    };
+    if (a.top_k && a.top_p < 1.0)
+      search(long_bins_kernel<0>, long_find_kernel<0>, long_list_kernel<0, false>,
+             long_border_kernel<0, false>);
+    else if (a.top_k)
+      search(long_bins_kernel<0>, long_find_kernel<0>, long_list_kernel<0, true>,
+             long_border_kernel<0, true>);
+    if (a.top_p < 1.0)
+      search(long_bins_kernel<1>, long_find_kernel<1>, long_list_kernel<1, true>,
+             long_border_kernel<1, true>);
+    else if (!a.top_k)
+      launch(long_kept_kernel, a, blocks, stream);
   }
   launch(long_draw_kernel, a, a.n, stream);
   return hipGetLastError();
@@ -500,8 +564,12 @@ hipError_t top_long(TopArgs a, void* workspace, hipStream_t stream) {
   a.parts = static_cast<TopPart*>(workspace);
   a.candidates = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) +
                                              round_up((size_t)blocks * sizeof(TopPart), 256));
+  a.group = group_of(THREADS, a.C, a.k);
   launch(top_part_kernel, a, blocks, stream);
-  launch(top_join_kernel, a, a.n, stream);
+  // (640 candidates a row, 2,000 rows: 19 us by 256 threads, 68 by 1,024; 8,192
+  // candidates, 64 rows: 30 and 15)
+  if ((int64_t)a.per_row * a.k <= 2048) launch(top_join_kernel<4>, a, a.n, stream);
+  else launch(top_join_kernel<16>, a, a.n, stream, 1024);
   return hipGetLastError();
 }
 

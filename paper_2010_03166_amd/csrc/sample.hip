@@ -13,7 +13,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
   row.load(from, a.C, team.t);
   float top, low;
   int32_t lanes;
-  if (!row_range(team, row, &top, &low, &lanes)) {
+  if (!row_range(team, row, a.group, &top, &low, &lanes)) {
     if (team.t == 0) {
       a.action[i] = -1;
       if (a.logp) a.logp[i] = 0.f;
@@ -112,7 +112,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
 // Blocks that share a CU, by the registers that a row takes.
 template <int G, int W, class Row>
 constexpr int blocks_of() {
-  const int waves = W < 16 && Row::CHUNKS > 4 ? 12 : 16;  // of a CU
+  const int waves = W < 8 && Row::CHUNKS > 4 ? 12 : 16;  // of a CU
   return waves * 64 / threads_of<G, W>();
 }
 
@@ -141,7 +141,7 @@ struct SampleKernel {
 extern "C" {
 
 size_t gnn_sample_workspace_bytes(int32_t n, int32_t C) {
-  if (n < 0 || C <= 0 || C > MOST_COLS || C <= LONG_COLS) return 0;
+  if (n < 0 || C <= 0 || C > MOST_COLS || C <= LONG_SAMPLE) return 0;
   return sample_long_bytes(n, C);
 }
 
@@ -189,9 +189,14 @@ gnn_status gnn_sample_actions(int32_t n, int32_t C, const float* Z, int64_t ld_z
   a.action = action;
   a.logp = logp;
   timer_begin(GNN_K_SAMPLE, stream);
-  const hipError_t e = C > LONG_COLS
-                           ? sample_long(a, workspace, stream)
-                           : run(choose<SampleArgs, SampleKernel>(C), a, stream);
+  hipError_t e;
+  if (C > LONG_SAMPLE) {
+    e = sample_long(a, workspace, stream);
+  } else {
+    const Launch<SampleArgs> l = choose<SampleArgs, SampleKernel>(C);
+    a.group = a.top_k ? group_of(l.lanes(), C, a.top_k) : 1;
+    e = run(l, a, stream);
+  }
   timer_end(GNN_K_SAMPLE, 4.0 * n * C, stream);
   GNN_HIP(e);
   return GNN_OK;

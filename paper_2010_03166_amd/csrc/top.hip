@@ -23,7 +23,7 @@ __global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
   row.load(from, a.C, team.t);
   float top, low;
   int32_t lanes;
-  if (!row_range(team, row, &top, &low, &lanes)) {
+  if (!row_range(team, row, a.group, &top, &low, &lanes)) {
     write_none(a, team, (int32_t)i);
     return;
   }
@@ -48,7 +48,7 @@ struct TopKernel {
 extern "C" {
 
 size_t gnn_top_workspace_bytes(int32_t n, int32_t C, int32_t k) {
-  if (n < 0 || C <= 0 || C > MOST_COLS || k <= 0 || k > MOST_TOP || C <= LONG_COLS) return 0;
+  if (n < 0 || C <= 0 || C > MOST_COLS || k <= 0 || k > MOST_TOP || C <= LONG_TOP) return 0;
   return top_long_bytes(n, C, k);
 }
 
@@ -83,8 +83,14 @@ gnn_status gnn_top_logits(int32_t n, int32_t C, const float* Z, int64_t ld_z, in
   a.logq = logq;
   a.rest = rest;
   timer_begin(GNN_K_SAMPLE, stream);
-  const hipError_t e = C > LONG_COLS ? top_long(a, workspace, stream)
-                                     : run(choose<TopArgs, TopKernel>(C), a, stream);
+  hipError_t e;
+  if (C > LONG_TOP) {
+    e = top_long(a, workspace, stream);
+  } else {
+    const Launch<TopArgs> l = choose<TopArgs, TopKernel>(C);
+    a.group = group_of(l.lanes(), C, k);
+    e = run(l, a, stream);
+  }
   timer_end(GNN_K_SAMPLE, 4.0 * n * C, stream);
   GNN_HIP(e);
   return GNN_OK;
