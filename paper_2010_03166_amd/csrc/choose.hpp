@@ -48,13 +48,11 @@ inline int bits_of(int32_t C) {
 // out), added to 2^52, whose last bits the whole number then is.  The numbers
 // are kept in scalar registers: as literals they took two moves a step.
 struct Exponential {
-  const double* table;
+  const double* table;  // TABLE's numbers times 2^bits
   double scale;
-  int bits;
   double c1, c2, c3, c4, one52;
 
-  __device__ __forceinline__ Exponential(const double* t, double s, int b)
-      : table(t), scale(s), bits(b) {
+  __device__ __forceinline__ Exponential(const double* t, double s) : table(t), scale(s) {
     constexpr double a = 0.6931471805599453 / 64.0;
     c1 = scalar(a);
     c2 = scalar(a * a / 2.0);
@@ -76,7 +74,7 @@ struct Exponential {
     p = fma(p, f, c1);
     p = fma(p, f, 1.0);
     const uint64_t unit = (uint64_t)__double_as_longlong(table[q & 63]);
-    const uint32_t hi = (uint32_t)(unit >> 32) + ((uint32_t)((q >> 6) + bits) << 20);
+    const uint32_t hi = (uint32_t)(unit >> 32) + ((uint32_t)(q >> 6) << 20);
     const double e = __longlong_as_double((long long)((uint64_t)hi << 32 | (uint32_t)unit));
     return (uint64_t)__double_as_longlong(fma(e, p, one52)) & 0xfffffffffffffull;
   }
@@ -224,9 +222,10 @@ __device__ __forceinline__ uint64_t unit_fraction(float u) {
 }
 
 // The entry in whose weight `target` falls, counted from the first of the
-// wavefront's; sums: the lane's, by chunks (of a row that is read again: not
-// used).  The lane that holds it writes the row's action.
-template <class T, class Row>
+// wavefront's.  KEPT: `sums` has the lane's sums of its chunks' weights (else
+// they are formed again: one of several wavefronts does it).  The lane that holds
+// the entry writes the row's action.
+template <bool KEPT, class T, class Row>
 __device__ __forceinline__ void pick_entry(const SampleArgs& a, const T& team, const Row& row,
                                            const Weights& weight, int32_t i, uint64_t target,
                                            double lse, const uint64_t* sums) {
@@ -236,11 +235,9 @@ __device__ __forceinline__ void pick_entry(const SampleArgs& a, const T& team, c
   int32_t col = 0;
   f4 z = {};
   row.each4([&](int32_t at, f4 v) INLINE {
-    uint64_t sum = 0;
-    if (Row::CHUNKS > 0) sum = sums[at_chunk++];
+    const int k = at_chunk++;
     if (found) return;
-    if (Row::CHUNKS == 0) sum = weight.sum4(v, at);
-    sum = lanes_sum<T::G>(sum);
+    const uint64_t sum = lanes_sum<T::G>(KEPT ? sums[k] : weight.sum4(v, at));
     found = target < sum;
     if (!found) {
       target -= sum;
@@ -377,24 +374,30 @@ Launch<Args> few(int32_t v) {
   return v == 3 ? held<Args, Kernel, G, 1, 3>() : held<Args, Kernel, G, 1, 4>();
 }
 
-// Rows of at most LONG_SAMPLE columns.
+// Rows of at most LONG_SAMPLE columns.  As many lanes as a row takes at three or
+// four chunks each, up to a wavefront's 64 of eight; `places` (the length of a
+// list that each lane compares its share of with all) asks for a lane to four.
 template <class Args, class Kernel>
-Launch<Args> choose(int32_t C) {
+Launch<Args> choose(int32_t C, int32_t places = 0) {
   const int32_t q = (int32_t)ceil_div(C, 4);
-  if (q == 1) return held<Args, Kernel, 1, 1, 1>();
-  if (q == 2) return held<Args, Kernel, 1, 1, 2>();
-  if (q <= 4) return few<Args, Kernel, 1>(q);
-  if (q <= 8) return few<Args, Kernel, 2>((q + 1) / 2);
-  if (q <= 16) return few<Args, Kernel, 4>((q + 3) / 4);
-  if (q <= 32) return few<Args, Kernel, 8>((q + 7) / 8);
-  if (q <= 64) return few<Args, Kernel, 16>((q + 15) / 16);
-  if (q <= 128) return few<Args, Kernel, 32>((q + 31) / 32);
-  if (q <= 256) return few<Args, Kernel, 64>((q + 63) / 64);
+  if (q == 1) return {Kernel::template small<1>(), 256, 256};
+  if (q == 2) return {Kernel::template small<2>(), 256, 256};
+  if (q <= 4) return {Kernel::template small<4>(), 256, 256};
+  if (q <= 6) return {Kernel::template small<6>(), 256, 256};
+  if (C <= Kernel::SMALL) return {Kernel::template small<8>(), 256, 256};
+  const int32_t lanes = std::max(q, places);
+  const auto three = [&](int32_t lanes) { return ceil_div(q, lanes) <= 3 ? 3 : 4; };
+  if (lanes <= 16) return few<Args, Kernel, 4>(three(4));
+  if (lanes <= 32) return few<Args, Kernel, 8>(three(8));
+  if (lanes <= 64) return few<Args, Kernel, 16>(three(16));
+  if (lanes <= 128) return few<Args, Kernel, 32>(three(32));
+  if (q <= 256) return few<Args, Kernel, 64>(three(64));
   if (q <= 384) return held<Args, Kernel, 64, 1, 6>();
   if (q <= 512) return held<Args, Kernel, 64, 1, 8>();
   if (q <= 1024) return held<Args, Kernel, 64, 4, 4>();
   if (q <= 2048) return held<Args, Kernel, 64, 4, 8>();
   if (q <= 4096) return held<Args, Kernel, 64, 8, 8>();
+  if (q <= 6144) return held<Args, Kernel, 64, 16, 6>();
   return held<Args, Kernel, 64, 16, 8>();
 }
 

@@ -14,9 +14,10 @@ namespace gnnprop {
 template <int G, int W>
 struct LongBins : Exchange<G, W> {
   static constexpr int BINS = 1024, LIST = 1024;
-  uint64_t bins[BINS + G];
-  uint64_t amount[LIST];
-  uint64_t place[LIST];
+  alignas(16) uint64_t words[BINS + G + 2 * LIST];
+  __device__ __forceinline__ uint64_t* bins() { return words; }
+  __device__ __forceinline__ uint64_t* amount() { return words + BINS + G; }
+  __device__ __forceinline__ uint64_t* place() { return words + BINS + G + LIST; }
   uint64_t lo, hi;
   Border border;
   int32_t count;
@@ -144,14 +145,14 @@ template <class T>
 __device__ __forceinline__ uint64_t wanted(const SampleArgs& a, int which, const T& team) {
   if (which == 0) return (uint64_t)a.top_k;
   uint64_t all = 0;
-  for (int k = team.t; k < BINS; k += T::LANES) all += team.s.bins[k];
+  for (int k = team.t; k < BINS; k += T::LANES) all += team.s.bins()[k];
   all = team.sum(all);
   const uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
   return P < 1 ? 1 : P < all ? P : all;
 }
 __device__ __forceinline__ Weights weights_of(const SampleArgs& a, const double* table, int which,
                                               const Joined& x, const LongRow& mine) {
-  return {Exponential(table, a.scale, a.bits), x.top,
+  return {Exponential(table, a.scale), x.top,
           which == 1 && a.top_k ? mine.kept[0] : NO_BORDER};
 }
 
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(THREADS) void long_bins_kernel(SampleArgs a) {
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
-  if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
+  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
   LongRow& mine = a.rows[at.i];
@@ -187,9 +188,9 @@ __global__ __launch_bounds__(THREADS) void long_bins_kernel(SampleArgs a) {
   }
   team.sync();
   for (int k = team.t; k < BINS; k += THREADS)
-    if (s.bins[k])
+    if (s.bins()[k])
       atomicAdd(reinterpret_cast<unsigned long long*>(&mine.of[WHICH].bins[k]),
-                (unsigned long long)s.bins[k]);
+                (unsigned long long)s.bins()[k]);
 }
 
 // A block a row: the border's bin.
@@ -198,7 +199,7 @@ __global__ __launch_bounds__(THREADS) void long_find_kernel(SampleArgs a) {
   __shared__ PartTeam::Shared s;
   const PartTeam team(s, threadIdx.x);
   Search& mine = a.rows[a.block0 + blockIdx.x].of[WHICH];
-  for (int k = team.t; k < BINS; k += THREADS) s.bins[k] = mine.bins[k];
+  for (int k = team.t; k < BINS; k += THREADS) s.bins()[k] = mine.bins[k];
   team.sync();
   const uint64_t P = wanted(a, WHICH, team);
   int32_t bin = -1;
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
-  if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
+  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
   LongRow& mine = a.rows[at.i];
@@ -251,8 +252,8 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
     bool in[4], any = false;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      in[j] = within(weight.kept, z[j], col + j) &
-              (bin < 0 || RowTeam::bin_of(z[j], x.top, look.scale) < bin);
+      const bool ahead = bin < 0 || RowTeam::bin_of(z[j], x.top, look.scale) < bin;
+      in[j] = ahead && within(weight.kept, z[j], col + j);
       any |= in[j];
     }
     if (!any) return;
@@ -274,7 +275,7 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
   __shared__ double s_table[64];
   const RowTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
-  if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
+  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
   LongPart* parts = a.parts + i * a.per_row;
   const Joined x = joined(team, parts, a.per_row);
   if (!x.ok) return;
@@ -290,8 +291,8 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
   if (bin >= 0) {
     if (m <= LIST) {
       for (int32_t k = team.t; k < m; k += 1024) {
-        s.place[k] = found.place[k];
-        s.amount[k] = found.amount[k];
+        s.place()[k] = found.place[k];
+        s.amount()[k] = found.amount[k];
       }
       if (team.t == 0) s.count = m;
       team.sync();
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
 
 __device__ __forceinline__ Weights final_weights(const SampleArgs& a, const double* table,
                                                  const Joined& x, const LongRow& mine) {
-  Weights w = {Exponential(table, a.scale, a.bits), x.top, NO_BORDER};
+  Weights w = {Exponential(table, a.scale), x.top, NO_BORDER};
   if (a.top_p < 1.0) w.kept = mine.kept[1];
   else if (a.top_k) w.kept = mine.kept[0];
   else if (a.cut > -INFINITY) w.kept = near_entries(x.top, a.cut);
@@ -339,7 +340,7 @@ __global__ __launch_bounds__(THREADS) void long_kept_kernel(SampleArgs a) {
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
-  if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
+  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
   const Weights weight = final_weights(a, s_table, x, a.rows[at.i]);
@@ -358,7 +359,7 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
   __shared__ uint64_t s_target;
   const SumTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
-  if (team.t < 64) s_table[team.t] = TABLE.at[team.t];
+  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
   const LongPart* parts = a.parts + i * a.per_row;
   const Joined x = joined(team, parts, a.per_row);
   if (!x.ok) {
@@ -416,21 +417,15 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
   target = s_target;
   row.load(from, a.C, team.t, s_part * PART_COLS);
   const Weights weight = final_weights(a, s_table, x, a.rows[i]);
-  uint64_t sums[PartRow::CHUNKS];
-  int at_chunk = 0;
   own = 0;
-  row.each4([&](int32_t col, f4 z) INLINE {
-    const uint64_t sum = weight.sum4(z, col);
-    own += sum;
-    sums[at_chunk++] = sum;
-  });
+  row.each4([&](int32_t col, f4 z) INLINE { own += weight.sum4(z, col); });
   own = lanes_sum<64>(own);
   if (team.lane == 0) s.sums[team.wave] = own;
   team.sync();
   ahead = 0;
   for (int k = 0; k < team.wave; ++k) ahead += s.sums[k];
   if (target < ahead || target >= ahead + own) return;
-  pick_entry(a, team, row, weight, (int32_t)i, target - ahead, lse, sums);
+  pick_entry<false>(a, team, row, weight, (int32_t)i, target - ahead, lse, nullptr);
 }
 
 // ------------------------------------------------------------- top logits

@@ -7,7 +7,8 @@ using namespace gnnprop;
 namespace {
 
 template <class T, class Row>
-__device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, int32_t i, const double* table) {
+__device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, int32_t i,
+                                           const double* table) {
   const float* from = a.Z + (int64_t)i * a.ld_z;
   Row row;
   row.load(from, a.C, team.t);
@@ -37,7 +38,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
     }
     return;
   }
-  Weights weight = {Exponential(table, a.scale, a.bits), top, NO_BORDER};
+  Weights weight = {Exponential(table, a.scale), top, NO_BORDER};
   if (a.top_k) weight.kept = first_entries(team, row, from, a.C, a.top_k, top, low, lanes);
   if (a.top_p < 1.0) {
     const float scale = (T::Shared::BINS - 1) * a.inv_range;
@@ -83,13 +84,15 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
   }
   if (a.cut > -INFINITY) weight.kept = earlier(weight.kept, near_entries(top, a.cut));
   // the action that holds the random number's share of the sum
-  constexpr int KEPT = Row::CHUNKS > 0 ? Row::CHUNKS : 1;
-  uint64_t own = 0, sums[KEPT];
+  // (the lanes' sums by chunks are kept for the draw, but of 1,024 threads, which
+  // have no registers for them: 2,000 x 20,011 with top-p 302 us, 205 without)
+  constexpr bool KEPT = T::W < 16;
+  uint64_t own = 0, sums[KEPT ? Row::CHUNKS : 1];
   int at_chunk = 0;
   row.each4([&](int32_t col, f4 z) INLINE {
     const uint64_t sum = weight.sum4(z, col);
     own += sum;
-    if (Row::CHUNKS > 0) sums[at_chunk++] = sum;
+    if (KEPT) sums[at_chunk++] = sum;
   });
   own = lanes_sum<T::G>(own);
   uint64_t ahead = 0, all = own;
@@ -106,7 +109,7 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
   uint64_t target = __umul64hi(all, unit_fraction(a.u[i]));
   if (target < ahead || target >= ahead + own) return;
   target -= ahead;
-  pick_entry(a, team, row, weight, i, target, lse, sums);
+  pick_entry<KEPT>(a, team, row, weight, i, target, lse, sums);
 }
 
 // Blocks that share a CU, by the registers that a row takes.
@@ -122,7 +125,7 @@ __global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>())) voi
   constexpr int R = threads_of<G, W>() / T::LANES;
   __shared__ typename T::Shared s[R];
   __shared__ double s_table[64];
-  if (threadIdx.x < 64) s_table[threadIdx.x] = TABLE.at[threadIdx.x];
+  if (threadIdx.x < 64) s_table[threadIdx.x] = ldexp(TABLE.at[threadIdx.x], a.bits);
   __syncthreads();
   const int own = threadIdx.x / T::LANES;
   const int64_t i = (a.block0 + blockIdx.x) * R + own;
@@ -131,9 +134,110 @@ __global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>())) voi
   sample_row<T, Row>(a, team, (int32_t)i, s_table);
 }
 
+// Rows of up to 32 columns: a lane has one to itself, and what comes before an
+// entry is told by comparing it with every other one (no bins, nothing but the
+// exponentials' table in LDS).
+template <int V>
+__global__ __launch_bounds__(256) void sample_small_kernel(SampleArgs a) {
+  constexpr int N = 4 * V;
+  __shared__ double s_table[64];
+  if (threadIdx.x < 64) s_table[threadIdx.x] = ldexp(TABLE.at[threadIdx.x], a.bits);
+  __syncthreads();
+  const int64_t i = (a.block0 + blockIdx.x) * 256 + threadIdx.x;
+  if (i >= a.n) return;
+  Held<1, 1, V> row;
+  row.load(a.Z + i * a.ld_z, a.C, 0);
+  float z[N], top = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    z[j] = row.z[j / 4][j % 4];
+    top = fmaxf(top, z[j]);
+    bad |= z[j] != z[j];
+  }
+  if (bad || !(fabsf(top) < INFINITY)) {
+    a.action[i] = -1;
+    if (a.logp) a.logp[i] = 0.f;
+    return;
+  }
+  double lse = 0.0;
+  if (a.logp) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) lse += (double)sum4(exp4(row.z[k], top));
+    lse = log_quick((float)lse);
+  }
+  int32_t action = -1;
+  if (a.scale == 0.0) {
+#pragma unroll
+    for (int j = N - 1; j >= 0; --j) action = z[j] == top ? j : action;
+  } else {
+    const Exponential of(s_table, a.scale);
+    uint64_t w[N], all = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      w[j] = of((double)z[j] - top);
+      if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (four at a time have registers)
+    }
+    if (a.top_k) {
+      uint32_t kept = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        int32_t before = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q) before += q < j ? z[q] >= z[j] : z[q] > z[j];
+        kept |= (uint32_t)(before < a.top_k) << j;
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = kept >> j & 1 ? w[j] : 0;
+    }
+    if (a.top_p < 1.0) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) all += w[j];
+      uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
+      P = P < 1 ? 1 : P < all ? P : all;
+      uint32_t kept = 0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        uint64_t before = 0;
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+          if (q != j) before += (q < j ? z[q] >= z[j] : z[q] > z[j]) ? w[q] : 0;
+        kept |= (uint32_t)(before < P) << j;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = kept >> j & 1 ? w[j] : 0;
+    }
+    if (a.cut > -INFINITY) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) w[j] = (double)z[j] - top >= a.cut ? w[j] : 0;
+    }
+    all = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) all += w[j];
+    const uint64_t target = __umul64hi(all, unit_fraction(a.u[i]));
+    uint64_t sum = all;
+#pragma unroll
+    for (int j = N - 1; j >= 0; --j) {  // (the first that the target is below of)
+      action = target < sum ? j : action;
+      sum -= w[j];
+    }
+  }
+  a.action[i] = action;
+  if (!a.logp) return;
+  float za = z[0];
+#pragma unroll
+  for (int j = 1; j < N; ++j) za = action == j ? z[j] : za;
+  a.logp[i] = (float)((double)za - top - lse);
+}
+
 struct SampleKernel {
+  // (200,000 x 32, T = 1 without and with top-p 0.9: a lane a row 24 and 51 us)
+  static constexpr int SMALL = 24;
   template <int G, int W, class Row>
   static constexpr auto of() { return sample_kernel<G, W, Row>; }
+  template <int V>
+  static constexpr auto small() { return sample_small_kernel<V>; }
 };
 
 }  // namespace

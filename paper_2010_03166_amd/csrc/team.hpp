@@ -57,11 +57,14 @@ struct Exchange {
 // once.
 template <int G, int W>
 struct Bins : Exchange<G, W> {
-  static constexpr int BINS = W > 1 ? 512 : G == 64 ? 256 : G == 32 ? 128 : G >= 8 ? 64 : 8 * G;
-  static constexpr int LIST = W > 1 ? 256 : G == 64 ? 128 : G == 32 ? 64 : G >= 8 ? 32 : 16;
-  uint64_t bins[BINS + G];  // (the last G, one a lane, for entries that are in none)
-  uint64_t amount[LIST];
-  uint64_t place[LIST];
+  static constexpr int BINS = W > 1 ? 512 : G == 64 ? 256 : G >= 16 ? 128 : G == 8 ? 64 : 8 * G;
+  static constexpr int LIST = W > 1 ? 256 : G == 64 ? 128 : G >= 16 ? 64 : G == 8 ? 32 : 16;
+  static constexpr int WORDS = BINS + G + 2 * LIST;
+  alignas(16) uint64_t words[WORDS];
+  // the last G, one a lane, are for entries that are in no bin
+  __device__ __forceinline__ uint64_t* bins() { return words; }
+  __device__ __forceinline__ uint64_t* amount() { return words + BINS + G; }
+  __device__ __forceinline__ uint64_t* place() { return words + BINS + G + LIST; }
   uint64_t lo, hi;
   Border border;
   int32_t count;
@@ -197,12 +200,12 @@ struct Team {
   __device__ __forceinline__ bool find(uint64_t P, int32_t* bin, uint64_t* base) const {
     constexpr int EACH = Shared::BINS / G;
     uint64_t own = 0;
-    for (int k = 0; k < EACH; ++k) own += s.bins[lane * EACH + k];
+    for (int k = 0; k < EACH; ++k) own += s.bins()[lane * EACH + k];
     uint64_t sum = before(own);
     const bool has = sum < P && sum + own >= P;
     int32_t b = lane * EACH;
     if (has)
-      for (uint64_t x = s.bins[b]; sum + x < P; x = s.bins[++b]) sum += x;
+      for (uint64_t x = s.bins()[b]; sum + x < P; x = s.bins()[++b]) sum += x;
     uint64_t who = __ballot(has);
     if (G < 64) who = who >> ((threadIdx.x & 63) / G * G) & ((1ull << (G & 63)) - 1);
     if (!who) return false;
@@ -213,7 +216,7 @@ struct Team {
   }
 
   __device__ __forceinline__ void clear() const {
-    for (int k = t; k < Shared::BINS; k += LANES) s.bins[k] = 0;
+    for (int k = t; k < Shared::BINS; k += LANES) s.bins()[k] = 0;
     if (t == 0) {
       s.count = 0;
       s.lo = ~0ull;
@@ -226,22 +229,22 @@ struct Team {
     add(in ? bin : Shared::BINS + lane, x);
   }
   __device__ __forceinline__ void add(int32_t bin, uint64_t x) const {
-    atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins[bin]), (unsigned long long)x);
+    atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins()[bin]), (unsigned long long)x);
   }
   __device__ __forceinline__ void list(float z, int32_t col, uint64_t x) const {
     const int32_t at = atomicAdd(&s.count, 1);
     if (at >= Shared::LIST) return;
-    s.place[at] = place(z, col);
-    s.amount[at] = x;
+    s.place()[at] = place(z, col);
+    s.amount()[at] = x;
   }
   // The border among the entries listed, `base` being the amounts before them.
   __device__ __forceinline__ Border settle(uint64_t P, uint64_t base) const {
     const int32_t m = s.count;
     for (int32_t i = t; i < m; i += LANES) {
-      const uint64_t own = s.place[i], x = s.amount[i];
+      const uint64_t own = s.place()[i], x = s.amount()[i];
       uint64_t sum = base;
 #pragma unroll 4
-      for (int32_t j = 0; j < m; ++j) sum += s.place[j] < own ? s.amount[j] : 0;
+      for (int32_t j = 0; j < m; ++j) sum += s.place()[j] < own ? s.amount()[j] : 0;
       if (sum < P && sum + x >= P) {
         s.border = {logit_of(own), (int32_t)(uint32_t)own};
       }
@@ -434,7 +437,7 @@ struct Listed {
 
 template <int G, int W>
 constexpr int threads_of() {
-  return W > 1 ? 64 * W : G == 1 ? 64 : 256;
+  return W > 1 ? 64 * W : 256;
 }
 
 // (written so that a NaN is refused)

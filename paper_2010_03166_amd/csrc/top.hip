@@ -9,15 +9,15 @@ template <int G, int W, class Row>
 __global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
   using T = Team<G, W>;
   constexpr int R = threads_of<G, W>() / T::LANES;
-  constexpr int MOST = Row::MOST < MOST_TOP
-                           ? (Row::MOST + 7) / 8 * 8 : MOST_TOP;
   __shared__ typename T::Shared s[R];
-  __shared__ uint64_t s_list[R][MOST];
   const int own = threadIdx.x / T::LANES;
   const int64_t i = (a.block0 + blockIdx.x) * R + own;
   if (i >= a.n) return;
   const T team(s[own], threadIdx.x % T::LANES);
-  uint64_t* list = s_list[own];
+  // (once the border is known, the list takes the place of what found it)
+  static_assert(T::Shared::WORDS >= (Row::MOST < MOST_TOP ? (Row::MOST + 7) / 8 * 8 : MOST_TOP),
+                "a row's first entries fit");
+  uint64_t* list = s[own].words;
   const float* from = a.Z + i * a.ld_z;
   Row row;
   row.load(from, a.C, team.t);
@@ -38,9 +38,76 @@ __global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
   write_top(a, team, list, (int32_t)i, top, in, out);
 }
 
+// Rows of up to 32 columns: a lane has one to itself, and an entry's place is
+// the number of those before it.
+template <int V>
+__global__ __launch_bounds__(256) void top_small_kernel(TopArgs a) {
+  constexpr int N = 4 * V;
+  const int64_t i = (a.block0 + blockIdx.x) * 256 + threadIdx.x;
+  if (i >= a.n) return;
+  Held<1, 1, V> row;
+  row.load(a.Z + i * a.ld_z, a.C, 0);
+  int32_t* index = a.index + i * a.k;
+  float* logq = a.logq + i * a.k;
+  float z[N], top = -INFINITY;
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    z[j] = row.z[j / 4][j % 4];
+    top = fmaxf(top, z[j]);
+    bad |= z[j] != z[j];
+  }
+  const bool none = bad || !(fabsf(top) < INFINITY);
+  int32_t rank[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) rank[j] = 0;
+#pragma unroll
+  for (int j = 1; j < N; ++j)
+#pragma unroll
+    for (int q = 0; q < j; ++q) {
+      const bool first = z[q] >= z[j];
+      rank[j] += first;
+      rank[q] += !first;
+    }
+  const float octaves = (float)(a.inv_t * 1.4426950408889634);
+  double in = 0.0, out = 0.0;
+  int32_t m = 0;  // places that are used
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float more = 0.f, less = 0.f;
+#pragma unroll
+    for (int j = 4 * k; j < 4 * k + 4; ++j) {
+      const float e = __builtin_amdgcn_exp2f((z[j] - top) * octaves);
+      const bool kept = rank[j] < a.k;
+      more += kept ? e : 0.f;
+      less += kept ? 0.f : e;
+      m += kept & (z[j] > -INFINITY);
+    }
+    in += more;
+    out += less;
+  }
+  if (none) m = 0;
+  for (int32_t j = m; j < a.k; ++j) {
+    index[j] = -1;
+    logq[j] = -INFINITY;
+  }
+  if (a.rest) a.rest[i] = none ? 0.f : (float)(out / (in + out));
+  if (none) return;
+  const double lse = log_quick((float)(in + out));
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (rank[j] < m) {
+      index[rank[j]] = j;
+      logq[rank[j]] = (float)(((double)z[j] - top) * a.inv_t - lse);
+    }
+}
+
 struct TopKernel {
+  static constexpr int SMALL = 32;
   template <int G, int W, class Row>
   static constexpr auto of() { return top_kernel<G, W, Row>; }
+  template <int V>
+  static constexpr auto small() { return top_small_kernel<V>; }
 };
 
 }  // namespace
@@ -87,7 +154,7 @@ gnn_status gnn_top_logits(int32_t n, int32_t C, const float* Z, int64_t ld_z, in
   if (C > LONG_TOP) {
     e = top_long(a, workspace, stream);
   } else {
-    const Launch<TopArgs> l = choose<TopArgs, TopKernel>(C);
+    const Launch<TopArgs> l = choose<TopArgs, TopKernel>(C, k);
     a.group = group_of(l.lanes(), C, k);
     e = run(l, a, stream);
   }
