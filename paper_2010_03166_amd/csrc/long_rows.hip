@@ -238,7 +238,10 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const uint64_t amount = !in[j] ? 0 : WHICH == 0 ? z[j] > -INFINITY : weight(z[j], col + j);
-        if (!amount) continue;
+        // (a count past the list's end need not be exact)
+        if (!amount ||
+            __hip_atomic_load(&to.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > LIST)
+          continue;
         const int32_t k = atomicAdd(&to.count, 1);
         if (k >= LIST) continue;
         to.place[k] = place(z[j], col + j);
@@ -307,19 +310,28 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
   if (LAST && a.cut > -INFINITY) weight.kept = earlier(b, near_entries(x.top, a.cut));
   if (team.t == 0) mine.kept[WHICH] = weight.kept;
   if (!LAST || bin < 0) return;
-  const auto add = [&](float z, int32_t col) INLINE {
-    const uint64_t w = weight(z, col);
+  const auto give = [&](int32_t part, uint64_t w) INLINE {
     if (w)
-      atomicAdd(reinterpret_cast<unsigned long long*>(&parts[col / PART_COLS].kept),
-                (unsigned long long)w);
+      atomicAdd(reinterpret_cast<unsigned long long*>(&parts[part].kept), (unsigned long long)w);
   };
   if (m <= LIST) {
-    for (int32_t k = team.t; k < m; k += 1024)
-      add(logit_of(found.place[k]), (int32_t)(uint32_t)found.place[k]);
+    for (int32_t k = team.t; k < m; k += 1024) {
+      const int32_t col = (int32_t)(uint32_t)found.place[k];
+      give(col / PART_COLS, weight(logit_of(found.place[k]), col));
+    }
   } else {
+    int32_t part = 0;  // (a lane's columns ascend)
+    uint64_t sum = 0;
     row.each([&](float z, int32_t col) INLINE {
-      if (RowTeam::bin_of(z, x.top, look.scale) == bin) add(z, col);
+      if (RowTeam::bin_of(z, x.top, look.scale) != bin || !within(weight.kept, z, col)) return;
+      if (col / PART_COLS != part) {
+        give(part, sum);
+        part = col / PART_COLS;
+        sum = 0;
+      }
+      sum += weight.all(z);
     });
+    give(part, sum);
   }
 }
 

@@ -232,6 +232,9 @@ struct Team {
     atomicAdd(reinterpret_cast<unsigned long long*>(&s.bins()[bin]), (unsigned long long)x);
   }
   __device__ __forceinline__ void list(float z, int32_t col, uint64_t x) const {
+    // (a count past the list's end need not be exact)
+    if (__hip_atomic_load(&s.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) > Shared::LIST)
+      return;
     const int32_t at = atomicAdd(&s.count, 1);
     if (at >= Shared::LIST) return;
     s.place()[at] = place(z, col);
@@ -312,12 +315,17 @@ struct Team {
         const uint64_t at = place(z, col);
         return at >= lo && at <= hi;
       };
+      uint64_t least = ~0ull, most = 0;
       row.each([&](float z, int32_t col) INLINE {
         if (!member(z, col) || !amount(z, col)) return;
-        const unsigned long long at = place(z, col);
-        atomicMin(reinterpret_cast<unsigned long long*>(&s.lo), at);
-        atomicMax(reinterpret_cast<unsigned long long*>(&s.hi), at);
+        const uint64_t at = place(z, col);
+        least = at < least ? at : least;
+        most = at > most ? at : most;
       });
+      if (least <= most) {
+        atomicMin(reinterpret_cast<unsigned long long*>(&s.lo), (unsigned long long)least);
+        atomicMax(reinterpret_cast<unsigned long long*>(&s.hi), (unsigned long long)most);
+      }
       sync();
       const uint64_t from = s.lo, range = s.hi - from;
       const int shift = range < Shared::BINS ? 0 : 64 - __builtin_ctz(Shared::BINS) - __clzll((long long)range);

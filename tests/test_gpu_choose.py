@@ -638,3 +638,82 @@ def test_timer_counts_the_calls():
     finally:
         G.gnn_timer_enable(False)
     assert launches == 2 and ms > 0
+
+
+def test_temperature_0_needs_no_random_numbers():
+    z, _ = _logits(50, 300, 6)
+    a = torch.full((50,), 7, dtype=torch.int32, device="cuda")
+    G.gnn_sample_actions(50, 300, _rows(z, 300, 0), 300, None, 0.0, 0, 1.0, 0.0, a, None, _ws(0))
+    assert np.array_equal(a.cpu().numpy(), z.argmax(1))
+
+
+def test_more_blocks_than_a_launch_has():
+    """2^29 and some rows of one column: 256 to a block, 2^21 blocks to a
+    launch."""
+    n = (1 << 29) + 300
+    Z = torch.zeros((n, 1), device="cuda")
+    Z[n - 1] = float("nan")
+    a = torch.full((n,), 7, dtype=torch.int32, device="cuda")
+    u = torch.zeros(n, device="cuda")
+    G.gnn_sample_actions(n, 1, Z, 1, u, 1.0, 0, 0.5, 0.0, a, None, _ws(0))
+    assert int((a[:-1] != 0).sum()) == 0 and int(a[-1]) == -1
+    q = u.fill_(3.0)
+    G.gnn_top_logits(n, 1, Z, 1, 1, 1.0, a, q, None, _ws(0))
+    assert int((a[:-1] != 0).sum()) == 0 and int(a[-1]) == -1
+    assert int((q[:-1] != 0).sum()) == 0 and float(q[-1]) == -np.inf
+    del q, u
+    a.zero_()
+    a[5] = -1
+    logq, dZ, out = torch.zeros((n, 1), device="cuda"), torch.ones((n, 1), device="cuda"), \
+        torch.ones(1, device="cuda")
+    Z[n - 1] = 2.0
+    G.gnn_distill_loss(n, 1, Z, 1, 1, a, logq, None, None, 1.0, out, None, dZ, 1,
+                       _ws(G.gnn_distill_workspace_bytes(n, 1, 1)))
+    assert int((dZ != 0).sum()) == 0 and float(out) == 0.0
+
+
+@pytest.mark.parametrize("n,C", [(80000, 30011), (40000, 60013)])
+def test_offsets_past_32_bits(n, C):
+    """2.4e9 logits: the last rows as in a call of their own."""
+    gen = torch.Generator("cuda").manual_seed(8)
+    Z = torch.randn((n, C), device="cuda", generator=gen)
+    u = torch.rand(n, device="cuda", generator=gen)
+    k, m = 5, 3
+    a, i = torch.empty(n, dtype=torch.int32, device="cuda"), \
+        torch.empty((n, k), dtype=torch.int32, device="cuda")
+    q, r, lp = torch.empty((n, k), device="cuda"), torch.empty(n, device="cuda"), \
+        torch.empty(n, device="cuda")
+    G.gnn_sample_actions(n, C, Z, C, u, 0.8, 100, 0.9, 0.0, a, lp,
+                         _ws(G.gnn_sample_workspace_bytes(n, C)))
+    G.gnn_top_logits(n, C, Z, C, k, 1.0, i, q, r, _ws(G.gnn_top_workspace_bytes(n, C, k)))
+    z = Z[-m:].cpu().numpy()
+    check_sample(z, u[-m:].cpu().numpy(), 0.8, 100, 0.9, 0.0, a[-m:].cpu().numpy(),
+                 lp[-m:].cpu().numpy())
+    check_top(z, k, 1.0, (i[-m:].cpu().numpy(), q[-m:].cpu().numpy(), r[-m:].cpu().numpy()))
+    i[:, 0] = (i[:, 0] + 1) % C  # something to learn
+    dZ, out, kl = torch.empty((n, C), device="cuda"), torch.empty(1, device="cuda"), \
+        torch.empty(n, device="cuda")
+    G.gnn_distill_loss(n, C, Z, C, k, i, q, r, None, 1.0, out, kl, dZ, C,
+                       _ws(G.gnn_distill_workspace_bytes(n, C, k)))
+    w = np.full(m, 1.0 / n)
+    got = dict(out=0.0, kl=kl[-m:].cpu().numpy(), dZ=dZ[-m:].cpu().numpy())
+    want = O.distill(z, i[-m:].cpu().numpy(), q[-m:].cpu().numpy(), r[-m:].cpu().numpy(), w, 1.0)
+    got["out"] = want["out"]
+    check_distill(got, z, i[-m:].cpu().numpy(), q[-m:].cpu().numpy(), r[-m:].cpu().numpy(),
+                  w.astype(np.float32), 1.0)
+
+
+@pytest.mark.parametrize("C", [200000, 1 << 20])
+def test_very_long_rows(C):
+    z, rng = _logits(3, C, 12, mask=0.1)
+    z[2] = np.round(z[2])  # many equal ones: a crowded bin
+    u = rng.random(3).astype(np.float32)
+    for T, top_k, top_p, min_p in ((1.0, 0, 0.9, 0.0), (0.7, 5000, 0.95, 0.001), (1.0, 0, 1.0, 0.01),
+                                   (1.0, 70000, 1.0, 0.0), (0.0, 0, 1.0, 0.0)):
+        a, lp = run_sample(z, u, T, top_k, top_p, min_p)
+        check_sample(z, u, T, top_k, top_p, min_p, a, lp)
+    check_top(z, 200, 1.0, run_top(z, 200, 1.0))
+    zero = np.zeros((2, C), np.float32)
+    a, _ = run_sample(zero, np.array([0.25, 0.75]), 1.0, 0, 0.5)
+    half = int(np.ceil(0.5 * C))
+    assert a.tolist() == [half // 4, 3 * half // 4]
