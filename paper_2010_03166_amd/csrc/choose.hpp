@@ -132,9 +132,10 @@ struct Weights {
   }
 };
 
-// One for each logit that is there.
+// One for each logit from some value on (-inf never is).
 struct Present {
-  __device__ __forceinline__ uint64_t operator()(float z, int32_t) const { return z > -INFINITY; }
+  float from;
+  __device__ __forceinline__ uint64_t operator()(float z, int32_t) const { return z >= from; }
 };
 
 // A row's largest logit, whether it is a finite number and none is a NaN; and of
@@ -189,14 +190,15 @@ __device__ __forceinline__ Border first_entries(const T& team, Row& row, const f
   Border b;
   int32_t bin;
   uint64_t base;
-  if (team.select(row, Present(), top, scale, k, &b, &bin, &base)) return b;
+  const Present counts = {low};
+  if (team.select(row, counts, top, scale, k, &b, &bin, &base)) return b;
   if constexpr (Row::CHUNKS > 0) {
     Reread<T::G, T::W> again;
     again.load(from, min(C, base_col + Row::MOST), team.t, base_col);
-    b = team.search(again, Present(), top, scale, bin, k, base);
+    b = team.search(again, counts, top, scale, bin, k, base);
     row.load(from, C, team.t, base_col);
   } else {
-    b = team.search(row, Present(), top, scale, bin, k, base);
+    b = team.search(row, counts, top, scale, bin, k, base);
   }
   return b;
 }
@@ -359,46 +361,28 @@ struct Launch {
   int32_t rows, threads;  // of a block
   int32_t lanes() const { return threads / rows; }
 };
-#define LAUNCH(G, W, ROW)                                                        \
-  Launch<Args>{Kernel::template of<G, W, ROW>(), threads_of<G, W>() / (G * W), \
-               threads_of<G, W>()}
 
-template <class Args, class Kernel, int G, int W, int V>
-Launch<Args> held() {
-  using Row = Held<G, W, V>;
-  return LAUNCH(G, W, Row);
-}
-
-template <class Args, class Kernel, int G>
-Launch<Args> few(int32_t v) {
-  return v == 3 ? held<Args, Kernel, G, 1, 3>() : held<Args, Kernel, G, 1, 4>();
-}
-
-// Rows of at most LONG_SAMPLE columns.  As many lanes as a row takes at three or
-// four chunks each, up to a wavefront's 64 of eight; `places` (the length of a
-// list that each lane compares its share of with all) asks for a lane to four.
+// Kernel::of<G, W, Row>() and Kernel::small<V>() (rows of up to Kernel::SMALL
+// columns, a lane each), for rows of at most LONG_SAMPLE columns.
 template <class Args, class Kernel>
-Launch<Args> choose(int32_t C, int32_t places = 0) {
-  const int32_t q = (int32_t)ceil_div(C, 4);
-  if (q == 1) return {Kernel::template small<1>(), 256, 256};
-  if (q == 2) return {Kernel::template small<2>(), 256, 256};
-  if (q <= 4) return {Kernel::template small<4>(), 256, 256};
-  if (q <= 6) return {Kernel::template small<6>(), 256, 256};
-  if (C <= Kernel::SMALL) return {Kernel::template small<8>(), 256, 256};
-  const int32_t lanes = std::max(q, places);
-  const auto three = [&](int32_t lanes) { return ceil_div(q, lanes) <= 3 ? 3 : 4; };
-  if (lanes <= 16) return few<Args, Kernel, 4>(three(4));
-  if (lanes <= 32) return few<Args, Kernel, 8>(three(8));
-  if (lanes <= 64) return few<Args, Kernel, 16>(three(16));
-  if (lanes <= 128) return few<Args, Kernel, 32>(three(32));
-  if (q <= 256) return few<Args, Kernel, 64>(three(64));
-  if (q <= 384) return held<Args, Kernel, 64, 1, 6>();
-  if (q <= 512) return held<Args, Kernel, 64, 1, 8>();
-  if (q <= 1024) return held<Args, Kernel, 64, 4, 4>();
-  if (q <= 2048) return held<Args, Kernel, 64, 4, 8>();
-  if (q <= 4096) return held<Args, Kernel, 64, 8, 8>();
-  if (q <= 6144) return held<Args, Kernel, 64, 16, 6>();
-  return held<Args, Kernel, 64, 16, 8>();
+struct Chosen {
+  template <int G, int W, int V>
+  Launch<Args> held() const {
+    return {Kernel::template of<G, W, Held<G, W, V>>(), threads_of<G, W>() / (G * W),
+            threads_of<G, W>()};
+  }
+};
+template <class Args, class Kernel>
+Launch<Args> choose(int32_t n, int32_t C, int32_t places = 0) {
+  const Shape s = shape_of(n, C, places, Kernel::SMALL, true);
+  if (s.G > 1) return of_shape(s, Chosen<Args, Kernel>());
+  switch (s.V) {
+    case 1: return {Kernel::template small<1>(), 256, 256};
+    case 2: return {Kernel::template small<2>(), 256, 256};
+    case 4: return {Kernel::template small<4>(), 256, 256};
+    case 6: return {Kernel::template small<6>(), 256, 256};
+  }
+  return {Kernel::template small<8>(), 256, 256};
 }
 
 template <class Args>

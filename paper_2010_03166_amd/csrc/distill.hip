@@ -268,9 +268,9 @@ __device__ __forceinline__ void stores_done(const T& team) {
 }
 
 template <int G, int W, class Row>
-__global__ __launch_bounds__(W > 1 ? 64 * W : 256) void distill_kernel(DistillArgs a) {
+__global__ __launch_bounds__((threads_of<G, W>())) void distill_kernel(DistillArgs a) {
   using T = Team<G, W, Exchange>;
-  constexpr int THREADS = W > 1 ? 64 * W : 256, R = THREADS / T::LANES;
+  constexpr int THREADS = threads_of<G, W>(), R = THREADS / T::LANES;
   __shared__ typename T::Shared s[R];
   __shared__ uint32_t s_bits[R][(Row::MOST + 31) / 32];
   __shared__ double s_loss[THREADS / 64];
@@ -387,35 +387,22 @@ struct Launch {
   void (*kernel)(DistillArgs);  // NULL: split rows
   int32_t rows, threads;
 };
-template <int G, int W, int V>
-Launch held() {
-  constexpr int THREADS = W > 1 ? 64 * W : 256;
-  return {distill_kernel<G, W, Held<G, W, V>>, THREADS / (G * W), THREADS};
-}
-template <int G>
-Launch few(int32_t v) {
-  return v == 3 ? held<G, 1, 3>() : held<G, 1, 4>();
-}
-// As many lanes as a row takes at three or four chunks each, and a quarter of
-// the list's places at least: a lane's places stay in registers.
-Launch choose(int32_t C, int32_t places) {
-  if (C < 4) return held<1, 1, 1>();
-  const int32_t q = (int32_t)ceil_div(C, 4), lanes = std::max(q, places);
-  const auto three = [&](int32_t lanes) { return (int32_t)ceil_div(q, lanes) <= 3 ? 3 : 4; };
-  if (lanes == 1) return held<1, 1, 1>();
-  if (lanes == 2) return held<1, 1, 2>();
-  if (lanes <= 4) return few<1>(three(1));
-  if (lanes <= 8) return few<2>(three(2));
-  if (lanes <= 16) return few<4>(three(4));
-  if (lanes <= 32) return few<8>(three(8));
-  if (lanes <= 64) return few<16>(three(16));
-  if (lanes <= 128) return few<32>(three(32));
-  if (q <= 256) return few<64>(three(64));
-  if (q <= 512) return held<64, 1, 8>();
-  if (q <= 1024) return held<64, 4, 4>();
-  if (q <= 2048) return held<64, 4, 8>();
-  if (q <= 4096) return held<64, 8, 8>();
-  return {nullptr, 1, 256};
+struct Chosen {
+  template <int G, int W, int V>
+  Launch held() const {
+    constexpr int THREADS = threads_of<G, W>();
+    return {distill_kernel<G, W, Held<G, W, V>>, THREADS / (G * W), THREADS};
+  }
+};
+Launch choose(int32_t n, int32_t C, int32_t places) {
+  if (C > 16384) return {nullptr, 1, 256};
+  const Shape s = shape_of(n, C, C < 4 ? 0 : places, 16, false);
+  if (s.G > 1) return of_shape(s, Chosen());
+  switch (s.V) {
+    case 1: return Chosen().held<1, 1, 1>();
+    case 2: return Chosen().held<1, 1, 2>();
+  }
+  return Chosen().held<1, 1, 4>();
 }
 
 // [losses | parts' sums]
@@ -423,7 +410,7 @@ struct Layout {
   size_t parts, total;
 };
 Layout layout_of(int32_t n, int32_t C, int32_t k) {
-  const Launch l = choose(C, k);
+  const Launch l = choose(n, C, k);
   Layout o;
   o.parts = round_up((size_t)ceil_div(n, l.rows) * sizeof(double), 256);
   o.total = o.parts + (l.kernel ? 0 : (size_t)n * ceil_div(C, SPLIT_COLS) * sizeof(Part));
@@ -464,7 +451,7 @@ gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, 
         if (ranges_overlap(outs[i], outb[i], outs[q], outb[q])) return GNN_ERR_ALIAS;
     }
   }
-  const Launch l = choose(C, k);
+  const Launch l = choose(n, C, k);
   DistillArgs a = {};
   a.n = n;
   a.C = C;

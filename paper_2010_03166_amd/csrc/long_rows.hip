@@ -237,7 +237,7 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
       if (!any) return;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const uint64_t amount = !in[j] ? 0 : WHICH == 0 ? z[j] > -INFINITY : weight(z[j], col + j);
+        const uint64_t amount = !in[j] ? 0 : WHICH == 0 ? z[j] >= look.from : weight(z[j], col + j);
         // (a count past the list's end need not be exact)
         if (!amount ||
             __hip_atomic_load(&to.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > LIST)
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
       team.sync();
       b = team.settle(P, base);
     } else if (WHICH == 0) {
-      b = team.search(row, Present(), x.top, look.scale, bin, P, base);
+      b = team.search(row, Present{look.from}, x.top, look.scale, bin, P, base);
     } else {
       b = team.search(row, weight, x.top, look.scale, bin, P, base);
     }

@@ -297,7 +297,7 @@ gnn_status gnn_sample_actions(int32_t n, int32_t C, const float* Z, int64_t ld_z
   if (C > LONG_SAMPLE) {
     e = sample_long(a, workspace, stream);
   } else {
-    const Launch<SampleArgs> l = choose<SampleArgs, SampleKernel>(C);
+    const Launch<SampleArgs> l = choose<SampleArgs, SampleKernel>(n, C);
     a.group = a.top_k ? group_of(l.lanes(), C, a.top_k) : 1;
     e = run(l, a, stream);
   }

@@ -11,6 +11,8 @@
 // holds the border are put in order.
 #pragma once
 
+#include <type_traits>
+
 #include "rows.hpp"
 
 // (a lambda; left to itself the compiler calls some, and a row goes to the stack)
@@ -442,6 +444,69 @@ struct Listed {
     for (int64_t k = t; k < count; k += G * W) f(logit_of(places[k]), (int32_t)(uint32_t)places[k]);
   }
 };
+
+// What holds a row of C columns: G lanes of a wavefront or W wavefronts, with V
+// chunks each, or one lane (G = 1) with a whole row of up to 32.
+struct Shape {
+  int32_t G, W, V;
+};
+// As few lanes as a row takes at four chunks each (eight from 64 lanes on: few
+// exchanges between lanes, few lanes past the row's end), more where the rows
+// are too few to give the chip's 1,024 vector units two wavefronts each: then a
+// row's latency counts.  `places`: entries that each lane compares its share of
+// with all the others (a quarter of them is what it gets at most).  `small`:
+// columns that a lane takes alone, of rows enough for a wavefront a unit.
+// `spread`: rows past 2,048 columns take more wavefronts too where there are few
+// (a draw gains what a loss, which has less to do and waits for all of them more
+// often, loses: 100 x 16,000 12.5 us in 512 threads, 18.2 in 1,024).
+inline Shape shape_of(int32_t n, int32_t C, int32_t places, int32_t small, bool spread) {
+  const int32_t q = (int32_t)ceil_div(C, 4);
+  if (q <= 2 || (C <= small && n >= 1 << 16)) return {1, 1, q <= 4 ? q == 3 ? 4 : q : q <= 6 ? 6 : 8};
+  if (!spread && q > 512) n = INT32_MAX;
+  if (q > 4096) return {64, 16, q <= 6144 ? 6 : 8};
+  if (q > 2048) return n < 256 ? Shape{64, 16, 4} : Shape{64, 8, 8};
+  if (q > 1024) return n < 256 ? Shape{64, 16, 2} : n < 512 ? Shape{64, 8, 4} : Shape{64, 4, 8};
+  if (q > 512) return n < 512 ? Shape{64, 8, 2} : Shape{64, 4, 4};
+  if (q > 256) return n < 1024 ? Shape{64, 4, 2} : Shape{64, 1, q <= 384 ? 6 : 8};
+  int32_t G = 4;
+  while (G < 64 && 4 * G < std::max(q, places)) G *= 2;
+  while (G < 64 && G < q && (int64_t)n * G < 64 * 2048) G *= 2;
+  return {G, 1, (int32_t)ceil_div(q, G)};
+}
+
+// f.held<G, W, V>() for a shape with G > 1.
+template <class F>
+auto of_shape(const Shape& s, F f) {
+  if (s.W == 16)
+    return s.V == 2   ? f.template held<64, 16, 2>()
+           : s.V == 4 ? f.template held<64, 16, 4>()
+           : s.V == 6 ? f.template held<64, 16, 6>()
+                      : f.template held<64, 16, 8>();
+  if (s.W == 8)
+    return s.V == 2   ? f.template held<64, 8, 2>()
+           : s.V == 4 ? f.template held<64, 8, 4>()
+                      : f.template held<64, 8, 8>();
+  if (s.W == 4)
+    return s.V == 2   ? f.template held<64, 4, 2>()
+           : s.V == 4 ? f.template held<64, 4, 4>()
+                      : f.template held<64, 4, 8>();
+  const auto few = [&](auto lanes) {
+    constexpr int G = decltype(lanes)::value;
+    return s.V == 1   ? f.template held<G, 1, 1>()
+           : s.V == 2 ? f.template held<G, 1, 2>()
+           : s.V == 3 ? f.template held<G, 1, 3>()
+                      : f.template held<G, 1, 4>();
+  };
+  switch (s.G) {
+    case 4: return few(std::integral_constant<int, 4>());
+    case 8: return few(std::integral_constant<int, 8>());
+    case 16: return few(std::integral_constant<int, 16>());
+    case 32: return few(std::integral_constant<int, 32>());
+  }
+  return s.V == 6   ? f.template held<64, 1, 6>()
+         : s.V == 8 ? f.template held<64, 1, 8>()
+                    : few(std::integral_constant<int, 64>());
+}
 
 template <int G, int W>
 constexpr int threads_of() {

@@ -154,7 +154,7 @@ gnn_status gnn_top_logits(int32_t n, int32_t C, const float* Z, int64_t ld_z, in
   if (C > LONG_TOP) {
     e = top_long(a, workspace, stream);
   } else {
-    const Launch<TopArgs> l = choose<TopArgs, TopKernel>(C, k);
+    const Launch<TopArgs> l = choose<TopArgs, TopKernel>(n, C, k);
     a.group = group_of(l.lanes(), C, k);
     e = run(l, a, stream);
   }
