@@ -1,10 +1,16 @@
-// Drawing actions from and finding the top logits of rows past 32,768
-// and 16,384 columns: parts of 4,096, a block each, and what is one of a row joined from
-// them by every block alike or by a launch of a block a row.  A draw reads its
-// row once for its range, twice for each border that is asked for, once for the
-// kept sums and a part of it for the action, out of the caches for the few rows
-// that are so long; top logits read it once, and the first k of each part go on.
-// Sums over parts are of whole numbers, or in a fixed order.
+// Drawing actions from rows past 32,768 columns and finding the top logits of
+// rows past 16,384: parts of 4,096 columns, a block each, and what is one of a
+// row joined from them by every block alike or by a launch of a block a row.  A
+// draw reads its row once for its range, twice for each border that is asked
+// for (bins, then the border's bin and the weights before it) and a part of it
+// for the action; the few rows that are so long come out of the caches.  Top
+// logits read it once, and the first k of each part go on.  Sums over parts are
+// of whole numbers, or in a fixed order.
+//
+// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 85 us
+// in ten launches of 4 to 16 us, without a border 24 to 28 us in three; 1 x
+// 131,071 14 us without, 47 with top-p (one block a row 56 and 179).  500 x
+// 65,536 without a border 75 us, 64 x 131,071's first 256 37.
 #include "choose.hpp"
 
 namespace gnnprop {
@@ -573,8 +579,8 @@ hipError_t top_long(TopArgs a, void* workspace, hipStream_t stream) {
                                              round_up((size_t)blocks * sizeof(TopPart), 256));
   a.group = group_of(THREADS, a.C, a.k);
   launch(top_part_kernel, a, blocks, stream);
-  // (640 candidates a row, 2,000 rows: 19 us by 256 threads, 68 by 1,024; 8,192
-  // candidates, 64 rows: 30 and 15)
+  // (2,000 rows of 640 candidates: 18 us by 256 threads, 68 by 1,024; 64 x 131,071
+  // with its 8,192 candidates a row 56 us by 256 threads, both launches, 41 by 1,024)
   if ((int64_t)a.per_row * a.k <= 2048) launch(top_join_kernel<4>, a, a.n, stream);
   else launch(top_join_kernel<16>, a, a.n, stream, 1024);
   return hipGetLastError();

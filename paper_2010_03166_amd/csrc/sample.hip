@@ -1,5 +1,18 @@
 // Actions drawn from rows of logits (temperature, top-k, top-p, min-p) by given
 // random numbers.
+//
+// A row is read once into the registers of its team (shape_of() in team.hpp), and
+// every pass goes over them: its range, the border of the first top_k, weights
+// into bins and top_p's border, the kept sum with the draw.  Formed once and
+// kept, the weights took 64 registers beside a row's 32 and spilled (16,384 x
+// 2,048 with top-p 303 us); formed again they cost 16 instructions each.
+//
+// Bound by instructions where the rows are many: 16,384 x 2,048 with top-p takes
+// 101 us, 3,170 vector instructions a wavefront of 2,048 entries, and the vector
+// units issue in nine of ten cycles (the bytes take 27 us); without a border 48.
+// 50,001 x 121 with top-k, top-p, min-p 39 us (the bytes 5): LDS where the first
+// 20 are compared.  Where they are few, by one row's latency beside the launch:
+// 8,000 x 41 6.9 us, 1 x 2,048 7.2.
 #include "choose.hpp"
 
 using namespace gnnprop;
@@ -211,9 +224,10 @@ __global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>())) voi
   sample_row<T, Row>(a, team, (int32_t)i, s_table);
 }
 
-// Rows of up to 32 columns: a lane has one to itself, and what comes before an
-// entry is told by comparing it with every other one (no bins, nothing but the
-// exponentials' table in LDS).
+// Rows of up to 24 columns, 65,536 of them or more: a lane has one to itself, and
+// what comes before an entry is told by comparing it with every other one (no
+// bins, nothing but the exponentials' table in LDS).  200,000 x 7 with top-p 21
+// us by teams, 8 so; 200,000 x 16 40 and 20; 200,000 x 32 34 and 51.
 template <int V>
 __global__ __launch_bounds__(256) void sample_small_kernel(SampleArgs a) {
   constexpr int N = 4 * V;
@@ -309,7 +323,6 @@ __global__ __launch_bounds__(256) void sample_small_kernel(SampleArgs a) {
 }
 
 struct SampleKernel {
-  // (200,000 x 32, T = 1 without and with top-p 0.9: a lane a row 24 and 51 us)
   static constexpr int SMALL = 24;
   template <int G, int W, class Row>
   static constexpr auto of() { return sample_kernel<G, W, Row>; }

@@ -8,7 +8,10 @@
 //   sum before it < P <= sum with it.
 // It is found without sorting the row: amounts are added up in bins of the
 // logits' distance from the largest, and only the entries of the bin that
-// holds the border are put in order.
+// holds the border are put in order.  Bins are so many that a few entries lie in
+// one where logits are spread; where they are not (equal logits, logits at the
+// type's lowest value beside others) the bin's entries are searched from memory:
+// 16,384 x 2,048 equal logits with top-p 312 us instead of 101.
 #pragma once
 
 #include <type_traits>
