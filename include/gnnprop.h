@@ -436,10 +436,10 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
 
 /* Acting, and teaching one network by another.  Rows of logits Z (n x C,
  * stride ld_z) as above; the order of a row's entries is: larger logits first,
- * equal ones (0 and -0 are) by their columns.  Logits of -inf are not there.  A
- * row whose largest logit is not a finite number, or with a NaN among them, is
- * left out.  1 <= C <= 2^24; temperatures T are 0 or 1e-6 to 1e6 (else
- * GNN_ERR_SHAPE).
+ * equal ones (0 and -0 are) by their columns.  Logits of -inf are not there.
+ * The first two calls leave out a row whose largest logit is not a finite
+ * number, and one with a NaN.  1 <= C <= 2^24; temperatures T are 0 (the first
+ * call) or 1e-6 to 1e6 (else GNN_ERR_SHAPE).
  *
  * gnn_sample_actions: each row draws an action by its random number u.  With
  *   e_j = exp((Z[i, j] - top) / T),  top the row's largest logit,
@@ -459,7 +459,8 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  * last number below 1).  action: n int32, -1 for rows left out.  logp (n
  * floats, may be NULL): the actions' log-probabilities under Z itself (T = 1,
  * nothing cut off), as gnn_action_logp gives them, 0 for rows left out: the
- * old_logp of gnn_policy_loss.  Workspace: gnn_sample_workspace_bytes.
+ * old_logp of gnn_policy_loss.  Workspace: gnn_sample_workspace_bytes (0 up to
+ * 32,768 columns, some 50 KB a row beyond).
  *
  * gnn_top_logits: the first k entries of each row's order (1 <= k <=
  * GNN_TOP_MOST), with T > 0:
@@ -482,11 +483,11 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  * 0, whose list has no index in range, or nothing but q of 0, or whose logits
  * are all -inf: of the first kind the logits may hold anything.  A row of
  * weight 0 adds nothing and has a gradient of 0.  weight: n floats (NULL: 1/n).
- * A q above 0 where the student has p = 0 makes kl infinite.  Columns of dZ's
- * rows past C are not written; kl (n floats) and dZ (stride ld_dz) may be NULL.
- * n = 0 gives out = 0.  Exponentials of the row are fp32's, everything of the
- * list is in double, and so are all sums.  Workspace:
- * gnn_distill_workspace_bytes.
+ * A q above 0 where the student has p = 0 makes kl infinite, a NaN or +inf among
+ * a row's logits shows in its kl and gradient.  Columns of dZ's rows past C are
+ * not written; kl (n floats) and dZ (stride ld_dz) may be NULL.  n = 0 gives
+ * out = 0.  Exponentials of the row are fp32's, everything of the list is in
+ * double, and so are all sums.  Workspace: gnn_distill_workspace_bytes.
  *
  * For all three: results are bit-reproducible, and no output may overlap an
  * input, another output or the workspace. */

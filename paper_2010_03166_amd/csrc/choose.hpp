@@ -278,13 +278,13 @@ struct TopArgs {
   int32_t per_row;
 };
 
-// The entries up to a border into the list (`count` of them, put to 0 before),
-// and the sums of exp((z - top) / T) over them and over the others (the lane's
-// shares).
+// The entries up to a border into the list (`count` of them, put to 0 before; at
+// most `most` are written), and the sums of exp((z - top) / T) over them and over
+// the others (the lane's shares).
 template <class T, class Row>
 __device__ __forceinline__ void collect(const T& team, const Row& row, const Border& b, float top,
-                                        double inv_t, uint64_t* list, double* in_sum,
-                                        double* out_sum) {
+                                        double inv_t, uint64_t* list, int32_t most,
+                                        double* in_sum, double* out_sum) {
   const float octaves = (float)(inv_t * 1.4426950408889634);
   double in = 0.0, out = 0.0;
   row.each4([&](int32_t col, f4 z) INLINE {
@@ -306,7 +306,8 @@ __device__ __forceinline__ void collect(const T& team, const Row& row, const Bor
     for (int j = 0; j < 4; ++j) {
       if (!kept[j]) continue;
       more += e[j];
-      list[atomicAdd(&team.s.count, 1)] = place(z[j], col + j);
+      const int32_t at = atomicAdd(&team.s.count, 1);
+      if (at < most) list[at] = place(z[j], col + j);
     }
     in += more;
   });
@@ -321,7 +322,7 @@ __device__ __forceinline__ void write_top(const TopArgs& a, const T& team, uint6
                                           int32_t i, float top, double in, double out) {
   int32_t* index = a.index + (int64_t)i * a.k;
   float* logq = a.logq + (int64_t)i * a.k;
-  const int32_t m = team.s.count;
+  const int32_t m = min(team.s.count, a.k);
   const double lse = log_quick((float)(in + out));
   // each in its place: those before it are counted, eight at a time
   for (int32_t j = m + team.t; j < (m + 7) / 8 * 8; j += T::LANES) list[j] = ~0ull;
@@ -363,9 +364,11 @@ struct Launch {
 };
 
 // Kernel::of<G, W, Row>() and Kernel::small<V>() (rows of up to Kernel::SMALL
-// columns, a lane each), for rows of at most LONG_SAMPLE columns.
+// columns, a lane each), for rows of at most Kernel::MOST columns.
 template <class Args, class Kernel>
 struct Chosen {
+  static constexpr bool SPREAD = true;
+  static constexpr int32_t MOST = Kernel::MOST;
   template <int G, int W, int V>
   Launch<Args> held() const {
     return {Kernel::template of<G, W, Held<G, W, V>>(), threads_of<G, W>() / (G * W),
@@ -374,7 +377,7 @@ struct Chosen {
 };
 template <class Args, class Kernel>
 Launch<Args> choose(int32_t n, int32_t C, int32_t places = 0) {
-  const Shape s = shape_of(n, C, places, Kernel::SMALL, true);
+  const Shape s = shape_of(n, C, places, Kernel::SMALL, Chosen<Args, Kernel>::SPREAD);
   if (s.G > 1) return of_shape(s, Chosen<Args, Kernel>());
   switch (s.V) {
     case 1: return {Kernel::template small<1>(), 256, 256};
@@ -392,7 +395,6 @@ hipError_t run(const Launch<Args>& l, Args a, hipStream_t stream) {
     l.kernel<<<(unsigned)std::min(blocks - a.block0, LAUNCH_BLOCKS), l.threads, 0, stream>>>(a);
   return hipGetLastError();
 }
-
 
 // Rows past LONG_SAMPLE and LONG_TOP columns (long_rows.hip).
 size_t sample_long_bytes(int32_t n, int32_t C);

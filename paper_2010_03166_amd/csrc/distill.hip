@@ -396,6 +396,8 @@ struct Launch {
   int32_t rows, threads;
 };
 struct Chosen {
+  static constexpr bool SPREAD = false;
+  static constexpr int32_t MOST = 16384;
   template <int G, int W, int V>
   Launch held() const {
     constexpr int THREADS = threads_of<G, W>();
@@ -403,8 +405,8 @@ struct Chosen {
   }
 };
 Launch choose(int32_t n, int32_t C, int32_t places) {
-  if (C > 16384) return {nullptr, 1, 256};
-  const Shape s = shape_of(n, C, C < 4 ? 0 : places, 16, false);
+  if (C > Chosen::MOST) return {nullptr, 1, 256};
+  const Shape s = shape_of(n, C, C < 4 ? 0 : places, 16, Chosen::SPREAD);
   if (s.G > 1) return of_shape(s, Chosen());
   switch (s.V) {
     case 1: return Chosen().held<1, 1, 1>();

@@ -418,6 +418,10 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
   for (int32_t k = p0; k < p1; ++k) own += parts[k].kept;
   const uint64_t wave = lanes_sum<64>(own);
   if (team.lane == 0) s.sums[team.wave] = wave;
+  if (team.t == 0) {
+    s_part = 0;
+    s_target = 0;
+  }
   team.sync();
   uint64_t ahead = team.before(own), all = 0;
   for (int k = 0; k < 4; ++k) {
@@ -467,10 +471,10 @@ __global__ __launch_bounds__(THREADS) void top_part_kernel(TopArgs a) {
     if (team.t == 0) s.count = 0;
     team.sync();
     double in, out;
-    collect(team, row, b, p.top, a.inv_t, s_list, &in, &out);
+    collect(team, row, b, p.top, a.inv_t, s_list, a.k, &in, &out);
     p.others = team.sum(out);
     team.sync();
-    m = s.count;
+    m = min(s.count, a.k);
   } else if (p.top == INFINITY) {
     p.lanes |= BAD_LANES;
   }
@@ -507,7 +511,8 @@ __global__ __launch_bounds__(64 * W) void top_join_kernel(TopArgs a) {
     const float e = __builtin_amdgcn_exp2f((z - top) * octaves);
     if (within(b, z, col) & (z > -INFINITY)) {
       in += e;
-      s_list[atomicAdd(&s.count, 1)] = place(z, col);
+      const int32_t at = atomicAdd(&s.count, 1);
+      if (at < a.k) s_list[at] = place(z, col);
     } else {
       out += e;
     }

@@ -46,11 +46,13 @@ __device__ __forceinline__ void sample_few(const SampleArgs& a, const T& team, c
     for (int j = 0; j < 4; ++j) any |= in[j] = within(weight.kept, z[j], col + j) && z[j] > -INFINITY;
     if (!any) return;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (in[j]) list[atomicAdd(&team.s.count, 1)] = place(z[j], col + j);
+    for (int j = 0; j < 4; ++j) {
+      const int32_t at = in[j] ? atomicAdd(&team.s.count, 1) : a.top_k;
+      if (at < a.top_k) list[at] = place(z[j], col + j);
+    }
   });
   team.sync();
-  const int32_t m = team.s.count;
+  const int32_t m = min(team.s.count, a.top_k);
   uint64_t sum = 0;
   for (int32_t e = team.t; e < m; e += T::LANES) sum += w[e] = weight.all(logit_of(list[e]));
   if (a.top_p < 1.0) {
@@ -323,7 +325,7 @@ __global__ __launch_bounds__(256) void sample_small_kernel(SampleArgs a) {
 }
 
 struct SampleKernel {
-  static constexpr int SMALL = 24;
+  static constexpr int32_t SMALL = 24, MOST = LONG_SAMPLE;
   template <int G, int W, class Row>
   static constexpr auto of() { return sample_kernel<G, W, Row>; }
   template <int V>

@@ -308,12 +308,15 @@ struct Team {
 
   // The border in a bin of many entries: by bins of their places, whose range
   // shrinks BINS times in each turn, at last to one entry.  (The row is one that
-  // is read again, so that a row in registers need not be kept for it.)
+  // is read again, so that a row in registers need not be kept for it.  Were it
+  // written to meanwhile, the amounts might not reach P any more: that ends the
+  // search too.)
   template <typename Row, typename Amount>
   __device__ __forceinline__ Border search(const Row& row, Amount amount, float top, float scale, int32_t bin,
                            uint64_t P, uint64_t base) const {
     uint64_t lo = 0, hi = ~0ull;
-    for (bool first = true;; first = false) {
+    for (int turn = 0; turn < 64; ++turn) {
+      const bool first = turn == 0;
       clear();
       const auto member = [&](float z, int32_t col) INLINE {
         if (first) return bin_of(z, top, scale) == bin;
@@ -342,7 +345,7 @@ struct Team {
       sync();
       int32_t b;
       uint64_t more = 0;
-      find(P - base, &b, &more);
+      if (!find(P - base, &b, &more)) break;
       base += more;
       lo = from + ((uint64_t)b << shift);
       hi = lo + ((1ull << shift) - 1);
@@ -356,6 +359,8 @@ struct Team {
       if (s.count <= Shared::LIST) return settle(P, base);
       sync();
     }
+    sync();
+    return NO_BORDER;
   }
 };
 
@@ -477,18 +482,21 @@ inline Shape shape_of(int32_t n, int32_t C, int32_t places, int32_t small, bool 
   return {G, 1, (int32_t)ceil_div(q, G)};
 }
 
-// f.held<G, W, V>() for a shape with G > 1.
+// f.held<G, W, V>() for a shape with G > 1, of rows of at most F::MOST columns,
+// spread as F::SPREAD says (no other shapes are built).
 template <class F>
 auto of_shape(const Shape& s, F f) {
-  if (s.W == 16)
-    return s.V == 2   ? f.template held<64, 16, 2>()
-           : s.V == 4 ? f.template held<64, 16, 4>()
-           : s.V == 6 ? f.template held<64, 16, 6>()
-                      : f.template held<64, 16, 8>();
-  if (s.W == 8)
-    return s.V == 2   ? f.template held<64, 8, 2>()
-           : s.V == 4 ? f.template held<64, 8, 4>()
-                      : f.template held<64, 8, 8>();
+  if constexpr (F::MOST > 16384) {
+    static_assert(F::SPREAD, "rows past 16,384 columns take 1,024 threads");
+    if (s.W == 16 && s.V == 6) return f.template held<64, 16, 6>();
+    if (s.W == 16 && s.V == 8) return f.template held<64, 16, 8>();
+  }
+  if constexpr (F::SPREAD) {
+    if (s.W == 16) return s.V == 2 ? f.template held<64, 16, 2>() : f.template held<64, 16, 4>();
+    if (s.W == 8 && s.V == 2) return f.template held<64, 8, 2>();
+    if (s.W == 8 && s.V == 4) return f.template held<64, 8, 4>();
+  }
+  if (s.W == 8) return f.template held<64, 8, 8>();
   if (s.W == 4)
     return s.V == 2   ? f.template held<64, 4, 2>()
            : s.V == 4 ? f.template held<64, 4, 4>()

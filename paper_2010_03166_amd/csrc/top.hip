@@ -40,7 +40,7 @@ __global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
   if (team.t == 0) team.s.count = 0;
   team.sync();
   double in, out;
-  collect(team, row, b, top, a.inv_t, list, &in, &out);
+  collect(team, row, b, top, a.inv_t, list, a.k, &in, &out);
   in = team.sum(in);
   out = team.sum(out);
   team.sync();
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void top_small_kernel(TopArgs a) {
 }
 
 struct TopKernel {
-  static constexpr int SMALL = 32;
+  static constexpr int32_t SMALL = 32, MOST = LONG_TOP;
   template <int G, int W, class Row>
   static constexpr auto of() { return top_kernel<G, W, Row>; }
   template <int V>

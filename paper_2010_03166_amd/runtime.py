@@ -604,8 +604,9 @@ class Trainer:
         is done."""
         n, C, f = self.n, self.C, self.f_top
         need = max(G.gnn_policy_workspace_bytes(n, C), G.gnn_sample_workspace_bytes(n, C),
-                   G.gnn_distill_workspace_bytes(n, C, G.GNN_TOP_MOST), G.gnn_gemm_workspace_bytes(n, C, f),
-                   G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C), 256)
+                   G.gnn_distill_workspace_bytes(n, C, G.GNN_TOP_MOST),
+                   G.gnn_gemm_workspace_bytes(n, C, f), G.gnn_gemm_workspace_bytes(f, C, n),
+                   G.gnn_gemm_workspace_bytes(n, f, C), 256)
         if self.policy_ws is None or self.policy_ws.numel() < need or self._Z.buf.shape[0] < n:
             with torch.cuda.stream(_stream_object(stream)):
                 self._Z = _Rows(C, self._Z.ld, self.device)

@@ -442,8 +442,8 @@ def test_no_rows():
 
 
 def test_many_blocks():
-    """More rows than one launch's blocks take at the narrowest width, and the
-    same results in every call."""
+    """Many rows of a lane each against torch's own sums, and the same results in
+    every call."""
     n, C = 300001, 3
     gen = torch.Generator(device="cuda").manual_seed(1)
     Z = torch.randn((n, C), device="cuda", generator=gen)
