@@ -415,15 +415,17 @@ Launch choose(int32_t n, int32_t C, int32_t places) {
   return Chosen().held<1, 1, 4>();
 }
 
-// [losses | parts' sums]
+// [losses | parts' sums]; a loss a row, though most blocks have several rows: fewer
+// rows are shared out over more blocks, and what is enough for the most rows has to
+// be for fewer.
 struct Layout {
   size_t parts, total;
 };
-Layout layout_of(int32_t n, int32_t C, int32_t k) {
-  const Launch l = choose(n, C, k);
+Layout layout_of(int32_t n, int32_t C) {
   Layout o;
-  o.parts = round_up((size_t)ceil_div(n, l.rows) * sizeof(double), 256);
-  o.total = o.parts + (l.kernel ? 0 : (size_t)n * ceil_div(C, SPLIT_COLS) * sizeof(Part));
+  o.parts = round_up((size_t)n * sizeof(double), 256);
+  o.total = o.parts +
+            (C > Chosen::MOST ? (size_t)n * ceil_div(C, SPLIT_COLS) * sizeof(Part) : 0);
   return o;
 }
 
@@ -433,7 +435,7 @@ extern "C" {
 
 size_t gnn_distill_workspace_bytes(int32_t n, int32_t C, int32_t k) {
   if (n < 0 || C <= 0 || C > MOST_COLS || k <= 0 || k > GNN_TOP_MOST) return 0;
-  return layout_of(n, C, k).total;
+  return layout_of(n, C).total;
 }
 
 gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, int32_t k,
@@ -446,7 +448,7 @@ gnn_status gnn_distill_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z, 
     return GNN_ERR_SHAPE;
   if (!out || (n > 0 && (!Z || !index || !logq))) return GNN_ERR_NULL;
   if (!buf16(workspace)) return GNN_ERR_UNSUPPORTED;
-  const Layout o = layout_of(n, C, k);
+  const Layout o = layout_of(n, C);
   if (workspace_bytes < o.total || (o.total > 0 && !workspace)) return GNN_ERR_WORKSPACE;
   {
     const size_t rows = (size_t)n * 4, list = rows * k;

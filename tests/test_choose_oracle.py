@@ -176,3 +176,16 @@ def test_distill_refusals():
     assert G.gnn_distill_workspace_bytes(-1, 3, 2) == 0 == G.gnn_distill_workspace_bytes(3, 3, 0)
     assert G.gnn_distill_workspace_bytes(3, 2 ** 24 + 1, 2) == 0
     assert G.gnn_distill_workspace_bytes(2 ** 31 - 1, 2 ** 24, 8) > 2 ** 31 * 4096
+
+
+def test_workspace_of_the_most_rows_serves_fewer():
+    rows = [0, 1, 2, 63, 64, 255, 256, 511, 512, 1023, 1024, 2047, 2049, 8191, 8193, 16385, 32769,
+            65535, 65536, 200000]
+    for C in (1, 3, 7, 16, 17, 121, 500, 1025, 2049, 5000, 16384, 16385, 32769):
+        for k in (1, 5, 64, 256):
+            for f in (lambda n: G.gnn_sample_workspace_bytes(n, C),
+                      lambda n: G.gnn_top_workspace_bytes(n, C, k),
+                      lambda n: G.gnn_distill_workspace_bytes(n, C, k)):
+                need = [f(n) for n in rows]
+                assert need == sorted(need), (C, k)
+            assert need == [G.gnn_distill_workspace_bytes(n, C, 256) for n in rows], (C, k)
