@@ -278,9 +278,9 @@ struct TopArgs {
   int32_t per_row;
 };
 
-// The entries up to a border into the list (`count` of them, put to 0 before; at
-// most `most` are written), and the sums of exp((z - top) / T) over them and over
-// the others (the lane's shares).
+// The entries up to a border into the list (of `most` places; `count` of them, put
+// to 0 before), and the sums of exp((z - top) / T) over them and over the others
+// (the lane's shares).
 template <class T, class Row>
 __device__ __forceinline__ void collect(const T& team, const Row& row, const Border& b, float top,
                                         double inv_t, uint64_t* list, int32_t most,
@@ -306,8 +306,7 @@ __device__ __forceinline__ void collect(const T& team, const Row& row, const Bor
     for (int j = 0; j < 4; ++j) {
       if (!kept[j]) continue;
       more += e[j];
-      const int32_t at = atomicAdd(&team.s.count, 1);
-      if (at < most) list[at] = place(z[j], col + j);
+      list[min(atomicAdd(&team.s.count, 1), most - 1)] = place(z[j], col + j);
     }
     in += more;
   });

@@ -216,8 +216,8 @@ struct Others {
   bool repeats;
 
   // bits: one for each column that the team holds.
-  __device__ __forceinline__ void load(const DistillArgs& a, const T& team, const float* from, int32_t col0,
-                       const int32_t* index, uint32_t* bits) {
+  __device__ __forceinline__ void load(const DistillArgs& a, const T& team, const float* from,
+                                       int32_t col0, const int32_t* index, uint32_t* bits) {
     row.load(from, a.C, team.t, col0);
     for (int32_t k = team.t; k < (Row::MOST + 31) / 32; k += T::LANES) bits[k] = 0;
     team.sync();

@@ -126,7 +126,9 @@ __global__ __launch_bounds__(THREADS) void long_range_kernel(SampleArgs a) {
   row_range(team, row, a.group, &p.top, &p.low, &p.lanes);
   p.least = INFINITY;
   if (a.top_k) {
-    row.each([&](float z, int32_t) INLINE { p.least = fminf(p.least, z > -INFINITY ? z : INFINITY); });
+    row.each([&](float z, int32_t) INLINE {
+      p.least = fminf(p.least, z > -INFINITY ? z : INFINITY);
+    });
     p.least = -team.max(-p.least);
   }
   if (a.logp) {

@@ -43,7 +43,8 @@ __device__ __forceinline__ void sample_few(const SampleArgs& a, const T& team, c
   row.each4([&](int32_t col, f4 z) INLINE {
     bool in[4], any = false;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) any |= in[j] = within(weight.kept, z[j], col + j) && z[j] > -INFINITY;
+    for (int j = 0; j < 4; ++j)
+      any |= in[j] = within(weight.kept, z[j], col + j) && z[j] > -INFINITY;
     if (!any) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -212,7 +213,8 @@ constexpr int blocks_of() {
 }
 
 template <int G, int W, class Row>
-__global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>())) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>()))
+void sample_kernel(SampleArgs a) {
   using T = Team<G, W>;
   constexpr int R = threads_of<G, W>() / T::LANES;
   __shared__ typename T::Shared s[R];

@@ -267,8 +267,9 @@ struct Team {
   // the amounts do not reach P.  False where a bin holds more entries than are
   // put in order at once: *bin and *base are for search() then.
   template <typename Row, typename Amount>
-  __device__ __forceinline__ bool select(const Row& row, Amount amount, float top, float scale, uint64_t P,
-                         Border* border, int32_t* bin, uint64_t* base) const {
+  __device__ __forceinline__ bool select(const Row& row, Amount amount, float top, float scale,
+                                         uint64_t P, Border* border, int32_t* bin,
+                                         uint64_t* base) const {
     if (!find(P, bin, base)) {
       *border = NO_BORDER;
       sync();
@@ -312,8 +313,8 @@ struct Team {
   // written to meanwhile, the amounts might not reach P any more: that ends the
   // search too.)
   template <typename Row, typename Amount>
-  __device__ __forceinline__ Border search(const Row& row, Amount amount, float top, float scale, int32_t bin,
-                           uint64_t P, uint64_t base) const {
+  __device__ __forceinline__ Border search(const Row& row, Amount amount, float top, float scale,
+                                           int32_t bin, uint64_t P, uint64_t base) const {
     uint64_t lo = 0, hi = ~0ull;
     for (int turn = 0; turn < 64; ++turn) {
       const bool first = turn == 0;
@@ -336,7 +337,8 @@ struct Team {
       }
       sync();
       const uint64_t from = s.lo, range = s.hi - from;
-      const int shift = range < Shared::BINS ? 0 : 64 - __builtin_ctz(Shared::BINS) - __clzll((long long)range);
+      const int shift = range < Shared::BINS
+                            ? 0 : 64 - __builtin_ctz(Shared::BINS) - __clzll((long long)range);
       row.each([&](float z, int32_t col) INLINE {
         if (!member(z, col)) return;
         const uint64_t x = amount(z, col);
@@ -426,7 +428,8 @@ struct Reread {
   template <class F>
   __device__ __forceinline__ void each4(F f) const {
 #pragma unroll 1
-    for (int k = 0; k < part; ++k) f(column(k), cut_cols(load_cols(row, column(k), C), column(k), C));
+    for (int k = 0; k < part; ++k)
+      f(column(k), cut_cols(load_cols(row, column(k), C), column(k), C));
   }
   template <class F>
   __device__ __forceinline__ void each(F f) const {
@@ -469,7 +472,8 @@ struct Shape {
 // often, loses: 100 x 16,000 12.5 us in 512 threads, 18.2 in 1,024).
 inline Shape shape_of(int32_t n, int32_t C, int32_t places, int32_t small, bool spread) {
   const int32_t q = (int32_t)ceil_div(C, 4);
-  if (q <= 2 || (C <= small && n >= 1 << 16)) return {1, 1, q <= 4 ? q == 3 ? 4 : q : q <= 6 ? 6 : 8};
+  if (q <= 2 || (C <= small && n >= 1 << 16))
+    return {1, 1, q <= 2 ? q : q <= 4 ? 4 : q <= 6 ? 6 : 8};
   if (!spread && q > 512) n = INT32_MAX;
   if (q > 4096) return {64, 16, q <= 6144 ? 6 : 8};
   if (q > 2048) return n < 256 ? Shape{64, 16, 4} : Shape{64, 8, 8};
