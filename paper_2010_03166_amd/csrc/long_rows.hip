@@ -2,15 +2,17 @@
 // rows past 16,384: parts of 4,096 columns, a block each, and what is one of a
 // row joined from them by every block alike or by a launch of a block a row.  A
 // draw reads its row once for its range, twice for each border that is asked
-// for (bins, then the border's bin and the weights before it) and a part of it
-// for the action; the few rows that are so long come out of the caches.  Top
-// logits read it once, and the first k of each part go on.  Sums over parts are
-// of whole numbers, or in a fixed order.
+// for (bins, then the border's bin and the weights before it; where the first
+// entries are few they are listed, and nothing after them reads the row) and a
+// part of it for the action; the few rows that are so long come out of the
+// caches.  Top logits read it once, and the first k of each part go on.  Sums
+// over parts are of whole numbers, or in a fixed order.
 //
-// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 85 us
-// in ten launches of 4 to 16 us, without a border 24 to 28 us in three; 1 x
-// 131,071 14 us without, 47 with top-p (one block a row 56 and 179).  500 x
-// 65,536 without a border 75 us, 64 x 131,071's first 256 37.
+// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 57 us
+// in five launches of 4 to 19 us (88 with the first 1,025, in ten), without a
+// border 24 to 28 us in three; 1 x 131,071 14 us without, 47 with top-p (one block
+// a row 56 and 179), 34 with top-k and top-p.  500 x 65,536 without a border 75 us,
+// 64 x 131,071's first 256 37.
 #include "choose.hpp"
 
 namespace gnnprop {
@@ -41,7 +43,7 @@ constexpr int32_t BAD_LANES = 1 << 16;  // (row_range's mark, in a part's count 
 // entries of the border's bin.
 struct Search {
   uint64_t bins[BINS];
-  uint64_t place[LIST], amount[LIST];
+  uint64_t entries[2 * LIST];  // places
   uint64_t wanted, base;  // the amount looked for, and what lies in bins before
   int32_t bin;            // the border's (-1: all are kept)
   int32_t count;          // entries in it
@@ -219,11 +221,33 @@ __global__ __launch_bounds__(THREADS) void long_find_kernel(SampleArgs a) {
   mine.bin = bin;
 }
 
+// A part's entries on their way to the row's list: one addition to its count for
+// all of them (one for each made a call some 45 ns longer).
+template <int MOST>
+struct PartList {
+  uint64_t places[MOST];
+  int32_t count, base;  // (the count may pass the list's end, the row's then does)
+
+  __device__ __forceinline__ void add(uint64_t place) {
+    const int32_t k = atomicAdd(&count, 1);
+    if (k < MOST) places[k] = place;
+  }
+  // (by the whole block; `count` has to be 0 at first)
+  __device__ __forceinline__ void give(const SumTeam& team, uint64_t* to, int32_t* total) {
+    team.sync();
+    if (team.t == 0) base = count ? atomicAdd(total, count) : 0;
+    team.sync();
+    for (int32_t k = team.t; k < min(count, MOST) && k + base < MOST; k += SumTeam::LANES)
+      to[base + k] = places[k];
+  }
+};
+
 // The entries of the border's bin go to the row's list; LAST: it is the last
 // border, and the weights of the bins before it are added up.
 template <int WHICH, bool LAST>
 __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
   __shared__ SumTeam::Shared s;
+  __shared__ PartList<LIST> own;
   __shared__ double s_table[64];
   const SumTeam team(s, threadIdx.x);
   const Where at = where(a);
@@ -237,6 +261,8 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
   const int32_t bin = to.bin;
   const Look look = look_for(a, WHICH, x);
   Weights weight = weights_of(a, s_table, WHICH, x, mine);
+  if (team.t == 0) own.count = 0;
+  team.sync();
   if (bin >= 0)
     row.each4([&](int32_t col, f4 z) INLINE {
       bool in[4], any = false;
@@ -244,18 +270,11 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
       for (int j = 0; j < 4; ++j) any |= in[j] = RowTeam::bin_of(z[j], x.top, look.scale) == bin;
       if (!any) return;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint64_t amount = !in[j] ? 0 : WHICH == 0 ? z[j] >= look.from : weight(z[j], col + j);
-        // (a count past the list's end need not be exact)
-        if (!amount ||
-            __hip_atomic_load(&to.count, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > LIST)
-          continue;
-        const int32_t k = atomicAdd(&to.count, 1);
-        if (k >= LIST) continue;
-        to.place[k] = place(z[j], col + j);
-        to.amount[k] = amount;
-      }
+      for (int j = 0; j < 4; ++j)
+        if (in[j] && (WHICH == 0 ? z[j] >= look.from : weight(z[j], col + j) != 0))
+          own.add(place(z[j], col + j));
     });
+  own.give(team, to.entries, &to.count);
   if (!LAST) return;
   if (a.cut > -INFINITY) weight.kept = earlier(weight.kept, near_entries(x.top, a.cut));
   uint64_t sum = 0;
@@ -302,8 +321,8 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
   if (bin >= 0) {
     if (m <= LIST) {
       for (int32_t k = team.t; k < m; k += 1024) {
-        s.place()[k] = found.place[k];
-        s.amount()[k] = found.amount[k];
+        s.place()[k] = found.entries[k];
+        s.amount()[k] = WHICH == 0 ? 1 : weight.all(logit_of(found.entries[k]));
       }
       if (team.t == 0) s.count = m;
       team.sync();
@@ -324,8 +343,8 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
   };
   if (m <= LIST) {
     for (int32_t k = team.t; k < m; k += 1024) {
-      const int32_t col = (int32_t)(uint32_t)found.place[k];
-      give(col / PART_COLS, weight(logit_of(found.place[k]), col));
+      const int32_t col = (int32_t)(uint32_t)found.entries[k];
+      give(col / PART_COLS, weight(logit_of(found.entries[k]), col));
     }
   } else {
     int32_t part = 0;  // (a lane's columns ascend)
@@ -350,6 +369,160 @@ __device__ __forceinline__ Weights final_weights(const SampleArgs& a, const doub
   else if (a.top_k) w.kept = mine.kept[0];
   else if (a.cut > -INFINITY) w.kept = near_entries(x.top, a.cut);
   return w;
+}
+
+// Where top_p's share of at most LIST first entries is looked for, the row's list
+// takes all entries up to the last of the border's bin, and a block a row does the
+// rest with the list in the place of the row: both borders and the draw.  Top
+// 1,000 of 64 x 131,071 57 us, 85 by the two searches of the whole row, of 1,000 x
+// 40,000 168 and 265; without top_p, where one search is saved, the other way is as
+// fast or faster (top 129 of 1,000 x 40,000 145 us, 160 so).
+__global__ __launch_bounds__(THREADS) void long_gather_kernel(SampleArgs a) {
+  __shared__ SumTeam::Shared s;
+  __shared__ PartList<2 * LIST> mine;
+  const SumTeam team(s, threadIdx.x);
+  const Where at = where(a);
+  PartRow row;
+  row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
+  const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
+  if (!x.ok) return;
+  Search& to = a.rows[at.i].of[0];
+  const Look look = look_for(a, 0, x);
+  const int32_t bin = to.bin < 0 ? BINS : to.bin;
+  if (team.t == 0) mine.count = 0;
+  team.sync();
+  row.each4([&](int32_t col, f4 z) INLINE {
+    if (!(max4(z) >= look.from)) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (z[j] >= look.from && RowTeam::bin_of(z[j], x.top, look.scale) <= bin)
+        mine.add(place(z[j], col + j));
+  });
+  mine.give(team, to.entries, &to.count);
+}
+
+// The border of P among the list's amounts, by bins from `top` down.
+// (few wavefronts wait for each other a shorter time, a crowded row's search from
+// memory wants many: 1,000 x 40,000 with 4, 8 and 16 164, 168 and 206 us, 64 x
+// 131,071 equal logits 611, 408 and 317)
+constexpr int FEW_WAVES = 8;
+using FewTeam = Team<64, FEW_WAVES, LongBins>;
+using FewRow = Listed<64, FEW_WAVES>;
+template <class Amount>
+__device__ __forceinline__ Border border_of(const FewTeam& team, const FewRow& row, Amount amount,
+                                            float top, float scale, uint64_t P) {
+  Border b;
+  int32_t bin;
+  uint64_t base;
+  if (!team.select(row, amount, top, scale, P, &b, &bin, &base))
+    b = team.search(row, amount, top, scale, bin, P, base);
+  team.sync();
+  return b;
+}
+
+// The action among the list's entries up to a border: its column's range shrinks
+// BINS times in each turn.
+__device__ __forceinline__ int32_t draw_few(const SampleArgs& a, const FewTeam& team,
+                                            const FewRow& row, Weights weight, float u) {
+  const float top = (float)weight.top;
+  uint64_t all = 0;
+  if (a.top_p < 1.0) {
+    const float scale = (BINS - 1) * a.inv_range;
+    team.clear();
+    row.each([&](float z, int32_t col) INLINE {
+      const uint64_t w = weight(z, col);
+      all += w;
+      team.add(FewTeam::bin_of(z, top, scale), w, w != 0);
+    });
+    all = team.sum(all);
+    const uint64_t P = (uint64_t)ceil(a.top_p * (double)all);
+    weight.kept = border_of(team, row, weight, top, scale, P < 1 ? 1 : P < all ? P : all);
+  }
+  if (a.cut > -INFINITY) weight.kept = earlier(weight.kept, near_entries(top, a.cut));
+  all = 0;
+  row.each([&](float z, int32_t col) INLINE { all += weight(z, col); });
+  all = team.sum(all);
+  uint64_t target = __umul64hi(all, unit_fraction(u));
+  int32_t from = 0, width = a.C;
+  while (width > 1) {
+    const int32_t end = from + width, step = (int32_t)ceil_div(width, BINS);
+    team.clear();
+    row.each([&](float z, int32_t col) INLINE {
+      if (col < from || col >= end) return;
+      const uint64_t w = weight(z, col);
+      if (w) team.add((col - from) / step, w);
+    });
+    team.sync();
+    int32_t bin = 0;
+    uint64_t base = 0;
+    team.find(target + 1, &bin, &base);
+    team.sync();
+    target -= base;
+    from += bin * step;
+    width = min(step, end - from);
+  }
+  return from;
+}
+
+__global__ __launch_bounds__(FewTeam::LANES) void long_few_kernel(SampleArgs a) {
+  __shared__ FewTeam::Shared s;
+  __shared__ double s_table[64];
+  __shared__ uint64_t s_list[2 * LIST];
+  const FewTeam team(s, threadIdx.x);
+  const int64_t i = a.block0 + blockIdx.x;
+  const Search& found = a.rows[i].of[0];
+  int32_t m = found.count;
+  for (int32_t k = team.t; k < min(m, 2 * LIST); k += FewTeam::LANES) s_list[k] = found.entries[k];
+  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  const LongPart* parts = a.parts + i * a.per_row;
+  const Joined x = joined(team, parts, a.per_row);
+  if (!x.ok) {
+    if (team.t == 0) {
+      a.action[i] = -1;
+      if (a.logp) a.logp[i] = 0.f;
+    }
+    return;
+  }
+  double lse = 0.0;
+  if (a.logp) {
+    for (int32_t k = team.t; k < a.per_row; k += FewTeam::LANES)
+      if (parts[k].sum != 0.0) lse += parts[k].sum * exp_exact((double)parts[k].top - x.top);
+    lse = log_quick((float)team.sum(lse));
+  }
+  const float* from = a.Z + i * a.ld_z;
+  const Look look = look_for(a, 0, x);
+  const Present counts = {look.from};
+  const uint64_t P = (uint64_t)a.top_k;
+  Border b;
+  if (m <= 2 * LIST) {
+    const FewRow all = {s_list, m, team.t};
+    team.clear();
+    all.each([&](float z, int32_t) INLINE {
+      team.add(FewTeam::bin_of(z, x.top, look.scale), 1, z >= look.from);
+    });
+    team.sync();
+    b = border_of(team, all, counts, x.top, look.scale, P);
+  } else {  // a crowded bin: its border from memory, then what is kept to the list
+    Reread<64, FEW_WAVES> row;
+    row.load(from, a.C, team.t);
+    b = team.search(row, counts, x.top, look.scale, found.bin, P, found.base);
+    team.sync();
+    if (team.t == 0) s.count = 0;
+    team.sync();
+    row.each([&](float z, int32_t col) INLINE {
+      if (!(z >= look.from) || !within(b, z, col)) return;
+      const int32_t k = atomicAdd(&s.count, 1);
+      if (k < 2 * LIST) s_list[k] = place(z, col);
+    });
+    team.sync();
+    m = min(s.count, 2 * LIST);
+    team.sync();
+  }
+  const int32_t col = draw_few(a, team, FewRow{s_list, m, team.t},
+                               {Exponential(s_table, a.scale), x.top, b}, a.u[i]);
+  if (team.t) return;
+  a.action[i] = col;
+  if (a.logp) a.logp[i] = (float)((double)from[col] - x.top - lse);
 }
 
 // The parts' weights, where no border was searched.
@@ -550,6 +723,13 @@ hipError_t sample_long(SampleArgs a, void* workspace, hipStream_t stream) {
   a.group = a.top_k ? group_of((int64_t)a.per_row * THREADS, a.C, a.top_k) : 1;
   const int64_t blocks = (int64_t)a.n * a.per_row;
   launch(long_range_kernel, a, blocks, stream);
+  if (a.scale > 0.0 && a.top_k && a.top_k <= LIST && a.top_p < 1.0) {
+    launch(long_bins_kernel<0>, a, blocks, stream);
+    launch(long_find_kernel<0>, a, a.n, stream);
+    launch(long_gather_kernel, a, blocks, stream);
+    launch(long_few_kernel, a, a.n, stream, FewTeam::LANES);
+    return hipGetLastError();
+  }
   if (a.scale > 0.0) {
     const auto search = [&](auto bins, auto find, auto list, auto border) {
       launch(bins, a, blocks, stream);

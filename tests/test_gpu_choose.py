@@ -717,3 +717,26 @@ def test_very_long_rows(C):
     a, _ = run_sample(zero, np.array([0.25, 0.75]), 1.0, 0, 0.5)
     half = int(np.ceil(0.5 * C))
     assert a.tolist() == [half // 4, 3 * half // 4]
+
+
+@pytest.mark.parametrize("C", [33000, 70001])
+def test_long_rows_first_entries(C):
+    """As many first entries as a list holds and more, of rows spread out, of few
+    levels and of one, of rows with fewer entries than are asked for."""
+    n = 6
+    for k, top_k in enumerate((2, 127, 128, 129, 1000, 1023, 1024, 1025, 2049, 5000)):
+        for j, (steps, mask) in enumerate(((0, 0.0), (60, 0.4), (3, 0.0), (1, 0.5), (0, 0.99))):
+            z, rng = _logits(n, C, 300 + k, mask=mask, skip=0.1, steps=steps)
+            for T, top_p, min_p in ((1.0, 0.9, 0.0), ((0.7, 1.0, 0.0), (1.4, 0.6, 0.01))[(k + j) % 2]):
+                u = rng.random(n).astype(np.float32)
+                a, lp = run_sample(z, u, T, top_k, top_p, min_p, pad=k % 3, shift=k % 4)
+                check_sample(z, u, T, top_k, top_p, min_p, a, lp)
+
+
+def test_a_million_columns_first_entries():
+    z, rng = _logits(2, 1 << 20, 400)
+    z[1] = np.where(np.arange(1 << 20) >= (1 << 20) - 1500, z[1], -np.inf)  # next to each other
+    for top_k, top_p in ((700, 0.95), (1024, 0.999), (60, 1.0)):
+        u = rng.random(2).astype(np.float32)
+        a, lp = run_sample(z, u, 0.9, top_k, top_p, 0.0)
+        check_sample(z, u, 0.9, top_k, top_p, 0.0, a, lp)
