@@ -8,10 +8,10 @@
 // caches.  Top logits read it once, and the first k of each part go on.  Sums
 // over parts are of whole numbers, or in a fixed order.
 //
-// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 57 us
-// in five launches of 4 to 19 us (88 with the first 1,025, in ten), without a
-// border 24 to 28 us in three; 1 x 131,071 14 us without, 47 with top-p (one block
-// a row 56 and 179), 34 with top-k and top-p.  500 x 65,536 without a border 75 us,
+// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 51 us
+// in five launches of 3 to 15 us (86 with the first 1,025, in ten), without a
+// border 24 to 28 us in three; 1 x 131,071 14 us without, 45 with top-p (one block
+// a row 56 and 179), 30 with top-k and top-p.  500 x 65,536 without a border 75 us,
 // 64 x 131,071's first 256 37.
 #include "choose.hpp"
 
@@ -374,8 +374,8 @@ __device__ __forceinline__ Weights final_weights(const SampleArgs& a, const doub
 // Where top_p's share of at most LIST first entries is looked for, the row's list
 // takes all entries up to the last of the border's bin, and a block a row does the
 // rest with the list in the place of the row: both borders and the draw.  Top
-// 1,000 of 64 x 131,071 57 us, 85 by the two searches of the whole row, of 1,000 x
-// 40,000 168 and 265; without top_p, where one search is saved, the other way is as
+// 1,000 of 64 x 131,071 51 us, 85 by the two searches of the whole row, of 1,000 x
+// 40,000 152 and 265; without top_p, where one search is saved, the other way is as
 // fast or faster (top 129 of 1,000 x 40,000 145 us, 160 so).
 __global__ __launch_bounds__(THREADS) void long_gather_kernel(SampleArgs a) {
   __shared__ SumTeam::Shared s;

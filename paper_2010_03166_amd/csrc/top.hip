@@ -4,10 +4,10 @@
 // (bins in LDS above what k groups of lanes hold the largest of), then one pass
 // for the exponentials of both parts and the list of the first k, in LDS in the
 // place of the bins, where each entry's place is the number of those before it.
-// Bound by instructions, some 1,640 a wavefront of 2,048 entries with k = 64:
-// 16,384 x 2,048 60 us (the bytes take 28), k = 8 46, k = 256 149, where the
+// Bound by instructions, some 1,680 a wavefront of 2,048 entries with k = 64:
+// 16,384 x 2,048 51 us (the bytes take 28), k = 8 41, k = 256 137, where the
 // comparisons of the list's entries with each other are most of it.  2,000 x
-// 20,011, k = 128: 77 us in two launches (64 + 16; the bytes 32).
+// 20,011, k = 128: 75 us in two launches (63 + 16; the bytes 32).
 #include "choose.hpp"
 
 using namespace gnnprop;
