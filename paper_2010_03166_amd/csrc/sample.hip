@@ -8,7 +8,7 @@
 // 2,048 with top-p 303 us); formed again they cost 16 instructions each.
 //
 // Bound by instructions where the rows are many: 16,384 x 2,048 with top-p takes
-// 101 us, 3,170 vector instructions a wavefront of 2,048 entries, and the vector
+// 101 us, 3,190 vector instructions a wavefront of 2,048 entries, and the vector
 // units issue in nine of ten cycles (the bytes take 27 us); without a border 48.
 // 50,001 x 121 with top-k, top-p, min-p 39 us (the bytes 5): LDS where the first
 // 20 are compared.  Where they are few, by one row's latency beside the launch:
