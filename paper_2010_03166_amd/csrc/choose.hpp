@@ -203,13 +203,29 @@ __device__ __forceinline__ Border first_entries(const T& team, Row& row, const f
   return b;
 }
 
+// The least float z with (double)z - top >= cut, for a cut that is not above 0.
+// The difference never falls as z grows, so the floats between -inf and the top
+// are halved in their order: at most 32 times, whatever the arguments.  (Walking
+// there from top + cut has no such bound.  Where the two cancel, all floats next
+// to 0 have a difference that is rounded to cut: 6e8 of them for 1 and
+// log(exp(-1)).)  It is nearly always next to top + cut, so that is tried first.
+__host__ __device__ inline float least_near(float top, double cut) {
+  uint32_t low = ordered(-INFINITY), high = ordered(top);
+  const auto probe = [&](uint32_t key) INLINE {
+    if (key <= low || key >= high) return;
+    if ((double)float_of(key) - top >= cut) high = key;
+    else low = key;
+  };
+  const uint32_t guess = ordered((float)((double)top + cut));
+  probe(guess);
+  probe(guess - 1);
+  probe(guess + 1);
+  while (high - low > 1) probe(low + (high - low) / 2);
+  return float_of(high);
+}
 // The border of the entries with z - top >= cut, in doubles.
 __device__ __forceinline__ Border near_entries(float top, double cut) {
-  float z = (float)((double)top + cut);
-  while ((double)z - top < cut) z = nextafterf(z, INFINITY);
-  for (float y = nextafterf(z, -INFINITY); (double)y - top >= cut; y = nextafterf(z, -INFINITY))
-    z = y;
-  return {z, 0x7fffffff};
+  return {least_near(top, cut), 0x7fffffff};
 }
 
 __device__ __forceinline__ Border earlier(Border a, Border b) {

@@ -33,10 +33,13 @@ __device__ __forceinline__ bool within(const Border& b, float z, int32_t col) {
   return (z > b.z) | ((z == b.z) & (col <= b.col));
 }
 
-// Bits whose unsigned order is the floats' (0 and -0 alike).
-__device__ __forceinline__ uint32_t ordered(float z) {
-  const uint32_t x = __float_as_uint(z + 0.f);
+// Bits whose unsigned order is the floats' (0 and -0 alike), and back.
+__host__ __device__ __forceinline__ uint32_t ordered(float z) {
+  const uint32_t x = __builtin_bit_cast(uint32_t, z + 0.f);
   return x >> 31 ? ~x : x | 0x80000000u;
+}
+__host__ __device__ __forceinline__ float float_of(uint32_t key) {
+  return __builtin_bit_cast(float, key >> 31 ? key & 0x7fffffffu : ~key);
 }
 // An entry's place in the order, as a number: smaller ones come first.
 __device__ __forceinline__ uint64_t place(float z, int32_t col) {
@@ -77,8 +80,7 @@ struct Bins : Exchange<G, W> {
 
 // The logit of an entry's place.
 __device__ __forceinline__ float logit_of(uint64_t place) {
-  const uint32_t key = ~(uint32_t)(place >> 32);
-  return __uint_as_float(key >> 31 ? key & 0x7fffffffu : ~key);
+  return float_of(~(uint32_t)(place >> 32));
 }
 
 // G lanes of a wavefront, or W whole wavefronts, that hold a row together.

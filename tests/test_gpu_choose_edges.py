@@ -1,0 +1,31 @@
+"""Drawn actions, top logits and the student's loss where a border, a NaN or
+the order of a sum decides (through the C ABI and the Trainer; tolerances as in
+test_gpu_choose.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_choose as base
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("C", [7, 20, 41, 121, 600, 3000, 5000, 9000, 20011, 33000, 70001])
+def test_min_p_where_the_largest_logit_and_the_cut_cancel(C):
+    """A largest logit that is -T ln(min_p) itself: the border lies next to 0, where
+    the differences of 6e8 floats are rounded to the cut.  Logits just around 0."""
+    rng = np.random.default_rng(C)
+    n = 40 if C <= 3000 else 6
+    around = [0.0, -0.0] + [s * 2.0 ** e for s in (1, -1) for e in (-149, -126, -60, -54, -53, -52, -30)]
+    for T, m in ((1.0, 1), (1.0, 2), (0.5, 2), (2.0, 5), (1.0, 10)):
+        min_p = math.exp(-m)
+        z = rng.choice(around, (n, C)).astype(np.float32)
+        z[:, C // 3] = T * m
+        z[1::3, :] += np.where(np.arange(C) == C // 3, 0.0, rng.standard_normal((n, C)))[1::3]
+        z[1::3] = np.minimum(z[1::3], T * m)
+        u = rng.random(n).astype(np.float32)
+        for top_k, top_p in ((0, 1.0), (0, 0.9), (C // 2, 1.0), (5, 0.95), (C // 2, 0.9)):
+            a, lp = base.run_sample(z, u, T, top_k, top_p, min_p)
+            base.check_sample(z, u, T, top_k, top_p, min_p, a, lp)
