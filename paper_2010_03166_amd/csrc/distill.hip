@@ -141,10 +141,13 @@ __device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& te
                                                int32_t from, int32_t end, F ready) {
   Places<T, E> places(named, row, team.t);
   float most = -INFINITY, top = high;
-  constexpr int32_t BAD = 1 << 16;
+  // (lanes with a place that is used, with a logq that is a NaN, with such a logit:
+  // the largest values do not tell of them)
+  constexpr int32_t BAD_Q = 1 << 10, BAD_Z = 1 << 20;
+  static_assert(T::LANES < BAD_Q, "each count stays below the next");
   int32_t used = 0;
   places.each([&](int32_t, float lq, float z, double&, double&) INLINE {
-    used = (used & BAD) | (lq != lq ? BAD + 1 : 1);
+    used |= 1 | (lq != lq ? BAD_Q : 0) | (z != z ? BAD_Z : 0);
     most = fmaxf(most, lq);
     top = fmaxf(top, z);
   });
@@ -153,8 +156,10 @@ __device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& te
   most = -low;
   rest = rest > 0.f ? rest : rest == rest ? 0.f : rest;
   if (rest > 0.f) most = fmaxf(most, (float)log_quick(rest));
+  const bool says = (used % BAD_Z >= BAD_Q) | (most > -INFINITY);
+  const bool nan = (used >= BAD_Z) | (sum != sum);
   Scalars s = {};
-  s.live = (used > 0) & ((used >= BAD) | (most > -INFINITY)) & (top > -INFINITY);
+  s.live = (used > 0) & says & (nan | (top > -INFINITY));
   if (!s.live) {
     ready(s);
     return s;
@@ -179,7 +184,9 @@ __device__ __forceinline__ Scalars row_scalars(const DistillArgs& a, const T& te
   s.kl = a.T * a.T * (cross / nq + log_of(np / nq));
   s.scale_q = 1.0 / nq;
   s.scale_p = 1.0 / np;
-  s.others = sum == 0.0 ? 0.f : (float)(a.T * (down * s.scale_p - r * s.scale_q / sum));
+  // (without entries of a share the factor is for those of -inf: 0, but for a NaN)
+  s.others = sum == 0.0 ? (np == np ? 0.f : NAN)
+                        : (float)(a.T * (down * s.scale_p - r * s.scale_q / sum));
   ready(s);
   if (!to) return s;
   places.each([&](int32_t c, float logq, float z, double q, double p) INLINE {

@@ -29,3 +29,34 @@ def test_min_p_where_the_largest_logit_and_the_cut_cancel(C):
         for top_k, top_p in ((0, 1.0), (0, 0.9), (C // 2, 1.0), (5, 0.95), (C // 2, 0.9)):
             a, lp = base.run_sample(z, u, T, top_k, top_p, min_p)
             base.check_sample(z, u, T, top_k, top_p, min_p, a, lp)
+
+
+@pytest.mark.parametrize("C", [2, 4, 7, 16, 41, 121, 600, 3000, 9000, 20011, 70001])
+def test_student_that_is_nan_everywhere(C):
+    """A row without a single number is not a row left out: its NaN shows in its kl
+    and gradient, whether the list names a NaN, -inf or nothing but them."""
+    n = 6
+    for k in sorted({1, min(C, 3), min(C, 200)}):
+        z, index, logq, rest, w = base._taught(n, C, k, 8, 1.0)
+        w[:] = 1.0 / n
+        z[0] = np.nan
+        z[1] = -np.inf
+        z[1, index[1, 0]] = np.nan                # named, all else is not there
+        z[2] = -np.inf
+        z[2, np.setdiff1d(np.arange(C), index[2])] = np.nan  # the others, where there are any
+        z[3] = np.nan
+        w[3] = 0.0                                # adds nothing
+        z[4] = np.nan
+        index[4] = -1                             # left out
+        shows = [0, 1] + ([2] if k < C else [])
+        for left in (rest, None):
+            want = base.O.distill(z, index, logq, left, w, 1.0)
+            r = base.run_distill(z, index, logq, left, w, 1.0)
+            assert np.isnan(r["out"]) and np.isnan(want["out"])
+            for i in shows:
+                assert np.isnan(r["kl"][i]) and np.isnan(want["kl"][i]), i
+                assert np.isnan(r["dZ"][i]).all() and np.isnan(want["dZ"][i]).all(), i
+            if k == C:
+                assert r["kl"][2] == 0 and np.all(r["dZ"][2] == 0)
+            assert np.isnan(r["kl"][3]) and np.all(r["dZ"][3:5] == 0) and r["kl"][4] == 0
+            assert np.isfinite(r["kl"][5]) and np.isfinite(r["dZ"][5]).all()
