@@ -294,13 +294,17 @@ struct TopArgs {
   int32_t per_row;
 };
 
-// The entries up to a border into the list (of `most` places; `count` of them, put
-// to 0 before), and the sums of exp((z - top) / T) over them and over the others
-// (the lane's shares).
-template <class T, class Row>
-__device__ __forceinline__ void collect(const T& team, const Row& row, const Border& b, float top,
-                                        double inv_t, uint64_t* list, int32_t most,
-                                        double* in_sum, double* out_sum) {
+// The entries up to a border into the list (of `most` places), and the sums of
+// exp((z - top) / T) over them and over the others (the lane's shares).  In any
+// order, counted in team.s.count (put to 0 before); or, ORDERED, the wavefront's
+// into a list of its own, by chunks and lanes, so that it is the same in every call:
+// returns how many.
+template <bool ORDERED, class T, class Row>
+__device__ __forceinline__ int32_t collect(const T& team, const Row& row, const Border& b,
+                                           float top, double inv_t, uint64_t* list, int32_t most,
+                                           double* in_sum, double* out_sum) {
+  static_assert(!ORDERED || T::G == 64, "whole wavefronts");
+  int32_t count = 0;
   const float octaves = (float)(inv_t * 1.4426950408889634);
   double in = 0.0, out = 0.0;
   row.each4([&](int32_t col, f4 z) INLINE {
@@ -316,18 +320,27 @@ __device__ __forceinline__ void collect(const T& team, const Row& row, const Bor
       less += kept[j] ? 0.f : e[j];
     }
     out += less;
-    if (!any) return;
+    if (ORDERED ? !__ballot(any) : !any) return;
     float more = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
+      int32_t at;
+      if constexpr (ORDERED) {
+        const uint64_t who = __ballot(kept[j]);
+        at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32),
+                                               __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+        count += __popcll(who);
+      }
       if (!kept[j]) continue;
+      if constexpr (!ORDERED) at = atomicAdd(&team.s.count, 1);
       more += e[j];
-      list[min(atomicAdd(&team.s.count, 1), most - 1)] = place(z[j], col + j);
+      list[min(at, most - 1)] = place(z[j], col + j);
     }
     in += more;
   });
   *in_sum = in;
   *out_sum = out;
+  return count;
 }
 
 // A row's outputs from the list of its first entries and the sums of both

@@ -629,7 +629,6 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
 
 __global__ __launch_bounds__(THREADS) void top_part_kernel(TopArgs a) {
   __shared__ TopTeam::Shared s;
-  __shared__ uint64_t s_list[MOST_TOP];
   const TopTeam team(s, threadIdx.x);
   const Where at = where(a);
   const float* from = a.Z + at.i * a.ld_z;
@@ -643,18 +642,24 @@ __global__ __launch_bounds__(THREADS) void top_part_kernel(TopArgs a) {
   int32_t m = 0;
   if (ok) {
     const Border b = first_entries(team, row, from, a.C, a.k, p.top, low, p.lanes, at.col0);
-    if (team.t == 0) s.count = 0;
-    team.sync();
+    // (in one order, since the join's sums go over them; a list for each wavefront in
+    // the place of what found the border)
+    static_assert(TopTeam::Shared::WORDS >= TopTeam::W * MOST_TOP, "the lists fit");
+    uint64_t* list = s.words + team.wave * MOST_TOP;
     double in, out;
-    collect(team, row, b, p.top, a.inv_t, s_list, a.k, &in, &out);
-    p.others = team.sum(out);
-    team.sync();
-    m = min(s.count, a.k);
+    const int32_t own = min(collect<true>(team, row, b, p.top, a.inv_t, list, a.k, &in, &out), a.k);
+    if (team.lane == 0) s.flags[team.wave] = own;
+    p.others = team.sum(out);  // (and every wavefront's count is there)
+    int32_t before = 0;
+    for (int k = 0; k < TopTeam::W; ++k) {
+      if (k < team.wave) before += s.flags[k];
+      m += s.flags[k];
+    }
+    for (int32_t k = team.lane; k < own && before + k < a.k; k += 64) to[before + k] = list[k];
   } else if (p.top == INFINITY) {
     p.lanes |= BAD_LANES;
   }
-  for (int32_t k = team.t; k < a.k; k += THREADS)
-    to[k] = k < m ? s_list[k] : place(-INFINITY, 0x7fffffff);
+  for (int32_t k = m + team.t; k < a.k; k += THREADS) to[k] = place(-INFINITY, 0x7fffffff);
   if (team.t == 0) a.parts[part] = p;
 }
 

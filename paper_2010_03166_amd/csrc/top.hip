@@ -40,7 +40,7 @@ __global__ __launch_bounds__((threads_of<G, W>())) void top_kernel(TopArgs a) {
   if (team.t == 0) team.s.count = 0;
   team.sync();
   double in, out;
-  collect(team, row, b, top, a.inv_t, list, a.k, &in, &out);
+  collect<false>(team, row, b, top, a.inv_t, list, a.k, &in, &out);
   in = team.sum(in);
   out = team.sum(out);
   team.sync();

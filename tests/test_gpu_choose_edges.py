@@ -60,3 +60,22 @@ def test_student_that_is_nan_everywhere(C):
                 assert r["kl"][2] == 0 and np.all(r["dZ"][2] == 0)
             assert np.isnan(r["kl"][3]) and np.all(r["dZ"][3:5] == 0) and r["kl"][4] == 0
             assert np.isfinite(r["kl"][5]) and np.isfinite(r["dZ"][5]).all()
+
+
+@pytest.mark.parametrize("C,k", [(16385, 3), (20011, 128), (70001, 256)])
+def test_long_rows_parts_are_listed_in_one_order(C, k):
+    """What the parts of a long row hand on, which later sums go over, lies in the
+    same order in every call."""
+    n = 60
+    Z = torch.randn((n, C), device="cuda", generator=torch.Generator("cuda").manual_seed(C))
+    need = base.G.gnn_top_workspace_bytes(n, C, k)
+    first = None
+    for _ in range(12):
+        ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+        i, q = torch.empty((n, k), dtype=torch.int32, device="cuda"), torch.empty((n, k), device="cuda")
+        rest = torch.empty(n, device="cuda")
+        base.G.gnn_top_logits(n, C, Z, C, k, 1.0, i, q, rest, ws)
+        got = (i, q, rest, ws)
+        first = first or got
+        for a, b in zip(first, got):
+            assert torch.equal(a, b)
