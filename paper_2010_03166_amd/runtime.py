@@ -603,10 +603,8 @@ class Trainer:
         other use, once they are replaced, until every stream that used them
         is done."""
         n, C, f = self.n, self.C, self.f_top
-        need = max(G.gnn_policy_workspace_bytes(n, C), G.gnn_sample_workspace_bytes(n, C),
-                   G.gnn_distill_workspace_bytes(n, C, G.GNN_TOP_MOST),
-                   G.gnn_gemm_workspace_bytes(n, C, f), G.gnn_gemm_workspace_bytes(f, C, n),
-                   G.gnn_gemm_workspace_bytes(n, f, C), 256)
+        need = max(G.gnn_policy_workspace_bytes(n, C), G.gnn_gemm_workspace_bytes(n, C, f),
+                   G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C), 256)
         if self.policy_ws is None or self.policy_ws.numel() < need or self._Z.buf.shape[0] < n:
             with torch.cuda.stream(_stream_object(stream)):
                 self._Z = _Rows(C, self._Z.ld, self.device)
@@ -653,6 +651,11 @@ class Trainer:
         t.record_stream(torch.cuda.current_stream())
         return t
 
+    def _workspace(self, nbytes: int, stream):
+        """Working memory of one call: what only some calls need is not kept for
+        those that do not (a draw's is some 50 KB a row past 32,768 columns)."""
+        return self._new((max(nbytes, 256),), torch.uint8, stream)
+
     def act(self, X: torch.Tensor, u: torch.Tensor, temperature: float = 1.0, top_k: int = 0,
             top_p: float = 1.0, min_p: float = 0.0, stream=None):
         """Draws each row's action under the present weights by its random
@@ -663,8 +666,9 @@ class Trainer:
         _, _, Z, ld = self._logits(X, stream)
         actions = self._new((self.n,), torch.int32, stream)
         logp = self._new((self.n,), torch.float32, stream)
+        ws = self._workspace(G.gnn_sample_workspace_bytes(self.n, self.C), stream)
         G.gnn_sample_actions(self.n, self.C, Z, ld, u, temperature, top_k, top_p, min_p, actions,
-                             logp, self.policy_ws, stream)
+                             logp, ws, stream)
         return actions, logp
 
     def top_logits(self, X: torch.Tensor, k: int, temperature: float = 1.0, stream=None):
@@ -674,8 +678,7 @@ class Trainer:
         tensors, for another Trainer's distill_step.  stream: as in
         action_logp."""
         _, _, Z, ld = self._logits(X, stream)
-        ws = self._new((max(G.gnn_top_workspace_bytes(self.n, self.C, k), 256),), torch.uint8,
-                       stream)
+        ws = self._workspace(G.gnn_top_workspace_bytes(self.n, self.C, k), stream)
         index = self._new((self.n, k), torch.int32, stream)
         logq = self._new((self.n, k), torch.float32, stream)
         rest = self._new((self.n,), torch.float32, stream)
@@ -736,7 +739,8 @@ class Trainer:
         n, C, k = self.n, self.C, int(index.shape[1])
         top, ld_top, Z, ld = self._logits(X, stream)
         dZ = self._dZ.view(n)
+        ws = self._workspace(G.gnn_distill_workspace_bytes(n, C, k), stream)
         G.gnn_distill_loss(n, C, Z, ld, k, index, logq, rest, weight, temperature,
-                           self.distill_out, None, dZ, ld, self.policy_ws, stream)
+                           self.distill_out, None, dZ, ld, ws, stream)
         self._learn(top, ld_top, dZ, ld, stream)
         return self.distill_out

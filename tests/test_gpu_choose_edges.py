@@ -79,3 +79,36 @@ def test_long_rows_parts_are_listed_in_one_order(C, k):
         first = first or got
         for a, b in zip(first, got):
             assert torch.equal(a, b)
+
+
+def test_policy_steps_keep_no_workspace_of_draws():
+    """What drawing and teaching work in is not held for policy steps: the shared
+    workspace is the policy's and the products', before those calls and after, and
+    its memory stays where it is (a captured step goes on using it)."""
+    n, C, f_in, h = 3000, 33000, 24, 16
+    rng, S, G = np.random.default_rng(3), base.synth, base.G
+    params = [S.LayerParams(S.glorot(f_in, h, rng), S.glorot(f_in, h, rng))]
+    f = 2 * h
+    tr = base.runtime.Trainer(base.prepared(S.power_law_graph(n, 2.1, 8.0, seed=7)), params, f_in,
+                              rng.standard_normal((f, C)).astype(np.float32), False, "sgd", lr=1e-3)
+    X = base.to_dev(rng.standard_normal((n, f_in)).astype(np.float32), 28)
+    assert G.gnn_sample_workspace_bytes(n, C) > 2 * max(
+        G.gnn_gemm_workspace_bytes(*x) for x in ((n, C, f), (f, C, n), (n, f, C)))
+    u = torch.rand(n, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    tr.policy_step(X, torch.zeros(n, dtype=torch.int32, device="cuda"), torch.ones(n, device="cuda"))
+    held = (tr.policy_ws.numel(), tr.policy_ws.data_ptr())
+    assert held[0] == max(G.gnn_policy_workspace_bytes(n, C), G.gnn_gemm_workspace_bytes(n, C, f),
+                          G.gnn_gemm_workspace_bytes(f, C, n), G.gnn_gemm_workspace_bytes(n, f, C), 256)
+    s = torch.cuda.Stream()
+    for stream in (None, s.cuda_stream):
+        torch.cuda.synchronize()
+        a, lp = tr.act(X, u, 0.9, 50, 0.9, 0.01, stream=stream)
+        index, logq, rest = tr.top_logits(X, 3, stream=stream)
+        torch.cuda.synchronize()
+        Z = tr._Z.view(n)[-9:].cpu().numpy()
+        last = lambda *ts: [t[-9:].cpu().numpy() for t in ts]
+        base.check_sample(Z, *last(u), 0.9, 50, 0.9, 0.01, *last(a, lp))
+        base.check_top(Z, 3, 1.0, last(index, logq, rest))
+        tr.distill_step(X, index, logq, rest, stream=stream)
+        torch.cuda.synchronize()
+        assert held == (tr.policy_ws.numel(), tr.policy_ws.data_ptr())
