@@ -451,10 +451,12 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  * and the action is the first of the kept entries, by columns, with which the
  * sum of their e passes u times the sum of all kept.  T = 0: the first entry
  * of the order, whatever the rest (u may be NULL).  Weights e are whole
- * multiples of 2^-51 (of 2^(log C - 62) where C > 2048, log C rounded up), each
- * off by less than 1e-13 and half a multiple; nothing else is rounded but
- * top_p's product and log min_p, in double, so that an action does not depend
- * on how a sum is formed, and equal logits are equally likely.
+ * multiples of a unit: 2^-51, where C > 2048 2^(log C - 62) with log C rounded
+ * up, and where C > 2^18 the larger of 2^-51 and 2^(log s - 62), s being the
+ * row's sum of e times at most 65/64 and log s rounded up.  Each is off by less
+ * than 1e-13 and half a unit; nothing else is rounded but top_p's product and
+ * log min_p, in double, so that an action does not depend on how a sum is
+ * formed, and equal logits are equally likely.
  * u: n floats in [0, 1) (those below or NaN count as 0, those above as the
  * last number below 1).  action: n int32, -1 for rows left out.  logp (n
  * floats, may be NULL): the actions' log-probabilities under Z itself (T = 1,

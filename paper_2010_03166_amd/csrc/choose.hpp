@@ -36,7 +36,13 @@ constexpr Table make_table() {
 static __constant__ const Table TABLE = make_table();
 
 // Units of a weight: 2^bits of them are the largest one.  At most 2^62 a row,
-// and 51 bits leave the product below a double's first bit.
+// and 51 bits leave the product below a double's first bit.  What rounding to
+// them can move from one side of a border to the other is C half units of a sum
+// of 2^bits or more: 2^(2 log C - 63) of it.  Past BY_SUM columns that would pass
+// 2^-27 (a random number's last bit is 2^-24, and among 2^24 columns all that are
+// below 2^-39 of the largest would be lost, 2^-15 of the sum), so there the units
+// follow from the row's sum (long_rows.hip): at most 2^-28 of it then.
+constexpr int32_t BY_SUM = 1 << 18;
 inline int bits_of(int32_t C) {
   int log = 0;
   while ((int64_t)1 << log < C) ++log;
@@ -90,6 +96,7 @@ struct SampleArgs {
   double scale;  // 64 / (T ln 2); 0: the best action
   float inv_range;  // 1 / (T ln(C / (1 - top_p))): no border of top_p is as far from the top
   int32_t bits, top_k;
+  double inv_t;  // 1 / T where units follow from the row's sum, or 0
   double top_p;
   double cut;   // T ln(min_p), or -inf
   double unit;  // 2^-bits where a sum of weights is that of the log-probabilities, or 0

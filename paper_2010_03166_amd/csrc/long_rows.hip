@@ -56,6 +56,7 @@ struct LongPart {
   float top, low, least;  // largest, least of the groups' largest, least logit
   int32_t lanes;          // groups with a logit
   double sum;             // of exp(z - top)
+  double mass;            // of exp((z - top) / T), where units follow from the row's sum
   uint64_t kept;          // weights
 };
 struct TopPart {
@@ -108,6 +109,30 @@ __device__ __forceinline__ Where where(const Args& a) {
   return {b / a.per_row, part, part * PART_COLS};
 }
 
+// The table of weights' exponentials, in units of all rows of a call, while the
+// block's reads are under way.
+__device__ __forceinline__ void start_table(const SampleArgs& a, double* table) {
+  if (threadIdx.x < 64) table[threadIdx.x] = ldexp(TABLE.at[threadIdx.x], a.bits);
+}
+// Past BY_SUM columns in units of the row, 2^62 of which are the least power of two
+// above its sum (an fp32 sum, good to 2e-5, and 1/64 for that).  Parts are added as
+// whole 256ths, in any order the same: every launch has to find the same units.
+template <class T>
+__device__ __forceinline__ void row_table(const SampleArgs& a, const T& team,
+                                          const LongPart* parts, const Joined& x,
+                                          double* table) {
+  if (a.inv_t == 0.0) return;
+  uint64_t sum = 0;
+  for (int32_t k = team.t; k < a.per_row; k += T::LANES)
+    if (parts[k].mass > 0.0)
+      sum += (uint64_t)ceil(256.0 * parts[k].mass *
+                            exp_exact(((double)parts[k].top - x.top) * a.inv_t));
+  sum = team.sum(sum);
+  const int bits = min(51, 62 + 8 - (64 - __clzll((long long)(sum + sum / 64))));
+  if (team.t < 64) table[team.t] = ldexp(TABLE.at[team.t], bits);
+  team.sync();
+}
+
 // ------------------------------------------------------------------ draws
 
 __global__ __launch_bounds__(THREADS) void long_range_kernel(SampleArgs a) {
@@ -137,6 +162,16 @@ __global__ __launch_bounds__(THREADS) void long_range_kernel(SampleArgs a) {
     const float shift = shift_of(p.top);
     row.each4([&](int32_t, f4 z) INLINE { p.sum += (double)sum4(exp4(z, shift)); });
     p.sum = team.sum(p.sum);
+  }
+  if (a.inv_t > 0.0) {
+    const float shift = shift_of(p.top), octaves = (float)(a.inv_t * 1.4426950408889634);
+    row.each4([&](int32_t, f4 z) INLINE {
+      f4 e;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f((z[j] - shift) * octaves);
+      p.mass += (double)sum4(e);
+    });
+    p.mass = team.sum(p.mass);
   }
   if (team.t == 0) a.parts[at.i * a.per_row + at.part] = p;
 }
@@ -175,9 +210,10 @@ __global__ __launch_bounds__(THREADS) void long_bins_kernel(SampleArgs a) {
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
-  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  start_table(a, s_table);
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
+  if (WHICH == 1) row_table(a, team, a.parts + at.i * a.per_row, x, s_table);
   LongRow& mine = a.rows[at.i];
   const Look look = look_for(a, WHICH, x);
   team.clear();
@@ -253,9 +289,10 @@ __global__ __launch_bounds__(THREADS) void long_list_kernel(SampleArgs a) {
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
-  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  start_table(a, s_table);
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
+  if (WHICH == 1 || LAST) row_table(a, team, a.parts + at.i * a.per_row, x, s_table);
   LongRow& mine = a.rows[at.i];
   Search& to = mine.of[WHICH];
   const int32_t bin = to.bin;
@@ -305,10 +342,11 @@ __global__ __launch_bounds__(1024) void long_border_kernel(SampleArgs a) {
   __shared__ double s_table[64];
   const RowTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
-  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  start_table(a, s_table);
   LongPart* parts = a.parts + i * a.per_row;
   const Joined x = joined(team, parts, a.per_row);
   if (!x.ok) return;
+  if (WHICH == 1 || LAST) row_table(a, team, parts, x, s_table);
   LongRow& mine = a.rows[i];
   const Search& found = mine.of[WHICH];
   const int32_t bin = found.bin, m = found.count;
@@ -473,7 +511,7 @@ __global__ __launch_bounds__(FewTeam::LANES) void long_few_kernel(SampleArgs a) 
   const Search& found = a.rows[i].of[0];
   int32_t m = found.count;
   for (int32_t k = team.t; k < min(m, 2 * LIST); k += FewTeam::LANES) s_list[k] = found.entries[k];
-  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  start_table(a, s_table);
   const LongPart* parts = a.parts + i * a.per_row;
   const Joined x = joined(team, parts, a.per_row);
   if (!x.ok) {
@@ -483,6 +521,7 @@ __global__ __launch_bounds__(FewTeam::LANES) void long_few_kernel(SampleArgs a) 
     }
     return;
   }
+  row_table(a, team, parts, x, s_table);
   double lse = 0.0;
   if (a.logp) {
     for (int32_t k = team.t; k < a.per_row; k += FewTeam::LANES)
@@ -533,9 +572,10 @@ __global__ __launch_bounds__(THREADS) void long_kept_kernel(SampleArgs a) {
   const Where at = where(a);
   PartRow row;
   row.load(a.Z + at.i * a.ld_z, a.C, team.t, at.col0);
-  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  start_table(a, s_table);
   const Joined x = joined(team, a.parts + at.i * a.per_row, a.per_row);
   if (!x.ok) return;
+  row_table(a, team, a.parts + at.i * a.per_row, x, s_table);
   const Weights weight = final_weights(a, s_table, x, a.rows[at.i]);
   uint64_t sum = 0;
   row.each4([&](int32_t col, f4 z) INLINE { sum += weight.sum4(z, col); });
@@ -552,7 +592,7 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
   __shared__ uint64_t s_target;
   const SumTeam team(s, threadIdx.x);
   const int64_t i = a.block0 + blockIdx.x;
-  if (team.t < 64) s_table[team.t] = ldexp(TABLE.at[team.t], a.bits);
+  start_table(a, s_table);
   const LongPart* parts = a.parts + i * a.per_row;
   const Joined x = joined(team, parts, a.per_row);
   if (!x.ok) {
@@ -562,6 +602,7 @@ __global__ __launch_bounds__(THREADS) void long_draw_kernel(SampleArgs a) {
     }
     return;
   }
+  row_table(a, team, parts, x, s_table);
   double lse = 0.0;
   if (a.logp) {
     for (int32_t k = team.t; k < a.per_row; k += THREADS)

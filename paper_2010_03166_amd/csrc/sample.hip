@@ -379,6 +379,7 @@ gnn_status gnn_sample_actions(int32_t n, int32_t C, const float* Z, int64_t ld_z
   a.inv_range = top_p < 1.0 && temperature > 0.0
                     ? (float)(1.0 / (temperature * std::log(C / (1.0 - top_p)))) : 0.f;
   a.bits = bits_of(C);
+  a.inv_t = C > BY_SUM && temperature > 0.0 ? 1.0 / temperature : 0.0;
   a.top_k = top_k < C ? top_k : 0;
   a.top_p = top_p;
   a.cut = min_p > 0.0 ? temperature * std::log(min_p) : -INFINITY;

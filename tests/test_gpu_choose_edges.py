@@ -112,3 +112,53 @@ def test_policy_steps_keep_no_workspace_of_draws():
         tr.distill_step(X, index, logq, rest, stream=stream)
         torch.cuda.synchronize()
         assert held == (tr.policy_ws.numel(), tr.policy_ws.data_ptr())
+
+
+@pytest.mark.parametrize("C", [1 << 20, (1 << 22) + 3, 1 << 24])
+def test_entries_that_count_only_together(C):
+    """One entry of weight 1 and all others below 2^(log C - 63), which is half of
+    what a sum as large as C would leave as a unit: together they are 2^-23 to 2^-15
+    of the sum, and numbers past the first entry's share draw them.  A weight is
+    off by 2^-52 and 1e-13 of itself, so what lies before an action by C 2^-52 +
+    2e-13 at most."""
+    half = 2.0 ** (math.ceil(math.log2(C)) - 63)
+    at, tol = C // 2, C * 2.0 ** -52 + 2e-13
+    u = np.array([0.0, 0.5, 1 - 2.0 ** -24, 1 - 2.0 ** -23], np.float32)
+    for T in (1.0, 0.7):
+        z = np.full((1, C), T * math.log(0.9 * half), np.float32)
+        z[0, at] = 0.0
+        t = math.exp(float(z[0, 0]) / T)
+        lse = math.log(1 + (C - 1) * math.exp(float(z[0, 0])))
+        z = np.broadcast_to(z, (len(u), C))
+        tail = (C - 1) * t
+        p = 1 - tail / 4           # a quarter of the others left out
+        for top_k, top_p, min_p, others in ((0, 1.0, 0.0, C - 1), (C - 5, 1.0, 0.0, C - 6),
+                                            (0, p, 0.0, None), (0, 1.0, t / 2, C - 1),
+                                            (C - 5, p, 0.0, None), (0, 1.0, 2 * t, 0)):
+            if others is None:     # (a share of the first C - 5 where they are asked for)
+                others = math.ceil((p * (1 + (top_k - 1 if top_k else C - 1) * t) - 1) / t)
+            a, lp = base.run_sample(z, u, T, top_k, top_p, min_p)
+            kept = 1 + others * t
+            if others == 0:
+                assert np.all(a == at)
+                continue
+            assert a.max() <= others + tol / t  # (those kept are the first)
+            for i in range(len(u)):
+                before = a[i] * t if a[i] <= at else 1 + (a[i] - 1) * t
+                own = 1.0 if a[i] == at else t
+                assert before - 2 * tol <= float(u[i]) * kept <= before + own + 2 * tol, (i, a[i])
+            want = np.where(a == at, 0.0, float(z[0, 0])) - lse
+            assert np.all(np.abs(lp - want) <= (20 + math.log(C)) * base.U + base.U * np.abs(want))
+
+
+def test_as_many_equal_logits_as_a_row_has():
+    """Sums of 2^24 largest weights fit: an action is a random number's 2^24th."""
+    C = 1 << 24
+    k = np.array([0, 1, 12345678, C - 1], np.int64)
+    z = np.broadcast_to(np.float32(-3.5), (4, C))
+    u = (k / C).astype(np.float32)
+    for T in (1.0, 5.0):
+        a, _ = base.run_sample(z, u, T)
+        assert np.array_equal(a, k)
+    a, _ = base.run_sample(z, u, 1.0, 0, 0.5)
+    assert np.array_equal(a, k // 2)
