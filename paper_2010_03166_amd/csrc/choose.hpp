@@ -414,13 +414,14 @@ template <class Args, class Kernel>
 Launch<Args> choose(int32_t n, int32_t C, int32_t places = 0) {
   const Shape s = shape_of(n, C, places, Kernel::SMALL, Chosen<Args, Kernel>::SPREAD);
   if (s.G > 1) return of_shape(s, Chosen<Args, Kernel>());
+  if constexpr (Kernel::SMALL > 24)
+    if (s.V == 8) return {Kernel::template small<8>(), 256, 256};
   switch (s.V) {
     case 1: return {Kernel::template small<1>(), 256, 256};
     case 2: return {Kernel::template small<2>(), 256, 256};
     case 4: return {Kernel::template small<4>(), 256, 256};
-    case 6: return {Kernel::template small<6>(), 256, 256};
   }
-  return {Kernel::template small<8>(), 256, 256};
+  return {Kernel::template small<6>(), 256, 256};
 }
 
 template <class Args>

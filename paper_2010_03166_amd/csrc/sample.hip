@@ -5,7 +5,8 @@
 // every pass goes over them: its range, the border of the first top_k, weights
 // into bins and top_p's border, the kept sum with the draw.  Formed once and
 // kept, the weights took 64 registers beside a row's 32 and spilled (16,384 x
-// 2,048 with top-p 303 us); formed again they cost 16 instructions each.
+// 2,048 with top-p 303 us); formed again they cost 16 instructions each.  (1,024
+// threads with eight chunks, past 24,576 columns, have 22 registers on the stack.)
 //
 // Bound by instructions where the rows are many: 16,384 x 2,048 with top-p takes
 // 101 us, 3,190 vector instructions a wavefront of 2,048 entries, and the vector
@@ -205,15 +206,17 @@ __device__ __forceinline__ void sample_row(const SampleArgs& a, const T& team, i
   pick_entry<KEPT>(a, team, row, weight, i, target, lse, sums);
 }
 
-// Blocks that share a CU, by the registers that a row takes.
+// The wavefronts that a vector unit has to hold: four of 256 threads' kernels, three
+// where a row takes more than four chunks; of 512 and 1,024 threads two and one, which
+// leaves the registers to the compiler (eight chunks of 512 threads take 164, one block
+// of a CU; held to 128, for two of them, 32 were spilled).
 template <int G, int W, class Row>
-constexpr int blocks_of() {
-  const int waves = W < 8 && Row::CHUNKS > 4 ? 12 : 16;  // of a CU
-  return waves * 64 / threads_of<G, W>();
+constexpr int waves_of() {
+  return W == 16 ? 1 : W == 8 ? 2 : Row::CHUNKS > 4 ? 3 : 4;
 }
 
 template <int G, int W, class Row>
-__global__ __launch_bounds__((threads_of<G, W>()), (blocks_of<G, W, Row>()))
+__global__ __launch_bounds__((threads_of<G, W>()), (waves_of<G, W, Row>()))
 void sample_kernel(SampleArgs a) {
   using T = Team<G, W>;
   constexpr int R = threads_of<G, W>() / T::LANES;
