@@ -162,3 +162,31 @@ def test_as_many_equal_logits_as_a_row_has():
         assert np.array_equal(a, k)
     a, _ = base.run_sample(z, u, 1.0, 0, 0.5)
     assert np.array_equal(a, k // 2)
+
+
+@pytest.mark.parametrize("n,C", [
+    (66000, 9), (66000, 13), (66000, 16), (66000, 17), (66000, 21), (66000, 24), (66000, 25),
+    (66000, 32), (66000, 33), (20000, 50), (20000, 121), (9000, 250), (2100, 1000), (1100, 1300),
+    (1100, 1537), (1100, 2048), (600, 2049), (300, 3000), (600, 4096), (300, 5000), (600, 6001),
+    (600, 8192), (300, 8193), (300, 12289), (300, 16384), (300, 20011), (100, 30000)])
+def test_rows_enough_for_every_shape(n, C):
+    """Rows as many as other shapes take (lanes alone, wavefronts alone, fewer
+    wavefronts): some of them against the oracle, all calls."""
+    z, rng = base._logits(n, C, 900, mask=0.2, skip=0.02)
+    u = rng.random(n).astype(np.float32)
+    some = np.unique(np.concatenate([np.arange(12), n - 1 - np.arange(12), rng.integers(0, n, 16)]))
+    for T, top_k, top_p, min_p in base.SETTINGS + [(0.8, C // 3 + 1, 0.9, 0.0)]:
+        a, lp = base.run_sample(z, u, T, top_k, top_p, min_p, pad=1, shift=3)
+        base.check_sample(z[some], u[some], T, top_k, top_p, min_p, a[some], lp[some])
+    for k in (1, 8, 70, 256):
+        got = base.run_top(z, k, 1.3, pad=1, shift=1)
+        base.check_top(z[some], k, 1.3, tuple(x[some] for x in got))
+        t = z + np.float32(0.3) * (np.arange(C) % 5).astype(np.float32)
+        index, logq, rest = base.run_top(t, k, 1.3)
+        left = np.setdiff1d(np.arange(n), some)
+        w = np.zeros(n, np.float32)      # (the loss is then of the rows looked at)
+        w[some] = 1.0 / len(some)
+        r = base.run_distill(z, index, logq, rest, w, 1.3, pad=2)
+        assert np.all(r["dZ"][left] == 0)
+        picked = dict(out=r["out"], kl=r["kl"][some], dZ=r["dZ"][some])
+        base.check_distill(picked, z[some], index[some], logq[some], rest[some], w[some], 1.3)
