@@ -453,7 +453,7 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  * of the order, whatever the rest (u may be NULL).  Weights e are whole
  * multiples of a unit: 2^-51, where C > 2048 2^(log C - 62) with log C rounded
  * up, and where C > 2^18 the larger of 2^-51 and 2^(log s - 62), s being the
- * row's sum of e times at most 65/64 and log s rounded up.  Each is off by less
+ * row's sum of e times at most 33/32 and log s rounded up.  Each is off by less
  * than 1e-13 and half a unit; nothing else is rounded but top_p's product and
  * log min_p, in double, so that an action does not depend on how a sum is
  * formed, and equal logits are equally likely.
@@ -461,8 +461,9 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  * last number below 1).  action: n int32, -1 for rows left out.  logp (n
  * floats, may be NULL): the actions' log-probabilities under Z itself (T = 1,
  * nothing cut off), as gnn_action_logp gives them, 0 for rows left out: the
- * old_logp of gnn_policy_loss.  Workspace: gnn_sample_workspace_bytes (0 up to
- * 32,768 columns, some 50 KB a row beyond).
+ * old_logp of gnn_policy_loss (where T is not 1 or something is cut off, not the
+ * probability with which the action was drawn).  Workspace:
+ * gnn_sample_workspace_bytes (0 up to 32,768 columns, some 50 KB a row beyond).
  *
  * gnn_top_logits: the first k entries of each row's order (1 <= k <=
  * GNN_TOP_MOST), with T > 0:
@@ -489,7 +490,8 @@ gnn_status gnn_policy_loss(int32_t n, int32_t C, const float* Z, int64_t ld_z,
  * a row's logits shows in its kl and gradient.  Columns of dZ's rows past C are
  * not written; kl (n floats) and dZ (stride ld_dz) may be NULL.  n = 0 gives
  * out = 0.  Exponentials of the row are fp32's, everything of the list is in
- * double, and so are all sums.  Workspace: gnn_distill_workspace_bytes.
+ * double, and so are all sums: kl is good to T^2 (6 ln C + 24) 2^-24 and its
+ * rounding.  Workspace: gnn_distill_workspace_bytes.
  *
  * For all three: results are bit-reproducible, and no output may overlap an
  * input, another output or the workspace. */

@@ -8,10 +8,10 @@
 // caches.  Top logits read it once, and the first k of each part go on.  Sums
 // over parts are of whole numbers, or in a fixed order.
 //
-// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 51 us
+// Bound by launches and their latency: 64 x 131,071 with top-k and top-p 52 us
 // in five launches of 3 to 15 us (86 with the first 1,025, in ten), without a
-// border 24 to 28 us in three; 1 x 131,071 14 us without, 45 with top-p (one block
-// a row 56 and 179), 30 with top-k and top-p.  500 x 65,536 without a border 75 us,
+// border 28 us in three; 1 x 131,071 14 us without, 46 with top-p (one block
+// a row 56 and 179), 29 with top-k and top-p.  500 x 65,536 without a border 76 us,
 // 64 x 131,071's first 256 37.
 #include "choose.hpp"
 

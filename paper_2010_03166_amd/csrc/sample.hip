@@ -9,11 +9,12 @@
 // threads with eight chunks, past 24,576 columns, have 22 registers on the stack.)
 //
 // Bound by instructions where the rows are many: 16,384 x 2,048 with top-p takes
-// 101 us, 3,190 vector instructions a wavefront of 2,048 entries, and the vector
-// units issue in nine of ten cycles (the bytes take 27 us); without a border 48.
+// 100 us, 3,190 vector instructions a wavefront of 2,048 entries, and the vector
+// units issue in nine of ten cycles (the bytes take 27 us); without a border 52,
+// the best action alone (T = 0) 31.
 // 50,001 x 121 with top-k, top-p, min-p 39 us (the bytes 5): LDS where the first
 // 20 are compared.  Where they are few, by one row's latency beside the launch:
-// 8,000 x 41 6.9 us, 1 x 2,048 7.2.
+// 8,000 x 41 6.7 us, 1 x 2,048 6.8.
 #include "choose.hpp"
 
 using namespace gnnprop;
@@ -234,7 +235,7 @@ void sample_kernel(SampleArgs a) {
 // Rows of up to 24 columns, 65,536 of them or more: a lane has one to itself, and
 // what comes before an entry is told by comparing it with every other one (no
 // bins, nothing but the exponentials' table in LDS).  200,000 x 7 with top-p 21
-// us by teams, 8 so; 200,000 x 16 40 and 20; 200,000 x 32 34 and 51.
+// us by teams, 7 so; 200,000 x 16 40 and 19; 200,000 x 32 34 and 51.
 template <int V>
 __global__ __launch_bounds__(256) void sample_small_kernel(SampleArgs a) {
   constexpr int N = 4 * V;

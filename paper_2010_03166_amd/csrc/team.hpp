@@ -11,7 +11,7 @@
 // holds the border are put in order.  Bins are so many that a few entries lie in
 // one where logits are spread; where they are not (equal logits, logits at the
 // type's lowest value beside others) the bin's entries are searched from memory:
-// 16,384 x 2,048 equal logits with top-p 312 us instead of 101.
+// 16,384 x 2,048 equal logits with top-p 309 us instead of 100.
 #pragma once
 
 #include <type_traits>

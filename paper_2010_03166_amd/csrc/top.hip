@@ -5,9 +5,9 @@
 // for the exponentials of both parts and the list of the first k, in LDS in the
 // place of the bins, where each entry's place is the number of those before it.
 // Bound by instructions, some 1,680 a wavefront of 2,048 entries with k = 64:
-// 16,384 x 2,048 51 us (the bytes take 28), k = 8 41, k = 256 137, where the
+// 16,384 x 2,048 51 us (the bytes take 28), k = 8 45, k = 256 135, where the
 // comparisons of the list's entries with each other are most of it.  2,000 x
-// 20,011, k = 128: 75 us in two launches (63 + 16; the bytes 32).
+// 20,011, k = 128: 74 us in two launches (63 + 16; the bytes 32).
 #include "choose.hpp"
 
 using namespace gnnprop;

@@ -660,8 +660,9 @@ class Trainer:
             top_p: float = 1.0, min_p: float = 0.0, stream=None):
         """Draws each row's action under the present weights by its random
         number (u: n floats in [0, 1)), as gnn_sample_actions does: (actions,
-        int32, their log-probabilities under the whole policy), new tensors, for
-        policy_step's actions and old_logp.  stream: as in action_logp."""
+        int32, their log-probabilities under the whole policy at temperature 1,
+        whatever they were drawn with), new tensors, for policy_step's actions and
+        old_logp.  stream: as in action_logp."""
         self._per_row("u", u)
         _, _, Z, ld = self._logits(X, stream)
         actions = self._new((self.n,), torch.int32, stream)
